@@ -293,12 +293,11 @@ def plain_attend(st):
 
 
 def plain_rows(x):
-    """8-bit codes of each row, and what one level stands for."""
-    v = x.float()
+    """8-bit codes of each row, and what one level stands for. In 64 bits: half the maximum lies between two codes."""
+    v = x.double()
     top = v.abs().amax(-1, keepdim=True)
-    fine = top >= 127 * 2.0 ** -126
-    codes = torch.round(v * torch.where(fine, 127 / top, torch.zeros_like(top))).clamp(-127, 127).to(torch.int8)
-    return codes, torch.where(fine, top / 127, torch.zeros_like(top)).squeeze(-1)
+    codes = torch.round(v * 127 / top).to(torch.int8)
+    return codes, (top / 127).float().squeeze(-1)
 
 
 def run(st):
