@@ -76,6 +76,9 @@ extern "C" {
 #define QSGD_ERR_KIND (-8)      /* unknown norm_kind or code_kind                     */
 #define QSGD_ERR_NO_DEVICE (-9) /* no usable CUDA device / kernel image for this GPU  */
 #define QSGD_ERR_SCRATCH (-10)  /* problem too large for the library's built-in scratch */
+#define QSGD_ERR_LAYOUT (-11)   /* cache: head size, page size, heads or strides      */
+#define QSGD_ERR_TYPE (-12)     /* an element type that the call does not take        */
+#define QSGD_ERR_SHAPE (-13)    /* a matrix or a number of rows or sequences out of range */
 
 /* Size of the scratch array built into the library for qsgd_encode_elias_static. */
 #define QSGD_STATIC_SCRATCH_BYTES (32u << 20)
@@ -86,6 +89,7 @@ extern "C" {
 #define QSGD_DEV_LEVEL 8u     /* a decoded level lies outside [1, s]                   */
 #define QSGD_DEV_TABLE 16u    /* offset table not ascending / bucket shorter than 32   */
 #define QSGD_DEV_TIMEOUT 32u  /* a bounded wait inside a kernel gave up                */
+#define QSGD_DEV_PAGE 64u     /* a length, a row range or a page number that the cache has not */
 
 typedef void* qsgd_stream_t; /* a cudaStream_t; NULL is the default stream */
 
@@ -321,6 +325,127 @@ int qsgd_policy_decode_sgd_step(const void* const* msgs, const uint64_t* const* 
                                 const uint64_t* payload_bytes, uint32_t K, const qsgd_policy* plan,
                                 uint32_t bucket, uint32_t s, int code_kind, float* x, float eta,
                                 uint32_t* status_dev, qsgd_stream_t stream);
+
+/*
+ * Few-bit values outside the gradient exchange. (The paper has no counterpart: buckets with a scale of
+ * their own, Section 4, rounded to the nearest level instead of at random.) A model that answers keeps
+ * its weights in 8 bits and the keys and values of what it has read in 4; these calls quantise them
+ * and work on the packed form.
+ */
+#define QSGD_TYPE_F32 0
+#define QSGD_TYPE_F16 1
+#define QSGD_TYPE_BF16 2
+
+/*
+ * A cache of keys and values in 4 bits. 64 neighbouring values of a token and head form a bucket with
+ * two numbers of the cache's type (F16 or BF16): lo, the smallest value (+0 for a zero of either sign), and step, the smallest number
+ * of the type with 15 * step >= largest - smallest. A value x is held as c in 0 .. 15, the nearest to
+ * (x - lo) / step, the lower one of two as near, and stands for lo + step * c: at most step / 2 away. A bucket that
+ * holds a value that is not finite, or whose span is beyond fp32, stands for NaN throughout; one whose step would lie below
+ * 2^-126 stands for lo.
+ *
+ * Tokens lie in pages of page_tokens (a multiple of 16). Head h of page i begins at data +
+ * i * page_stride + h * head_stride and holds page_tokens / 16 tiles of 18 * head_dim bytes, each
+ *   key codes [head_dim / 64][16 tokens][32 bytes] | key pairs [16][head_dim / 64] (lo, step)
+ *   | value codes | value pairs, likewise;
+ * code i of a bucket: bits [4 * (i % 8), +4) of u32 word i / 8.
+ *   data         16-byte aligned, page_stride and head_stride multiples of 16 bytes such that no two
+ *                (page, head) overlap; nothing needs clearing
+ *   head_dim     64, 128, 192 or 256
+ */
+typedef struct {
+  void* data;           /* device */
+  uint64_t n_pages;
+  uint64_t page_stride; /* bytes */
+  uint64_t head_stride; /* bytes */
+  uint32_t page_tokens;
+  uint32_t heads;       /* of keys and values */
+  uint32_t head_dim;
+  int type;             /* QSGD_TYPE_F16 or QSGD_TYPE_BF16: of lo and step, and of what goes in and comes out */
+} qsgd_cache;
+
+/*
+ * Which tokens a call deals with. Sequence b has lengths[b] tokens in the cache, those of the call
+ * included; its token p lies in page table[b * table_stride + p / page_tokens]. Rows
+ * [starts[b], starts[b + 1]) of the call's arrays are its last tokens, in order; with starts NULL every
+ * sequence has one row, its last token. Rows that belong to no sequence (behind starts[sequences]) are
+ * neither read nor written. A length beyond the table's row or below zero, rows that do not ascend inside [0, rows], or a
+ * page number outside [0, n_pages) raise QSGD_DEV_PAGE; what the call does for that sequence (for starts that
+ * do not ascend: for any row) is then unspecified, inside its buffers.
+ */
+typedef struct {
+  const int32_t* table;   /* device, [sequences][table_stride], the first table_pages of each row in use */
+  uint64_t table_stride;
+  uint32_t table_pages;
+  uint32_t sequences;
+  const int32_t* lengths; /* device, [sequences] */
+  const int32_t* starts;  /* device, [sequences + 1], or NULL (then rows == sequences) */
+  uint64_t rows;
+} qsgd_cache_rows;
+
+/* Bytes of one page whose heads lie one after another (page_stride of such a cache; head_stride is this / heads). 0 for sizes that are not taken. */
+size_t qsgd_cache_page_bytes(uint32_t page_tokens, uint32_t heads, uint32_t head_dim);
+
+/*
+ * Quantise into the cache, and read back. k and v are [rows][heads][head_dim] of the cache's type,
+ * 16-byte aligned, the last axis contiguous, the strides of the others given in elements (multiples of
+ * 8). Rows in front of a sequence's first token (more rows than tokens) are not written, and read back
+ * as zero. Two rows of one write must not have the same place in the cache. Reads round lo + step * c to the type once.
+ */
+int qsgd_cache_write(const qsgd_cache* cache, const qsgd_cache_rows* rows, const void* k, uint64_t k_row_stride,
+                     uint64_t k_head_stride, const void* v, uint64_t v_row_stride, uint64_t v_head_stride,
+                     uint32_t* status_dev, qsgd_stream_t stream);
+int qsgd_cache_read(const qsgd_cache* cache, const qsgd_cache_rows* rows, void* k, uint64_t k_row_stride,
+                    uint64_t k_head_stride, void* v, uint64_t v_row_stride, uint64_t v_head_stride,
+                    uint32_t* status_dev, qsgd_stream_t stream);
+
+/*
+ * Attention over the cache: each row is a query of q_heads heads (a multiple of the cache's heads; query
+ * head h uses key head h / (q_heads / heads)) at the position of its token, and sees the tokens up to its own:
+ *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q . k_t),  lse = ln sum_t p_t
+ * over what the cache stands for. A row that sees no token (an empty sequence, or a row in front of the first
+ * token) gives 0 and -infinity.
+ *   q, out       [rows][q_heads][head_dim] as k and v above; scores, sums and the output are kept in fp32,
+ *                p in 16 bits of fraction, the output is rounded to the type once
+ *   lse          [rows][q_heads] fp32, contiguous, or NULL
+ *   workspace    qsgd_cache_attend_workspace_bytes() of scratch, 16-byte aligned. Every part that is read was
+ *                written by the same call, so nothing needs clearing; calls that overlap on the GPU need one each.
+ */
+size_t qsgd_cache_attend_workspace_bytes(const qsgd_cache* cache, uint32_t q_heads);
+int qsgd_cache_attend(const qsgd_cache* cache, const qsgd_cache_rows* rows, const void* q, uint64_t q_row_stride,
+                      uint64_t q_head_stride, uint32_t q_heads, float scale, void* out, uint64_t out_row_stride,
+                      uint64_t out_head_stride, float* lse, void* workspace, uint32_t* status_dev, qsgd_stream_t stream);
+
+/*
+ * Products in 8-bit integers with a scale for each row of either operand.
+ *
+ * qsgd_quantize_rows: a row x becomes scale = max|x| / 127 and int8 codes, the whole numbers nearest to
+ * x * 127 / max|x| (ties to even).
+ * A row with max|x| below 127 * 2^-126 becomes scale 0 and zeros; one that holds a value that is not finite becomes
+ * scale NaN and zeros, so that whatever is computed from it is NaN.
+ *   x            [rows][cols] of `type` (F32, F16 or BF16), row_stride elements apart
+ *   codes        int8, codes_stride bytes apart (at least cols); bytes behind a row's codes are left as they were
+ *   scale        [rows] fp32
+ *
+ * qsgd_matmul_i8: out[m][n] = (sum_k a[m][k] * b[n][k]) * a_scale[m] * b_scale[n] + bias[n]; the sum is exact in 32 bits, the rest in
+ * fp32 in this order, rounded to `type` once. b has a row for each output channel, as a linear layer's weight.
+ *   cols         1 to 131071 (beyond, 32 bits could overflow); rows and channels below 2^31; either may be 0
+ *   strides      in elements. Rows that begin on 16-byte boundaries (base and stride multiples of 16 bytes) are read by bulk
+ *                copies; others are taken too, more slowly
+ *   bias         [n] fp32 or NULL
+ *
+ * qsgd_linear_i8: the two in one call, for activations that are quantised on the way (x W^T). workspace:
+ * qsgd_linear_i8_workspace_bytes() of scratch, 16-byte aligned, nothing to clear; calls that overlap on the GPU need one each.
+ */
+int qsgd_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row_stride, int type, int8_t* codes,
+                       uint64_t codes_stride, float* scale, qsgd_stream_t stream);
+int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, const int8_t* b, uint64_t b_stride,
+                   const float* b_scale, const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out,
+                   uint64_t out_stride, int type, qsgd_stream_t stream);
+size_t qsgd_linear_i8_workspace_bytes(uint64_t m, uint32_t cols);
+int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w, uint64_t w_stride, const float* w_scale,
+                   const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int out_type,
+                   void* workspace, qsgd_stream_t stream);
 
 /*
  * Per-kernel timing (measurement aid; the paper has no counterpart). While enabled, every

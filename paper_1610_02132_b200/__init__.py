@@ -7,4 +7,7 @@ from .binding import (CODE_ELIAS, CODE_ELIAS_DENSE, CODE_FIXED, NORM_L2, NORM_MA
                       qsgd_sgd_step, qsgd_static_scratch_bytes, qsgd_workspace_bytes,
                       Policy, qsgd_policy_decode_accumulate, qsgd_policy_decode_sgd_step,
                       qsgd_policy_encode, qsgd_policy_message_capacity, qsgd_policy_workspace_bytes,
-                      qsgd_test_default_wait_polls, qsgd_test_set_wait_polls, qsgd_set_launch_chaining)
+                      qsgd_test_default_wait_polls, qsgd_test_set_wait_polls, qsgd_set_launch_chaining,
+                      DEV_PAGE, Cache, qsgd_cache_attend, qsgd_cache_attend_workspace_bytes, qsgd_cache_page_bytes,
+                      qsgd_cache_read, qsgd_cache_write, qsgd_linear_i8, qsgd_linear_i8_workspace_bytes, qsgd_matmul_i8,
+                      qsgd_quantize_rows, quantize_rows_alloc)

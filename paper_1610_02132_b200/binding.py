@@ -18,6 +18,9 @@ NORM_L2, NORM_MAX = 0, 1
 CODE_FIXED, CODE_ELIAS, CODE_ELIAS_DENSE = 0, 1, 2
 
 DEV_CAPACITY, DEV_OVERRUN, DEV_POSITION, DEV_LEVEL, DEV_TABLE, DEV_TIMEOUT = 1, 2, 4, 8, 16, 32
+DEV_PAGE = 64
+
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 EXPORTS = ["qsgd_message_capacity", "qsgd_workspace_bytes", "qsgd_fixed_layout", "qsgd_encode",
            "qsgd_decode_accumulate", "qsgd_sgd_step", "qsgd_decode_sgd_step",
@@ -28,7 +31,9 @@ EXPORTS = ["qsgd_message_capacity", "qsgd_workspace_bytes", "qsgd_fixed_layout",
            "qsgd_policy_plan_sizes", "qsgd_policy_plan", "qsgd_policy_message_capacity",
            "qsgd_policy_workspace_bytes", "qsgd_policy_encode", "qsgd_policy_decode_accumulate",
            "qsgd_policy_decode_sgd_step", "qsgd_test_set_wait_polls", "qsgd_test_default_wait_polls",
-           "qsgd_set_launch_chaining"]
+           "qsgd_set_launch_chaining", "qsgd_cache_page_bytes", "qsgd_cache_write", "qsgd_cache_read",
+           "qsgd_cache_attend_workspace_bytes", "qsgd_cache_attend", "qsgd_quantize_rows", "qsgd_matmul_i8",
+           "qsgd_linear_i8_workspace_bytes", "qsgd_linear_i8"]
 
 _lib = None
 
@@ -42,6 +47,18 @@ class PolicyStruct(C.Structure):
     _fields_ = [("bucket_src", C.c_void_p), ("bucket_len", C.c_void_p), ("n_buckets", C.c_uint64),
                 ("raw_src", C.c_void_p), ("raw_start", C.c_void_p), ("n_raw_segments", C.c_uint64),
                 ("n_raw", C.c_uint64), ("n", C.c_uint64), ("quads", C.c_uint32)]
+
+
+class CacheStruct(C.Structure):
+    """qsgd_cache of include/qsgd.h."""
+    _fields_ = [("data", C.c_void_p), ("n_pages", C.c_uint64), ("page_stride", C.c_uint64), ("head_stride", C.c_uint64),
+                ("page_tokens", C.c_uint32), ("heads", C.c_uint32), ("head_dim", C.c_uint32), ("type", C.c_int)]
+
+
+class CacheRowsStruct(C.Structure):
+    """qsgd_cache_rows of include/qsgd.h."""
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_uint64), ("table_pages", C.c_uint32), ("sequences", C.c_uint32),
+                ("lengths", C.c_void_p), ("starts", C.c_void_p), ("rows", C.c_uint64)]
 
 
 def lib():
@@ -100,6 +117,25 @@ def lib():
         L.qsgd_policy_decode_sgd_step.argtypes = [C.POINTER(vp), C.POINTER(vp), pu64, u32, pp, u32, u32,
                                                   C.c_int, vp, C.c_float, vp, vp]
         L.qsgd_policy_decode_sgd_step.restype = C.c_int
+        pc, pr = C.POINTER(CacheStruct), C.POINTER(CacheRowsStruct)
+        L.qsgd_cache_page_bytes.argtypes = [u32, u32, u32]
+        L.qsgd_cache_page_bytes.restype = sz
+        L.qsgd_cache_write.argtypes = [pc, pr, vp, u64, u64, vp, u64, u64, vp, vp]
+        L.qsgd_cache_write.restype = C.c_int
+        L.qsgd_cache_read.argtypes = L.qsgd_cache_write.argtypes
+        L.qsgd_cache_read.restype = C.c_int
+        L.qsgd_cache_attend_workspace_bytes.argtypes = [pc, u32]
+        L.qsgd_cache_attend_workspace_bytes.restype = sz
+        L.qsgd_cache_attend.argtypes = [pc, pr, vp, u64, u64, u32, C.c_float, vp, u64, u64, vp, vp, vp, vp]
+        L.qsgd_cache_attend.restype = C.c_int
+        L.qsgd_quantize_rows.argtypes = [vp, u64, u32, u64, C.c_int, vp, u64, vp, vp]
+        L.qsgd_quantize_rows.restype = C.c_int
+        L.qsgd_matmul_i8.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp]
+        L.qsgd_matmul_i8.restype = C.c_int
+        L.qsgd_linear_i8_workspace_bytes.argtypes = [u64, u32]
+        L.qsgd_linear_i8_workspace_bytes.restype = sz
+        L.qsgd_linear_i8.argtypes = [vp, u64, C.c_int, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp, vp]
+        L.qsgd_linear_i8.restype = C.c_int
         L.qsgd_set_launch_chaining.argtypes = [C.c_int]
         L.qsgd_set_launch_chaining.restype = C.c_int
         L.qsgd_test_set_wait_polls.argtypes = [u32]
@@ -308,6 +344,80 @@ def qsgd_policy_decode_sgd_step(msgs, tables, plan, s, code_kind, x, eta, status
     _covered(x, "x", plan)
     _check(_native.policy_decode(msgs, tables, payload_bytes, C.addressof(plan.struct), plan.bucket, s, code_kind, x, eta,
                                  status_dev, stream))
+
+
+# ------------------------------- few-bit values outside the gradient exchange -----------------
+def qsgd_cache_page_bytes(page_tokens, heads, head_dim):
+    return int(lib().qsgd_cache_page_bytes(page_tokens, heads, head_dim))
+
+
+class Cache:
+    """A 4-bit cache of keys and values (qsgd_cache): its memory, [pages, heads, bytes of a page and head] in uint8, and what
+    the calls have to know of it. `data` may be given: any strides, as long as the last dimension is contiguous."""
+
+    def __init__(self, n_pages, page_tokens, heads, head_dim, dtype=torch.bfloat16, device="cuda", data=None):
+        page = qsgd_cache_page_bytes(page_tokens, heads, head_dim)
+        if not page or dtype not in (torch.float16, torch.bfloat16) or n_pages < 1:
+            raise QsgdError("a cache has at least one page, of a multiple of 16 tokens, with heads of 64, 128, 192 or 256 "
+                            "numbers in float16 or bfloat16")
+        if data is None:
+            data = torch.empty(n_pages, heads, page // heads, dtype=torch.uint8, device=device)
+        if data.dtype != torch.uint8 or tuple(data.shape) != (n_pages, heads, page // heads) or data.stride(2) != 1:
+            raise QsgdError("data must be uint8, [%d, %d, %d], contiguous along its last dimension" % (n_pages, heads, page // heads))
+        self.data, self.dtype = data, dtype
+        self.n_pages, self.page_tokens, self.heads, self.head_dim = n_pages, page_tokens, heads, head_dim
+        self.struct = CacheStruct(data.data_ptr(), n_pages, data.stride(0), data.stride(1), page_tokens, heads, head_dim, TYPES[dtype])
+        self.address = C.addressof(self.struct)
+
+
+def qsgd_cache_write(cache, table, lengths, k, v, status_dev, starts=None, stream=None):
+    """Quantises k and v, [rows, heads, head_dim], into the cache: the last tokens of every sequence (one each, or rows
+    starts[b] to starts[b + 1]). table [sequences, pages], lengths (these tokens included) and starts are int32."""
+    _check(_native.cache_store(True, cache.address, cache.data, table, lengths, starts, k, v, status_dev, stream))
+
+
+def qsgd_cache_read(cache, table, lengths, k, v, status_dev, starts=None, stream=None):
+    """Reads the last tokens of every sequence back into k and v; arguments as qsgd_cache_write."""
+    _check(_native.cache_store(False, cache.address, cache.data, table, lengths, starts, k, v, status_dev, stream))
+
+
+def qsgd_cache_attend_workspace_bytes(cache, q_heads):
+    return int(lib().qsgd_cache_attend_workspace_bytes(C.byref(cache.struct), q_heads))
+
+
+def qsgd_cache_attend(cache, table, lengths, q, out, workspace, status_dev, starts=None, scale=None, lse=None, stream=None):
+    """out <- attention of q, [rows, q_heads, head_dim], over the cache: a row sees the tokens up to its own. scale defaults
+    to 1 / sqrt(head_dim); lse, [rows, q_heads] in fp32, receives the logarithm of the sum of exponentials."""
+    _check(_native.cache_attend(cache.address, cache.data, table, lengths, starts, q, out, workspace, status_dev, scale, lse, stream))
+
+
+def qsgd_quantize_rows(x, codes, scale, stream=None):
+    """Rows of x (fp32, fp16 or bf16) as int8 codes and an fp32 scale each."""
+    _check(_native.quantize_rows(x, codes, scale, stream))
+
+
+def qsgd_matmul_i8(a, a_scale, b, b_scale, out, bias=None, stream=None):
+    """out <- (a b^T) * a_scale[:, None] * b_scale + bias, for int8 a and b; the sum is exact."""
+    _check(_native.matmul_i8(a, a_scale, b, b_scale, out, bias, stream))
+
+
+def qsgd_linear_i8_workspace_bytes(rows, cols):
+    return int(lib().qsgd_linear_i8_workspace_bytes(rows, cols))
+
+
+def qsgd_linear_i8(x, w, w_scale, out, workspace, bias=None, stream=None):
+    """out <- x w^T + bias with the rows of x quantised on the way; w and w_scale as qsgd_quantize_rows leaves them."""
+    _check(_native.linear_i8(x, w, w_scale, out, workspace, bias, stream))
+
+
+def quantize_rows_alloc(x, stream=None):
+    """Allocates codes whose rows begin on 16-byte boundaries (what the products read fastest) and scales, then calls
+    qsgd_quantize_rows. Returns (codes, scale)."""
+    rows, cols = x.shape
+    codes = torch.zeros(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=x.device)[:, :cols]
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    qsgd_quantize_rows(x, codes, scale, stream)
+    return codes, scale
 
 
 # ------------------------------- conveniences (allocation only) -----------------------------

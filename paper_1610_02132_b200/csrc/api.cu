@@ -65,7 +65,8 @@ static const char* const kKernelNames[kKernCount] = {
     "quantize_fixed", "quantize_tail", "decode_fixed", "sgd_step", "elias_length",
     "elias_scatter", "decode_elias", "decode_elias_sparse", "raw_gather", "raw_decode",
     "decode_elias_teams", "decode_elias_fields", "decode_elias_bytes",
-    "decode_elias_dense"};
+    "decode_elias_dense", "cache_write", "cache_read", "cache_attend", "cache_join", "quantize_rows", "matmul_i8",
+    "matmul_i8_few"};
 
 namespace {
 
@@ -392,6 +393,9 @@ const char* qsgd_status_string(int status) {
     case QSGD_ERR_KIND: return "unknown norm or code kind";
     case QSGD_ERR_NO_DEVICE: return "no usable CUDA device";
     case QSGD_ERR_SCRATCH: return "problem too large for the built-in scratch array";
+    case QSGD_ERR_LAYOUT: return "head size, page size, heads or strides outside what the cache takes";
+    case QSGD_ERR_TYPE: return "element type not taken here";
+    case QSGD_ERR_SHAPE: return "a matrix or a number of rows or sequences is outside what is taken";
     default: return status > 0 ? cudaGetErrorString((cudaError_t)status) : "unknown status";
   }
 }

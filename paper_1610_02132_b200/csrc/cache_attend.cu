@@ -1,0 +1,622 @@
+// Attention over the 4-bit cache.
+//
+// For a query row q (one head of one query), with keys k_t = lo + step * c_t (a group g of 64 coordinates has its own pair):
+//   s_t = sum_g step_tg * (q_g . c_tg) + lo_tg * sum(q_g),   p_t = 2^(a s_t - m),   a = scale * log2(e),
+//   o   = (sum_t p_t v_t) / sum_t p_t,    sum_t p_t v_tg = sum_t (p_t step_tg) (c_tg - 8) + sum_t p_t (lo_tg + 8 step_tg).
+// The codes go to the tensor cores as they are (integers of four bits are exact in the operand types), the pairs are applied in fp32:
+//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, q's own type, fp32 sums);
+//            a code reaches the operand as 128 + c (bf16) or 16 + c (fp16), a mask and an or on the packed word, and the constant
+//            times sum(q_g) is taken off afterwards;
+//   output   A = (c - 8) of 16 coordinates x 16 tokens, B = p * step as the sum of two bf16 numbers (16 bits of p: one bf16 would
+//            put as much error into the output as rounding the output itself does). Codes are centred here because these sums run over the
+//            whole sequence and the constant part would bury them.
+// The rows of a score tile are permuted (kToken) so that the transpose of p between the two products is one movmatrix, and reads
+// of codes from shared memory meet no bank twice.
+//
+// What bounds it: with up to 8 rows a key head, HBM: 9/8 * head_dim bytes a token and head, each read once, against about 150
+// integer and 24 tensor instructions per 16 tokens. So everything is arranged around the stream of tiles. The tiles of all (sequence, key
+// head, row tile) segments form one line of units; CTA i takes the i-th of equal stretches of it, whatever the lengths are, and warp w of a CTA every
+// eighth tile of a piece, through a ring of its own that bulk copies fill. A piece that is a whole segment is written out; the
+// others leave (m, sum, o) in the workspace, at most two a CTA, and a second kernel joins them, a CTA for each boundary and row.
+#include "cache.cuh"
+
+namespace qsgd {
+
+namespace {
+
+constexpr uint32_t kWarps = 8, kThreads = 32 * kWarps;
+constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
+constexpr uint32_t kLeastChunk = kWarps;  // units of a stretch: a tile for each warp
+constexpr uint32_t kMostRowTile = 16;
+constexpr uint32_t kPolls = 1u << 22;
+constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that differences of maxima are numbers
+
+struct JoinInfo {                         // of the piece that a CTA begins with, written by every CTA of every call
+  uint32_t parts;                         // CTAs from `first` on hold a part of the segment; 0: nothing to join at this boundary
+  uint32_t first, first_slot;             // the segment's first part
+  uint32_t head, row0, rows;              // first row (query * group + head in group) of the row tile, rows in it
+  uint32_t start;                         // first query row of the sequence
+  uint32_t unused;
+};
+
+struct AttendParams {
+  CacheView c;
+  const uint16_t* q;
+  uint16_t* out;
+  uint64_t q_token, q_head, out_token, out_head;
+  float* lse;
+  uint32_t q_heads, group;
+  float scale_log2;
+  JoinInfo* join;
+  float* parts;                           // [CTA][2][rows * (dim + 2)]
+};
+
+__host__ __device__ constexpr size_t part_floats(uint32_t rows, uint32_t dim) { return (size_t)rows * (dim + 2); }
+
+// Token of a tile that row r (of 8) of a score tile stands for; rows 8 .. 15 are the same behind 8. Lane (g, t) of a warp reads key
+// codes of token kToken[g] and value codes of tokens kToken[2 t] and kToken[2 t + 1]: both sets of four rows of 32 bytes that go
+// together differ modulo 4.
+__device__ __forceinline__ uint32_t token_of(uint32_t r) { return (0x57463120u >> (4 * r)) & 7u; }
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+
+__device__ __forceinline__ void copy_tile(uint32_t dst, const uint8_t* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar) : "memory");
+}
+
+template <int TYPE>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (TYPE == QSGD_TYPE_BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+__device__ __forceinline__ float exp2_approx(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// Nibbles s of the two halves of a word as operands: kBias + code.
+template <int TYPE>
+struct KeyCode;
+template <>
+struct KeyCode<QSGD_TYPE_BF16> {          // 128 + c: the code in the last four of seven fraction bits
+  static constexpr float kBias = 128.0f;
+  static __device__ __forceinline__ uint32_t operand(uint32_t w, int s) { return ((w >> (4 * s)) & 0x000f000fu) | 0x43004300u; }
+};
+template <>
+struct KeyCode<QSGD_TYPE_F16> {           // 16 + c: the code in the first four of ten fraction bits (1024 + c would cost ten bits of the sum)
+  static constexpr float kBias = 16.0f;
+  static __device__ __forceinline__ uint32_t operand(uint32_t w, int s) {
+    return ((s < 2 ? w << (6 - 4 * s) : w >> (4 * s - 6)) & 0x03c003c0u) | 0x4c004c00u;
+  }
+};
+
+__device__ __forceinline__ uint32_t value_operand(uint32_t w, int s) {       // c - 8 in bf16, exact
+  const uint32_t biased = ((w >> (4 * s)) & 0x000f000fu) | 0x43004300u;
+  __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&biased), __floats2bfloat162_rn(136.0f, 136.0f));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+
+// One sequence on the line of units.
+struct Sequence {
+  uint32_t b, start, n, tiles, row_tiles;
+  int64_t length;
+  uint64_t units;
+};
+template <int ROWS>
+__device__ __forceinline__ Sequence sequence_at(const AttendParams& p, uint32_t b) {
+  bool bad;
+  const SequenceRows s = rows_of(p.c, b, &bad);
+  if (bad) atomicOr(p.c.status, QSGD_DEV_PAGE);
+  Sequence q;
+  q.b = b; q.start = s.start; q.n = s.n; q.length = s.length;
+  q.tiles = (uint32_t)((s.length + kCacheTile - 1) / kCacheTile);
+  if (q.tiles == 0) q.tiles = 1;          // nothing to attend to: a unit that writes the empty result
+  q.row_tiles = (s.n * p.group + ROWS - 1) / ROWS;
+  q.units = (uint64_t)p.c.heads * q.row_tiles * q.tiles;
+  return q;
+}
+
+template <int TYPE, int D, int NT>
+struct Shape {
+  static constexpr int kRows = 8 * NT, kGroups = D / 64;
+  static constexpr uint32_t kTileBytes = 18 * D;
+  // Ring stages of a warp: about 9 KB of tiles in flight at NT = 1 (two CTAs an SM: 150 KB), and room for the warp's part of the join.
+  static constexpr uint32_t kStages = D == 64 ? 8 : D == 128 ? 4 : 3;
+  static constexpr uint32_t kRing = kStages * kTileBytes;
+  static constexpr uint32_t kRowFloats = D + 8;                             // of the join: rows shifted by 8 banks
+  static constexpr uint32_t kPart = kRows * kRowFloats * 4;
+  static constexpr uint32_t kPerWarp = ((kRing > kPart ? kRing : kPart) + 127) / 128 * 128;
+  static constexpr uint32_t kSmem = kWarps * kPerWarp;
+  static constexpr int kCtas = D <= 128 && NT == 1 ? 2 : 1;
+};
+
+template <int TYPE, int D, int NT>
+__global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_attend_kernel(const __grid_constant__ AttendParams p) {
+  using S = Shape<TYPE, D, NT>;
+  constexpr int J = S::kGroups, R = S::kRows;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t bars[kWarps][S::kStages];
+  __shared__ uint64_t scan[kWarps];
+  __shared__ uint64_t found_base;
+  __shared__ uint32_t found_b;
+  __shared__ float part_m[kWarps][R], part_l[kWarps][R];
+
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, t = lane & 3u;
+  uint8_t* const ring = smem + warp * S::kPerWarp;
+  const uint32_t ring_u32 = smem_u32(ring), bar_u32 = smem_u32(&bars[warp][0]);
+  if (lane == 0) {
+#pragma unroll
+    for (uint32_t s = 0; s < S::kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_u32 + 8 * s) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  chain_wait();
+
+  // ---- this CTA's stretch of the line of units, and the sequence that it begins in -------------------------------------
+  uint64_t total = 0;
+  for (uint32_t b = tid; b < p.c.sequences; b += kThreads) total += sequence_at<R>(p, b).units;
+#pragma unroll
+  for (int m = 16; m; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
+  if (lane == 0) scan[warp] = total;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kWarps; ++w) total += scan[w];
+  uint64_t chunk = (total + gridDim.x - 1) / gridDim.x;
+  if (chunk < kLeastChunk) chunk = kLeastChunk;
+  const uint64_t u0 = blockIdx.x * chunk, u1 = u0 + chunk < total ? u0 + chunk : total;
+  if (u0 >= total) {
+    if (tid == 0) p.join[blockIdx.x].parts = 0;
+    return;
+  }
+  uint64_t base = 0;
+  for (uint32_t b0 = 0;; b0 += kThreads) {                 // ends: u0 < total
+    const uint64_t mine = b0 + tid < p.c.sequences ? sequence_at<R>(p, b0 + tid).units : 0;
+    uint64_t sum = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const uint64_t up = __shfl_up_sync(0xffffffffu, sum, m);
+      if (lane >= (uint32_t)m) sum += up;
+    }
+    __syncthreads();
+    if (lane == 31) scan[warp] = sum;
+    __syncthreads();
+    uint64_t here = base, all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) {
+      if (w < warp) here += scan[w];
+      all += scan[w];
+    }
+    here += sum - mine;
+    if (here <= u0 && u0 < here + mine) { found_base = here; found_b = b0 + tid; }
+    base += all;
+    if (base > u0) break;
+  }
+  __syncthreads();
+
+  Sequence seq = sequence_at<R>(p, found_b);
+  uint64_t seq_base = found_base;
+  uint32_t phases = 0;                                      // bit s: parity of the next wait on stage s
+  bool timed_out = false;
+
+  for (uint64_t u = u0; u < u1;) {
+    while (u >= seq_base + seq.units) {                     // (a sequence without rows has no units)
+      seq_base += seq.units;
+      seq = sequence_at<R>(p, seq.b + 1);
+    }
+    const uint64_t off = u - seq_base;
+    const uint64_t segment = off / seq.tiles;
+    const uint32_t tile0 = (uint32_t)(off - segment * seq.tiles);
+    const uint32_t tile1 = u1 - u < seq.tiles - tile0 ? tile0 + (uint32_t)(u1 - u) : seq.tiles;
+    const uint32_t head = (uint32_t)(segment / seq.row_tiles), row_tile = (uint32_t)(segment - (uint64_t)head * seq.row_tiles);
+    const uint32_t row0 = row_tile * R, rows_all = seq.n * p.group;
+    const uint32_t rows = rows_all - row0 < (uint32_t)R ? rows_all - row0 : (uint32_t)R;
+
+    // ---- queries: operands, sums of each group, and how far each row sees ------------------------------------------------
+    uint32_t qf[NT][J][4][2];
+    float qsum[NT][J][2];
+    int32_t see[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint32_t r = 8 * nt + g;
+      const bool live = r < rows;
+      const uint32_t query = (row0 + r) / p.group, hh = (row0 + r) - query * p.group;
+      const uint16_t* src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)(head * p.group + hh) * p.q_head + 16 * t;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;
+        if (live) {
+          a = __ldg(reinterpret_cast<const uint4*>(src + 64 * j));
+          b = __ldg(reinterpret_cast<const uint4*>(src + 64 * j + 8));
+        }
+        const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum += (from_bits16<TYPE>(wa[i] & 0xffffu) + from_bits16<TYPE>(wa[i] >> 16)) +
+                 (from_bits16<TYPE>(wb[i] & 0xffffu) + from_bits16<TYPE>(wb[i] >> 16));
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {                       // coordinates s and s + 4 of each word of eight
+          qf[nt][j][s][0] = __byte_perm(wa[s >> 1], wa[(s >> 1) + 2], s & 1 ? 0x7632 : 0x5410);
+          qf[nt][j][s][1] = __byte_perm(wb[s >> 1], wb[(s >> 1) + 2], s & 1 ? 0x7632 : 0x5410);
+        }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        qsum[nt][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+        qsum[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t rr = 8 * nt + 2 * t + e;
+        const int64_t far = rr < rows ? seq.length - (int64_t)(seq.n - 1 - (row0 + rr) / p.group) : 0;
+        see[nt][e] = far > 0 ? (int32_t)far : 0;
+      }
+    }
+    // Tokens that the first row sees (all rows see them) and that the last row sees.
+    const int64_t see_all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group);
+    const int64_t see_any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
+    uint32_t tile_end = see_any <= 0 ? 0u : (uint32_t)((see_any + kCacheTile - 1) / kCacheTile);
+    if (tile_end > tile1) tile_end = tile1;
+    const uint32_t my0 = tile0 + warp;
+    const uint32_t count = my0 < tile_end ? (tile_end - my0 + kWarps - 1) / kWarps : 0u;      // tiles of this warp
+
+    float o[NT][J][4][4], lsum[NT][2], osum[NT][J][2], top[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[nt][j][i][0] = o[nt][j][i][1] = o[nt][j][i][2] = o[nt][j][i][3] = 0.0f;
+        osum[nt][j][0] = osum[nt][j][1] = 0.0f;
+      }
+      lsum[nt][0] = lsum[nt][1] = 0.0f;
+      top[nt][0] = top[nt][1] = kNoMax;
+    }
+
+    // ---- the warp's tiles ----------------------------------------------------------------------------------------------
+    uint64_t source = 0;                                    // of tile (i & ~31) + lane, as a byte offset
+    auto look_up = [&](uint32_t i0) {
+      const uint32_t i = i0 + lane;
+      source = 0;
+      if (i < count) {
+        const uint32_t tile = my0 + kWarps * i, page = tile / p.c.page_tiles;
+        int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
+        if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
+        source = (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
+      }
+    };
+    auto issue = [&](uint32_t i) {
+      if (i < count) {
+        if ((i & 31u) == 0) look_up(i);
+        const uint64_t from = __shfl_sync(0xffffffffu, source, i & 31u);
+        const uint32_t s = i % S::kStages;
+        if (lane == 0) copy_tile(ring_u32 + s * S::kTileBytes, p.c.data + from, S::kTileBytes, bar_u32 + 8 * s);
+      }
+    };
+#pragma unroll 1
+    for (uint32_t i = 0; i < S::kStages; ++i) issue(i);
+
+#pragma unroll 1
+    for (uint32_t i = 0; i < count; ++i) {
+      const uint32_t s = i % S::kStages;
+      const uint8_t* const tile = ring + s * S::kTileBytes;
+      {
+        const uint32_t parity = (phases >> s) & 1u;
+        phases ^= 1u << s;
+        uint32_t polls = 0;
+        while (!mbar_try(bar_u32 + 8 * s, parity))
+          if (++polls >= kPolls) { timed_out = true; break; }
+      }
+      const uint32_t first = (my0 + kWarps * i) * kCacheTile;
+      const uint32_t ka = token_of(g), kb = ka + 8;
+      float sc[NT][4];                                      // scores: tokens ka, ka, kb, kb; rows 2t, 2t + 1, 2t, 2t + 1
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
+      const uint32_t* const key_pair = reinterpret_cast<const uint32_t*>(tile + 8 * D);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint2 ca = *reinterpret_cast<const uint2*>(tile + (j * 16 + ka) * 32 + 8 * t);
+        const uint2 cb = *reinterpret_cast<const uint2*>(tile + (j * 16 + kb) * 32 + 8 * t);
+        float acc[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t a[4] = {KeyCode<TYPE>::operand(ca.x, e), KeyCode<TYPE>::operand(cb.x, e), KeyCode<TYPE>::operand(ca.y, e),
+                                 KeyCode<TYPE>::operand(cb.y, e)};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma16816<TYPE>(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
+        }
+        const uint32_t pa = key_pair[ka * J + j], pb = key_pair[kb * J + j];
+        const float step_a = from_bits16<TYPE>(pa >> 16), step_b = from_bits16<TYPE>(pb >> 16);
+        const float rest_a = fmaf(-KeyCode<TYPE>::kBias, step_a, from_bits16<TYPE>(pa & 0xffffu));
+        const float rest_b = fmaf(-KeyCode<TYPE>::kBias, step_b, from_bits16<TYPE>(pb & 0xffffu));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          sc[nt][0] += fmaf(step_a, acc[nt][0], rest_a * qsum[nt][j][0]);
+          sc[nt][1] += fmaf(step_a, acc[nt][1], rest_a * qsum[nt][j][1]);
+          sc[nt][2] += fmaf(step_b, acc[nt][2], rest_b * qsum[nt][j][0]);
+          sc[nt][3] += fmaf(step_b, acc[nt][3], rest_b * qsum[nt][j][1]);
+        }
+      }
+
+      // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
+      const bool masked = (int64_t)first + kCacheTile > see_all;            // of the warp: some row does not see the whole tile
+      uint32_t seen = 0xffffffffu;                                          // bit 4 * nt + e
+      bool raise = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sc[nt][e] *= p.scale_log2;
+          if (masked && (int32_t)(e < 2 ? ka : kb) >= see[nt][e & 1] - (int32_t)first) {
+            seen &= ~(1u << (4 * nt + e));
+            sc[nt][e] = -INFINITY;
+          }
+          raise |= sc[nt][e] > top[nt][e & 1] + 8.0f;
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = fmaxf(sc[nt][e], sc[nt][e + 2]);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            m = fmaxf(m, top[nt][e]);
+            const float f = exp2_approx(top[nt][e] - m);
+            top[nt][e] = m;
+            lsum[nt][e] *= f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+              osum[nt][j][e] *= f;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) { o[nt][j][r][e] *= f; o[nt][j][r][e + 2] *= f; }
+            }
+          }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[nt][e] = exp2_approx(sc[nt][e] - top[nt][e & 1]);
+        lsum[nt][0] += sc[nt][0] + sc[nt][2];
+        lsum[nt][1] += sc[nt][1] + sc[nt][3];
+      }
+
+      // ---- output ---------------------------------------------------------------------------------------------------------
+      const uint8_t* const values = tile + 9 * D;
+      const uint32_t* const value_pair = reinterpret_cast<const uint32_t*>(values + 8 * D);
+      const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint32_t pa = value_pair[ka * J + j], pb = value_pair[kb * J + j];
+        const float step_a = from_bits16<TYPE>(pa >> 16), step_b = from_bits16<TYPE>(pb >> 16);
+        const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pa & 0xffffu)), mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pb & 0xffffu));
+        uint32_t bh[NT][2], bl[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float w[4] = {sc[nt][0] * step_a, sc[nt][1] * step_a, sc[nt][2] * step_b, sc[nt][3] * step_b};
+          float z[4] = {sc[nt][0] * mid_a, sc[nt][1] * mid_a, sc[nt][2] * mid_b, sc[nt][3] * mid_b};
+          if (masked) {                                     // what a row does not see may hold anything: no product with it
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!(seen >> (4 * nt + e) & 1u)) w[e] = z[e] = 0.0f;
+          }
+          osum[nt][j][0] += z[0] + z[2];
+          osum[nt][j][1] += z[1] + z[3];
+          const uint32_t h0 = pack16<QSGD_TYPE_BF16>(w[0], w[1]), h1 = pack16<QSGD_TYPE_BF16>(w[2], w[3]);
+          const uint32_t l0 = pack16<QSGD_TYPE_BF16>(w[0] - __uint_as_float(h0 << 16), w[1] - __uint_as_float(h0 & 0xffff0000u));
+          const uint32_t l1 = pack16<QSGD_TYPE_BF16>(w[2] - __uint_as_float(h1 << 16), w[3] - __uint_as_float(h1 & 0xffff0000u));
+          bh[nt][0] = transpose8x8(h0);
+          bh[nt][1] = transpose8x8(h1);
+          bl[nt][0] = transpose8x8(l0);
+          bl[nt][1] = transpose8x8(l1);
+        }
+        const uint8_t* const codes = values + j * 512 + 4 * g;
+        const uint32_t c0 = *reinterpret_cast<const uint32_t*>(codes + va * 32), c1 = *reinterpret_cast<const uint32_t*>(codes + vb * 32);
+        const uint32_t c2 = *reinterpret_cast<const uint32_t*>(codes + (va + 8) * 32), c3 = *reinterpret_cast<const uint32_t*>(codes + (vb + 8) * 32);
+        const uint32_t lo01 = __byte_perm(c0, c1, 0x5410), hi01 = __byte_perm(c0, c1, 0x7632);
+        const uint32_t lo23 = __byte_perm(c2, c3, 0x5410), hi23 = __byte_perm(c2, c3, 0x7632);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {                       // rows: coordinates 64 j + 8 g + r, and those + 4
+          const uint32_t a[4] = {value_operand(lo01, r), value_operand(hi01, r), value_operand(lo23, r), value_operand(hi23, r)};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma16816<QSGD_TYPE_BF16>(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
+            mma16816<QSGD_TYPE_BF16>(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
+          }
+        }
+      }
+      __syncwarp();                                         // the stage's readers are done
+      issue(i + S::kStages);
+    }
+
+    // ---- the warps' parts are joined ----------------------------------------------------------------------------------------
+    float* const mine = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t r = 8 * nt + 2 * t + e;
+        float l = lsum[nt][e];
+#pragma unroll
+        for (int m = 4; m < 32; m <<= 1) l += __shfl_xor_sync(0xffffffffu, l, m);
+        if (g == 0) { part_m[warp][r] = top[nt][e]; part_l[warp][r] = l; }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          float z = osum[nt][j][e];
+#pragma unroll
+          for (int m = 4; m < 32; m <<= 1) z += __shfl_xor_sync(0xffffffffu, z, m);
+          float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
+          *reinterpret_cast<float4*>(at) = make_float4(o[nt][j][0][e] + z, o[nt][j][1][e] + z, o[nt][j][2][e] + z, o[nt][j][3][e] + z);
+          *reinterpret_cast<float4*>(at + 4) =
+              make_float4(o[nt][j][0][e + 2] + z, o[nt][j][1][e + 2] + z, o[nt][j][2][e + 2] + z, o[nt][j][3][e + 2] + z);
+        }
+      }
+    __syncthreads();
+    const bool whole = tile0 == 0 && tile1 == seq.tiles;
+    float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + (u == u0 ? 0 : 1)) * part_floats(R, D);
+    for (uint32_t i = tid; i < rows * (D / 4); i += kThreads) {
+      const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
+      float m = kNoMax, l = 0.0f;
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) m = fmaxf(m, part_m[w][r]);
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) {
+        const float f = exp2_approx(part_m[w][r] - m);
+        const float4 v = *reinterpret_cast<const float4*>(smem + w * S::kPerWarp + (r * S::kRowFloats + 4 * d4) * 4);
+        l = fmaf(f, part_l[w][r], l);
+        sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+      }
+      if (whole) {
+        const uint32_t query = (row0 + r) / p.group, hh = head * p.group + (row0 + r) - query * p.group;
+        const uint64_t row = seq.start + query;
+        const bool sees = seq.length - (int64_t)(seq.n - 1 - query) > 0;
+        const float f = sees ? 1.0f / l : 0.0f;
+        *reinterpret_cast<uint2*>(p.out + row * p.out_token + (uint64_t)hh * p.out_head + 4 * d4) =
+            sees ? make_uint2(pack16<TYPE>(sum.x * f, sum.y * f), pack16<TYPE>(sum.z * f, sum.w * f)) : make_uint2(0u, 0u);
+        if (p.lse && d4 == 0) p.lse[row * p.q_heads + hh] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      } else {
+        *reinterpret_cast<float4*>(part + r * D + 4 * d4) = sum;
+        if (d4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
+      }
+    }
+    if (u == u0 && tid == 0) {
+      JoinInfo j{0, 0, 0, head, row0, rows, seq.start, 0};
+      const uint64_t begin = u - tile0, end = begin + seq.tiles;            // the segment on the line of units
+      if (tile0 && begin / chunk == blockIdx.x - 1) {       // this CTA's start is the first boundary inside the segment
+        j.first = blockIdx.x - 1;
+        j.first_slot = begin == (uint64_t)(blockIdx.x - 1) * chunk ? 0u : 1u;
+        j.parts = (uint32_t)((end - 1) / chunk) - j.first + 1;
+      }
+      p.join[blockIdx.x] = j;
+    }
+    // Bulk copies write where these reads were: order the two kinds of access before the next piece's first copy.
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    u += tile1 - tile0;
+  }
+  if (timed_out) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+}
+
+// Parts of a segment that several CTAs hold, one row to a CTA: a warp to every eighth part, each D / 32 coordinates a lane.
+template <int TYPE, int D, int R>
+__global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_constant__ AttendParams p, uint32_t n) {
+  constexpr int V = D / 32;
+  __shared__ float sum[kWarps][D];
+  __shared__ float part_m[kWarps], part_l[kWarps];
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, r = blockIdx.x / n, cta = blockIdx.x - r * n;
+  chain_wait();
+  const JoinInfo j = p.join[cta];
+  if (j.parts == 0 || r >= j.rows) return;
+  float m = kNoMax, l = 0.0f, o[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) o[i] = 0.0f;
+  for (uint32_t k = warp; k < j.parts; k += kWarps) {
+    const float* part = p.parts + ((uint64_t)(j.first + k) * 2 + (k == 0 ? j.first_slot : 0u)) * part_floats(R, D);
+    const float pm = part[R * D + r], pl = part[R * D + R + r], top = fmaxf(m, pm), f = exp2_approx(m - top), e = exp2_approx(pm - top);
+    l = fmaf(e, pl, l * f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = fmaf(e, part[r * D + 32 * i + lane], o[i] * f);
+    m = top;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) sum[warp][32 * i + lane] = o[i];
+  if (lane == 0) { part_m[warp] = m; part_l[warp] = l; }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    m = kNoMax;
+    l = 0.0f;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) m = fmaxf(m, part_m[w]);
+    float v = 0.0f;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) {
+      const float f = exp2_approx(part_m[w] - m);
+      l = fmaf(f, part_l[w], l);
+      v = fmaf(f, sum[w][threadIdx.x], v);
+    }
+    const uint32_t query = (j.row0 + r) / p.group, hh = j.head * p.group + (j.row0 + r) - query * p.group;
+    const uint64_t row = j.start + query;
+    const bool sees = m > kNoMax || !(l == 0.0f);           // no token: no maximum and no sum
+    p.out[row * p.out_token + (uint64_t)hh * p.out_head + threadIdx.x] = sees ? (uint16_t)to_bits16<TYPE>(v / l) : (uint16_t)0;
+    if (p.lse && threadIdx.x == 0) p.lse[row * p.q_heads + hh] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+  }
+}
+
+template <int TYPE, int D, int NT>
+int launch_attend(AttendParams& p, cudaStream_t stream) {
+  using S = Shape<TYPE, D, NT>;
+  static KernelSite site;
+  auto kern = cache_attend_kernel<TYPE, D, NT>;
+  int sms = 0, occ = 0;
+  const int st = site.lookup(kern, kThreads, S::kSmem, &sms, &occ);
+  if (st) return st;
+  uint32_t grid = (uint32_t)(sms * occ);
+  if (grid > kMostCtas) grid = kMostCtas;
+  {
+    ScopedKernel sk(kKernCacheAttend, stream);
+    const cudaError_t e = launch_chained(kern, grid, kThreads, S::kSmem, stream, p);
+    if (e != cudaSuccess) return (int)e;
+  }
+  ScopedKernel sk(kKernCacheJoin, stream);
+  return (int)launch_chained(cache_join_kernel<TYPE, D, S::kRows>, grid * S::kRows, kThreads, 0, stream, p, grid);
+}
+
+template <int TYPE>
+int dispatch(AttendParams& p, uint32_t dim, bool wide, cudaStream_t stream) {
+  switch (dim) {
+    case 64: return wide ? launch_attend<TYPE, 64, 2>(p, stream) : launch_attend<TYPE, 64, 1>(p, stream);
+    case 128: return wide ? launch_attend<TYPE, 128, 2>(p, stream) : launch_attend<TYPE, 128, 1>(p, stream);
+    case 192: return launch_attend<TYPE, 192, 1>(p, stream);
+    default: return launch_attend<TYPE, 256, 1>(p, stream);
+  }
+}
+
+}  // namespace
+
+size_t cache_attend_workspace_bytes(uint32_t head_dim) {
+  return kMostCtas * (sizeof(JoinInfo) + 2 * sizeof(float) * part_floats(kMostRowTile, head_dim));
+}
+
+int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, const AttendArgs& a, cudaStream_t stream) {
+  AttendParams p;
+  p.c = view;
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.out = static_cast<uint16_t*>(a.out);
+  p.q_token = a.q_token; p.q_head = a.q_head; p.out_token = a.out_token; p.out_head = a.out_head;
+  p.lse = a.lse;
+  p.q_heads = a.q_heads;
+  p.group = a.q_heads / view.heads;
+  p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+  p.join = reinterpret_cast<JoinInfo*>(a.workspace);
+  p.parts = reinterpret_cast<float*>(a.workspace + kMostCtas * sizeof(JoinInfo));
+  // 16 rows to a tile where a sequence has more than 8 on average: the codes are unpacked half as often.
+  const bool wide = (uint64_t)view.rows * p.group > 8ull * view.sequences;
+  return type == QSGD_TYPE_BF16 ? dispatch<QSGD_TYPE_BF16>(p, head_dim, wide, stream) : dispatch<QSGD_TYPE_F16>(p, head_dim, wide, stream);
+}
+
+}  // namespace qsgd

@@ -1,0 +1,31 @@
+// Rows in 8-bit integers with a scale each, and their products: the internal launch interface.
+#pragma once
+
+#include "qsgd_common.cuh"
+
+namespace qsgd {
+
+int launch_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row_stride, int type, int8_t* codes, uint64_t codes_stride,
+                         float* scale, cudaStream_t stream);
+
+struct MatmulArgs {
+  const int8_t* a;
+  const int8_t* b;
+  const float* a_scale;
+  const float* b_scale;
+  const float* bias;          // or nullptr
+  void* out;
+  uint64_t a_stride, b_stride, out_stride;
+  uint32_t m, n, k;
+  int type;
+};
+int launch_matmul_i8(const MatmulArgs& args, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// The sum, scaled: in fp32, in this order, rounded to the output's type once.
+__device__ __forceinline__ float scaled_sum(int32_t sum, float a_scale, float b_scale, float bias) {
+  return __fadd_rn(__fmul_rn(__fmul_rn(__int2float_rn(sum), a_scale), b_scale), bias);
+}
+#endif
+
+}  // namespace qsgd

@@ -9,6 +9,9 @@
 // tensors and are not raise the package's own exception, handed over once by set_error.
 #include <Python.h>
 
+#include <cmath>
+
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -309,6 +312,238 @@ PyObject* sgd_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   QSGD_CATCH
 }
 
+// ---- few-bit values outside the gradient exchange ---------------------------------------------------
+// These calls take strided tensors, several to a call, so what each must be is checked here by one rule.
+
+[[noreturn]] void refuse(const char* format, const char* name, long long a = 0, long long b = 0) {
+  PyErr_Format(g_error ? g_error : PyExc_RuntimeError, format, name, a, b);
+  throw Fail{};
+}
+
+// A CUDA tensor of a type and number of dimensions, on the device of the others; the last dimension contiguous.
+const at::Tensor& strided(PyObject* o, const char* name, c10::ScalarType type, int64_t dims, c10::Device device) {
+  if (!THPVariable_Check(o)) refuse("%s must be a CUDA tensor", name);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda()) refuse("%s must be a CUDA tensor", name);
+  if (t.device() != device) refuse("%s is on another device than the call's first tensor", name);
+  if (t.scalar_type() != type) refuse("%s has another element type than the call takes", name);
+  if (t.dim() != dims) refuse("%s must have %lld dimensions", name, dims);
+  if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) refuse("%s must be contiguous along its last dimension", name);
+  return t;
+}
+const at::Tensor& whole(PyObject* o, const char* name, c10::ScalarType type, int64_t dims, c10::Device device) {
+  const at::Tensor& t = strided(o, name, type, dims, device);
+  if (!t.is_contiguous()) refuse("%s must be contiguous", name);
+  return t;
+}
+void sized(const at::Tensor& t, const char* name, int64_t dim, int64_t size) {
+  if (t.size(dim) != size) refuse("%s must have the size %lld in dimension %lld", name, size, dim);
+}
+uint64_t stride_of(const at::Tensor& t, int64_t dim) { return t.size(dim) > 1 ? static_cast<uint64_t>(t.stride(dim)) : 0u; }
+
+c10::Device device_of(PyObject* o, const char* name) {
+  if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) refuse("%s must be a CUDA tensor", name);
+  return THPVariable_Unpack(o).device();
+}
+
+// The given stream, or the current one of the tensors' device.
+qsgd_stream_t stream_on(PyObject* o, c10::Device device) {
+  if (o == Py_None) return c10::cuda::getCurrentCUDAStream(device.index()).stream();
+  PyObject* index = PyObject_GetAttrString(o, "device_index");
+  if (index) {
+    const long long at = PyLong_AsLongLong(index);
+    Py_DECREF(index);
+    if (at == -1 && PyErr_Occurred()) throw Fail{};
+    if (at != device.index()) refuse("%s is on another device than the tensors", "stream");
+  } else {
+    PyErr_Clear();                                    // a bare holder of a cuda_stream
+  }
+  return stream_of(o);
+}
+
+int type_code(c10::ScalarType t, const char* name) {
+  switch (t) {
+    case at::kFloat: return QSGD_TYPE_F32;
+    case at::kHalf: return QSGD_TYPE_F16;
+    case at::kBFloat16: return QSGD_TYPE_BF16;
+    default: refuse("%s must hold float32, float16 or bfloat16", name);
+  }
+}
+
+// What the calls on a cache share: (address of a qsgd_cache, its data, table, lengths, starts or None).
+struct CacheCall {
+  const qsgd_cache* cache;
+  qsgd_cache_rows rows{};
+  c10::Device device;
+  c10::ScalarType type;
+  CacheCall(PyObject* const* a) : cache(static_cast<const qsgd_cache*>(address(a[0]))), device(device_of(a[1], "the cache's data")) {
+    type = cache->type == QSGD_TYPE_F16 ? at::kHalf : at::kBFloat16;
+    const at::Tensor& table = strided(a[2], "table", at::kInt, 2, device);
+    const at::Tensor& lengths = whole(a[3], "lengths", at::kInt, 1, device);
+    sized(table, "table", 0, lengths.size(0));
+    rows.table = table.const_data_ptr<int32_t>();
+    rows.table_stride = stride_of(table, 0);
+    if (table.size(1) > 0x7fffffff || lengths.size(0) > 0x7fffffff) refuse("%s is too large", "table");
+    rows.table_pages = static_cast<uint32_t>(table.size(1));
+    rows.sequences = static_cast<uint32_t>(lengths.size(0));
+    rows.lengths = lengths.const_data_ptr<int32_t>();
+    if (a[4] != Py_None) {
+      const at::Tensor& starts = whole(a[4], "starts", at::kInt, 1, device);
+      sized(starts, "starts", 0, lengths.size(0) + 1);
+      rows.starts = starts.const_data_ptr<int32_t>();
+    }
+  }
+  const at::Tensor& dense(PyObject* o, const char* name, int64_t heads, bool first) {
+    const at::Tensor& t = strided(o, name, type, 3, device);
+    if (first) rows.rows = static_cast<uint64_t>(t.size(0));
+    sized(t, name, 0, static_cast<int64_t>(rows.rows));
+    if (heads) sized(t, name, 1, heads);
+    sized(t, name, 2, cache->head_dim);
+    return t;
+  }
+  uint32_t* status(PyObject* o) const { return static_cast<uint32_t*>(whole(o, "status_dev", at::kInt, 1, device).data_ptr()); }
+};
+
+// cache_store(write, cache, data, table, lengths, starts or None, k, v, status, stream)
+PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  QSGD_ARGS(10)
+  QSGD_TRY
+  CacheCall c(a + 1);
+  const at::Tensor& k = c.dense(a[6], "k", c.cache->heads, true);
+  const at::Tensor& v = c.dense(a[7], "v", c.cache->heads, false);
+  uint32_t* status = c.status(a[8]);
+  const qsgd_stream_t stream = stream_on(a[9], c.device);
+  const bool write = a[0] == Py_True;
+  const c10::cuda::CUDAGuard guard(c.device);
+  return unlocked([&] {
+    return write ? qsgd_cache_write(c.cache, &c.rows, k.const_data_ptr(), stride_of(k, 0), stride_of(k, 1), v.const_data_ptr(),
+                                    stride_of(v, 0), stride_of(v, 1), status, stream)
+                 : qsgd_cache_read(c.cache, &c.rows, k.data_ptr(), stride_of(k, 0), stride_of(k, 1), v.data_ptr(), stride_of(v, 0),
+                                   stride_of(v, 1), status, stream);
+  });
+  QSGD_CATCH
+}
+
+// cache_attend(cache, data, table, lengths, starts or None, q, out, workspace, status, scale or None, lse or None, stream)
+PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  QSGD_ARGS(12)
+  QSGD_TRY
+  CacheCall c(a);
+  const at::Tensor& q = c.dense(a[5], "q", 0, true);
+  const int64_t heads = q.size(1);
+  const size_t need = heads > 0 && heads <= 0x7fffffff ? qsgd_cache_attend_workspace_bytes(c.cache, static_cast<uint32_t>(heads)) : 0;
+  if (need == 0) refuse("%s must have a multiple of the cache's %lld heads", "q", c.cache->heads);
+  const at::Tensor& out = c.dense(a[6], "out", heads, false);
+  const at::Tensor& ws = whole(a[7], "workspace", at::kByte, 1, c.device);
+  if (ws.nbytes() < need) refuse("%s must have %lld bytes", "workspace", static_cast<long long>(need));
+  float* lse = nullptr;
+  if (a[10] != Py_None) {
+    const at::Tensor& t = whole(a[10], "lse", at::kFloat, 2, c.device);
+    sized(t, "lse", 0, q.size(0));
+    sized(t, "lse", 1, heads);
+    lse = t.data_ptr<float>();
+  }
+  const float scale = a[9] == Py_None ? 1.0f / std::sqrt(static_cast<float>(c.cache->head_dim)) : f32(a[9]);
+  uint32_t* status = c.status(a[8]);
+  const qsgd_stream_t stream = stream_on(a[11], c.device);
+  const c10::cuda::CUDAGuard guard(c.device);
+  return unlocked([&] {
+    return qsgd_cache_attend(c.cache, &c.rows, q.const_data_ptr(), stride_of(q, 0), stride_of(q, 1), static_cast<uint32_t>(heads), scale,
+                             out.data_ptr(), stride_of(out, 0), stride_of(out, 1), lse, ws.data_ptr(), status, stream);
+  });
+  QSGD_CATCH
+}
+
+// quantize_rows(x, codes, scale, stream)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  QSGD_ARGS(4)
+  QSGD_TRY
+  const c10::Device device = device_of(a[0], "x");
+  const c10::ScalarType kind = THPVariable_Unpack(a[0]).scalar_type();
+  const int type = type_code(kind, "x");
+  const at::Tensor& x = strided(a[0], "x", kind, 2, device);
+  const at::Tensor& codes = strided(a[1], "codes", at::kChar, 2, device);
+  const at::Tensor& scale = whole(a[2], "scale", at::kFloat, 1, device);
+  sized(codes, "codes", 0, x.size(0));
+  sized(codes, "codes", 1, x.size(1));
+  sized(scale, "scale", 0, x.size(0));
+  if (x.size(1) > 0x7fffffff) refuse("%s has too many columns", "x");
+  const qsgd_stream_t stream = stream_on(a[3], device);
+  const c10::cuda::CUDAGuard guard(device);
+  return unlocked([&] {
+    return qsgd_quantize_rows(x.const_data_ptr(), static_cast<uint64_t>(x.size(0)), static_cast<uint32_t>(x.size(1)), stride_of(x, 0), type,
+                              codes.data_ptr<int8_t>(), stride_of(codes, 0), scale.data_ptr<float>(), stream);
+  });
+  QSGD_CATCH
+}
+
+// What the two products share: b, its scales, bias, and the output of m rows.
+struct ProductCall {
+  const at::Tensor& b;
+  const at::Tensor& scale;
+  const at::Tensor& out;
+  const float* bias = nullptr;
+  int type;
+  ProductCall(PyObject* ob, PyObject* os, PyObject* oo, PyObject* obias, const at::Tensor& a, const char* name, const char* scale_name,
+              c10::Device device)
+      : b(strided(ob, name, at::kChar, 2, device)), scale(whole(os, scale_name, at::kFloat, 1, device)),
+        out(strided(oo, "out", THPVariable_Check(oo) ? THPVariable_Unpack(oo).scalar_type() : at::kFloat, 2, device)),
+        type(type_code(out.scalar_type(), "out")) {
+    sized(b, name, 1, a.size(1));
+    sized(scale, scale_name, 0, b.size(0));
+    sized(out, "out", 0, a.size(0));
+    sized(out, "out", 1, b.size(0));
+    if (obias != Py_None) {
+      const at::Tensor& t = whole(obias, "bias", at::kFloat, 1, device);
+      sized(t, "bias", 0, b.size(0));
+      bias = t.const_data_ptr<float>();
+    }
+    if (a.size(1) > 0x7fffffff) refuse("%s has too many columns", name);
+  }
+};
+
+// matmul_i8(a, a_scale, b, b_scale, out, bias or None, stream)
+PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  QSGD_ARGS(7)
+  QSGD_TRY
+  const c10::Device device = device_of(a[0], "a");
+  const at::Tensor& x = strided(a[0], "a", at::kChar, 2, device);
+  const at::Tensor& x_scale = whole(a[1], "a_scale", at::kFloat, 1, device);
+  sized(x_scale, "a_scale", 0, x.size(0));
+  const ProductCall c(a[2], a[3], a[4], a[5], x, "b", "b_scale", device);
+  const qsgd_stream_t stream = stream_on(a[6], device);
+  const c10::cuda::CUDAGuard guard(device);
+  return unlocked([&] {
+    return qsgd_matmul_i8(x.const_data_ptr<int8_t>(), stride_of(x, 0), x_scale.const_data_ptr<float>(), c.b.const_data_ptr<int8_t>(),
+                          stride_of(c.b, 0), c.scale.const_data_ptr<float>(), c.bias, static_cast<uint64_t>(x.size(0)),
+                          static_cast<uint64_t>(c.b.size(0)), static_cast<uint32_t>(x.size(1)), c.out.data_ptr(), stride_of(c.out, 0), c.type,
+                          stream);
+  });
+  QSGD_CATCH
+}
+
+// linear_i8(x, w, w_scale, out, workspace, bias or None, stream)
+PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  QSGD_ARGS(7)
+  QSGD_TRY
+  const c10::Device device = device_of(a[0], "x");
+  const c10::ScalarType kind = THPVariable_Unpack(a[0]).scalar_type();
+  const int x_type = type_code(kind, "x");
+  const at::Tensor& x = strided(a[0], "x", kind, 2, device);
+  const ProductCall c(a[1], a[2], a[3], a[5], x, "w", "w_scale", device);
+  const at::Tensor& ws = whole(a[4], "workspace", at::kByte, 1, device);
+  const size_t need = qsgd_linear_i8_workspace_bytes(static_cast<uint64_t>(x.size(0)), static_cast<uint32_t>(x.size(1)));
+  if (ws.nbytes() < need) refuse("%s must have %lld bytes", "workspace", static_cast<long long>(need));
+  const qsgd_stream_t stream = stream_on(a[6], device);
+  const c10::cuda::CUDAGuard guard(device);
+  return unlocked([&] {
+    return qsgd_linear_i8(x.const_data_ptr(), stride_of(x, 0), x_type, c.b.const_data_ptr<int8_t>(), stride_of(c.b, 0),
+                          c.scale.const_data_ptr<float>(), c.bias, static_cast<uint64_t>(x.size(0)), static_cast<uint64_t>(c.b.size(0)),
+                          static_cast<uint32_t>(x.size(1)), c.out.data_ptr(), stride_of(c.out, 0), c.type, ws.data_ptr(), stream);
+  });
+  QSGD_CATCH
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_XINCREF(cls);
   Py_XSETREF(g_error, cls);
@@ -318,6 +553,8 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 #define QSGD_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {QSGD_FAST(encode),        QSGD_FAST(encode_static), QSGD_FAST(policy_encode),
                           QSGD_FAST(decode),        QSGD_FAST(policy_decode), QSGD_FAST(sgd_step),
+                          QSGD_FAST(cache_store),   QSGD_FAST(cache_attend),  QSGD_FAST(quantize_rows),
+                          QSGD_FAST(matmul_i8),     QSGD_FAST(linear_i8),
                           {"set_error", set_error, METH_O, nullptr},          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_qsgd_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -124,6 +124,7 @@ enum KernelId {
   kKernQuantize = 0, kKernQuantizeTail, kKernDecodeFixed, kKernSgdStep, kKernEliasLength,
   kKernEliasScatter, kKernDecodeElias, kKernDecodeEliasSparse, kKernRawGather, kKernRawDecode,
   kKernDecodeEliasTeams, kKernDecodeEliasFields, kKernDecodeEliasBytes, kKernDecodeEliasDense,
+  kKernCacheWrite, kKernCacheRead, kKernCacheAttend, kKernCacheJoin, kKernQuantizeRows, kKernMatmulI8, kKernMatmulI8Few,
   kKernCount      // (kKernDecodeElias: streams of strings by table)
 };
 
