@@ -3,14 +3,17 @@
 // For a query row q (one head of one query), with keys k_t = lo + step * c_t (a group g of 64 coordinates has its own pair):
 //   s_t = sum_g step_tg * (q_g . c_tg) + lo_tg * sum(q_g),   p_t = 2^(a s_t - m),   a = scale * log2(e),
 //   o   = (sum_t p_t v_t) / sum_t p_t,    sum_t p_t v_tg = sum_t (p_t step_tg) (c_tg - 8) + sum_t p_t (lo_tg + 8 step_tg).
-// The codes go to the tensor cores as they are (integers of four bits are exact in the operand types), the pairs are applied in fp32:
-//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, q's own type, fp32 sums);
-//            a code reaches the operand as 128 + c (bf16) or 16 + c (fp16), a mask and an or on the packed word, and the constant
-//            times sum(q_g) is taken off afterwards;
-//   output   A = (c - 8) of 16 coordinates x 16 tokens, B = p * step as the sum of two bf16 numbers (16 bits of p: one bf16 would
-//            put as much error into the output as rounding the output itself does). Codes are centred here because these sums run over the
-//            whole sequence and the constant part would bury them.
-// The rows of a score tile are permuted (kToken) so that the transpose of p between the two products is one movmatrix, and reads
+// The codes go to the tensor cores as they are, centred (c - 8 is exact in fp16), and the pairs are applied in fp32:
+//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp32 sums). A row of q is multiplied by a power of
+//            two that puts its largest number at 8 to 16: 16-bit numbers of either type fit fp16 then, but for what lies 2^-17 and more below
+//            the largest, which loses no more than fp32 sums do.
+//   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two that puts the largest step so far at 64
+//            (p may reach 2^8). For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
+//            For fp16 p * step goes as the sum of two fp16 numbers, since one would put as much error into the output as rounding it does.
+// Unpacking: a nibble under the exponent of 1024 or of 64 is 1024 + c or 64 + c where it stands, so four pairs of codes take four
+// logical operations and one shift, and a subtraction each on the otherwise idle multiply pipe. (With bf16 operands, whose seven bits of fraction
+// need every nibble moved into place, and p in two bf16 numbers: 143 us against 4 fewer shifts per word and half the products here.)
+// The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
 // What bounds it: with up to 8 rows a key head, HBM: 9/8 * head_dim bytes a token and head, each read once, against about 150
@@ -29,7 +32,11 @@ constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
 constexpr uint32_t kLeastChunk = kWarps;  // units of a stretch: a tile for each warp
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kPolls = 1u << 22;
+constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;     // 2^-120, 2^126
 constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that differences of maxima are numbers
+
+template <bool V>
+struct Constant { static constexpr bool value = V; };
 
 struct JoinInfo {                         // of the piece that a CTA begins with, written by every CTA of every call
   uint32_t parts;                         // CTAs from `first` on hold a part of the segment; 0: nothing to join at this boundary
@@ -73,14 +80,9 @@ __device__ __forceinline__ void copy_tile(uint32_t dst, const uint8_t* src, uint
                "r"(bytes), "r"(bar) : "memory");
 }
 
-template <int TYPE>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if (TYPE == QSGD_TYPE_BF16)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
@@ -95,26 +97,18 @@ __device__ __forceinline__ float exp2_approx(float v) {
   return r;
 }
 
-// Nibbles s of the two halves of a word as operands: kBias + code.
-template <int TYPE>
-struct KeyCode;
-template <>
-struct KeyCode<QSGD_TYPE_BF16> {          // 128 + c: the code in the last four of seven fraction bits
-  static constexpr float kBias = 128.0f;
-  static __device__ __forceinline__ uint32_t operand(uint32_t w, int s) { return ((w >> (4 * s)) & 0x000f000fu) | 0x43004300u; }
-};
-template <>
-struct KeyCode<QSGD_TYPE_F16> {           // 16 + c: the code in the first four of ten fraction bits (1024 + c would cost ten bits of the sum)
-  static constexpr float kBias = 16.0f;
-  static __device__ __forceinline__ uint32_t operand(uint32_t w, int s) {
-    return ((s < 2 ? w << (6 - 4 * s) : w >> (4 * s - 6)) & 0x03c003c0u) | 0x4c004c00u;
-  }
-};
-
-__device__ __forceinline__ uint32_t value_operand(uint32_t w, int s) {       // c - 8 in bf16, exact
-  const uint32_t biased = ((w >> (4 * s)) & 0x000f000fu) | 0x43004300u;
-  __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&biased), __floats2bfloat162_rn(136.0f, 136.0f));
-  return *reinterpret_cast<uint32_t*>(&r);
+// The codes of a word, less 8: pair s holds nibble s of either half.
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
+  const uint32_t v = w >> 8;
+  c[0] = sub_f16x2((w & 0x000f000fu) | 0x64006400u, 0x64086408u);          // 1024 + c, less 1032
+  c[1] = sub_f16x2((w & 0x00f000f0u) | 0x54005400u, 0x54805480u);          // 64 + c, less 72
+  c[2] = sub_f16x2((v & 0x000f000fu) | 0x64006400u, 0x64086408u);
+  c[3] = sub_f16x2((v & 0x00f000f0u) | 0x54005400u, 0x54805480u);
 }
 
 // One sequence on the line of units.
@@ -235,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 
     // ---- queries: operands, sums of each group, and how far each row sees ------------------------------------------------
     uint32_t qf[NT][J][4][2];
-    float qsum[NT][J][2];
+    float qsum[NT][J][2], factor[NT][2];
     int32_t see[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -243,23 +237,50 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       const bool live = r < rows;
       const uint32_t query = (row0 + r) / p.group, hh = (row0 + r) - query * p.group;
       const uint16_t* src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)(head * p.group + hh) * p.q_head + 16 * t;
+      uint4 raw[J][2];
+      float top_q = 0.0f;
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        uint4 a = make_uint4(0, 0, 0, 0), b = a;
+        raw[j][0] = raw[j][1] = make_uint4(0, 0, 0, 0);
         if (live) {
-          a = __ldg(reinterpret_cast<const uint4*>(src + 64 * j));
-          b = __ldg(reinterpret_cast<const uint4*>(src + 64 * j + 8));
+          raw[j][0] = __ldg(reinterpret_cast<const uint4*>(src + 64 * j));
+          raw[j][1] = __ldg(reinterpret_cast<const uint4*>(src + 64 * j + 8));
         }
-        const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t w[4] = {raw[j][h].x, raw[j][h].y, raw[j][h].z, raw[j][h].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            top_q = fmaxf(top_q, fmaxf(fabsf(from_bits16<TYPE>(w[i] & 0xffffu)), fabsf(from_bits16<TYPE>(w[i] >> 16))));
+        }
+      top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 1));
+      top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 2));
+      // 2^(3 - e) for a largest number of [2^e, 2^(e + 1)); nothing to scale in a row of zeros, infinities or NaN
+      const int32_t e = (int32_t)(__float_as_uint(top_q) >> 23) - 127;
+      int32_t up = 3 - e;
+      if (up > 120) up = top_q > 0.0f ? 120 : 0;
+      if (e == 128) up = 0;
+      const float times = __uint_as_float((uint32_t)(127 + up) << 23);
+      const float back = p.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+      factor[nt][0] = __shfl_sync(0xffffffffu, back, 8 * t);
+      factor[nt][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sum += (from_bits16<TYPE>(wa[i] & 0xffffu) + from_bits16<TYPE>(wa[i] >> 16)) +
-                 (from_bits16<TYPE>(wb[i] & 0xffffu) + from_bits16<TYPE>(wb[i] >> 16));
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t w[4] = {raw[j][h].x, raw[j][h].y, raw[j][h].z, raw[j][h].w};
+          float x[8];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {                       // coordinates s and s + 4 of each word of eight
-          qf[nt][j][s][0] = __byte_perm(wa[s >> 1], wa[(s >> 1) + 2], s & 1 ? 0x7632 : 0x5410);
-          qf[nt][j][s][1] = __byte_perm(wb[s >> 1], wb[(s >> 1) + 2], s & 1 ? 0x7632 : 0x5410);
+          for (int i = 0; i < 4; ++i) { x[2 * i] = from_bits16<TYPE>(w[i] & 0xffffu) * times; x[2 * i + 1] = from_bits16<TYPE>(w[i] >> 16) * times; }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                     // coordinates i and i + 4 of each word of eight
+            sum += x[i] + x[i + 4];
+            qf[nt][j][i][h] = pack16<QSGD_TYPE_F16>(x[i], x[i + 4]);
+          }
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -267,10 +288,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         qsum[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t rr = 8 * nt + 2 * t + e;
+      for (int e2 = 0; e2 < 2; ++e2) {
+        const uint32_t rr = 8 * nt + 2 * t + e2;
         const int64_t far = rr < rows ? seq.length - (int64_t)(seq.n - 1 - (row0 + rr) / p.group) : 0;
-        see[nt][e] = far > 0 ? (int32_t)far : 0;
+        see[nt][e2] = far > 0 ? (int32_t)far : 0;
       }
     }
     // Tokens that the first row sees (all rows see them) and that the last row sees.
@@ -295,40 +316,22 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     }
 
     // ---- the warp's tiles ----------------------------------------------------------------------------------------------
-    uint64_t source = 0;                                    // of tile (i & ~31) + lane, as a byte offset
-    auto look_up = [&](uint32_t i0) {
-      const uint32_t i = i0 + lane;
-      source = 0;
-      if (i < count) {
-        const uint32_t tile = my0 + kWarps * i, page = tile / p.c.page_tiles;
-        int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
-        if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
-        source = (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
-      }
+    // Lane l knows where tiles l, l + 32, ... of the warp lie, and starts their copies.
+    auto look_up = [&](uint32_t i) -> const uint8_t* {
+      const uint32_t tile = my0 + kWarps * i, page = tile / p.c.page_tiles;
+      int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
+      if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
+      return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
     };
-    auto issue = [&](uint32_t i) {
-      if (i < count) {
-        if ((i & 31u) == 0) look_up(i);
-        const uint64_t from = __shfl_sync(0xffffffffu, source, i & 31u);
-        const uint32_t s = i % S::kStages;
-        if (lane == 0) copy_tile(ring_u32 + s * S::kTileBytes, p.c.data + from, S::kTileBytes, bar_u32 + 8 * s);
-      }
-    };
+    const uint8_t* source = lane < count ? look_up(lane) : nullptr;
 #pragma unroll 1
-    for (uint32_t i = 0; i < S::kStages; ++i) issue(i);
+    for (uint32_t i = 0; i < S::kStages && i < count; ++i)
+      if (lane == i) copy_tile(ring_u32 + i * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * i);
 
-#pragma unroll 1
-    for (uint32_t i = 0; i < count; ++i) {
-      const uint32_t s = i % S::kStages;
-      const uint8_t* const tile = ring + s * S::kTileBytes;
-      {
-        const uint32_t parity = (phases >> s) & 1u;
-        phases ^= 1u << s;
-        uint32_t polls = 0;
-        while (!mbar_try(bar_u32 + 8 * s, parity))
-          if (++polls >= kPolls) { timed_out = true; break; }
-      }
-      const uint32_t first = (my0 + kWarps * i) * kCacheTile;
+    float cap = kLeastCap;                                  // power of two that no step so far exceeds
+    uint32_t stage = 0;
+    auto take_tile = [&](auto masked_, const uint8_t* const tile, const uint32_t first) {
+      constexpr bool kMasked = decltype(masked_)::value;
       const uint32_t ka = token_of(g), kb = ka + 8;
       float sc[NT][4];                                      // scores: tokens ka, ka, kb, kb; rows 2t, 2t + 1, 2t, 2t + 1
 #pragma unroll
@@ -338,45 +341,66 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       for (int j = 0; j < J; ++j) {
         const uint2 ca = *reinterpret_cast<const uint2*>(tile + (j * 16 + ka) * 32 + 8 * t);
         const uint2 cb = *reinterpret_cast<const uint2*>(tile + (j * 16 + kb) * 32 + 8 * t);
+        const uint32_t pa = key_pair[ka * J + j], pb = key_pair[kb * J + j];
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
+        uint32_t ax[4], ay[4], bx[4], by[4];
+        unpack(ca.x, ax); unpack(ca.y, ay); unpack(cb.x, bx); unpack(cb.y, by);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t a[4] = {KeyCode<TYPE>::operand(ca.x, e), KeyCode<TYPE>::operand(cb.x, e), KeyCode<TYPE>::operand(ca.y, e),
-                                 KeyCode<TYPE>::operand(cb.y, e)};
+          const uint32_t a[4] = {ax[e], bx[e], ay[e], by[e]};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816<TYPE>(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
+          for (int nt = 0; nt < NT; ++nt) mma16816(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
         }
-        const uint32_t pa = key_pair[ka * J + j], pb = key_pair[kb * J + j];
         const float step_a = from_bits16<TYPE>(pa >> 16), step_b = from_bits16<TYPE>(pb >> 16);
-        const float rest_a = fmaf(-KeyCode<TYPE>::kBias, step_a, from_bits16<TYPE>(pa & 0xffffu));
-        const float rest_b = fmaf(-KeyCode<TYPE>::kBias, step_b, from_bits16<TYPE>(pb & 0xffffu));
+        const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pa & 0xffffu)), mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pb & 0xffffu));
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          sc[nt][0] += fmaf(step_a, acc[nt][0], rest_a * qsum[nt][j][0]);
-          sc[nt][1] += fmaf(step_a, acc[nt][1], rest_a * qsum[nt][j][1]);
-          sc[nt][2] += fmaf(step_b, acc[nt][2], rest_b * qsum[nt][j][0]);
-          sc[nt][3] += fmaf(step_b, acc[nt][3], rest_b * qsum[nt][j][1]);
-        }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sc[nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? mid_a : mid_b, qsum[nt][j][e & 1], sc[nt][e]));
       }
 
-      // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
-      const bool masked = (int64_t)first + kCacheTile > see_all;            // of the warp: some row does not see the whole tile
-      uint32_t seen = 0xffffffffu;                                          // bit 4 * nt + e
+      // ---- the pairs of the values ----------------------------------------------------------------------------------------
+      const uint8_t* const values = tile + 9 * D;
+      const uint32_t* const value_pair = reinterpret_cast<const uint32_t*>(values + 8 * D);
+      float step[J][2], mid[J][2];
       bool raise = false;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t pv = value_pair[(h ? kb : ka) * J + j];
+          step[j][h] = from_bits16<TYPE>(pv >> 16);
+          mid[j][h] = fmaf(8.0f, step[j][h], from_bits16<TYPE>(pv & 0xffffu));
+          if (kMasked && (int64_t)first + (h ? kb : ka) >= see_any) step[j][h] = mid[j][h] = 0.0f;      // was never written, perhaps
+          raise |= step[j][h] > cap;
+        }
+
+      // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
+      uint32_t seen = 0xffffffffu;                                          // bit 4 * nt + e
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          sc[nt][e] *= p.scale_log2;
-          if (masked && (int32_t)(e < 2 ? ka : kb) >= see[nt][e & 1] - (int32_t)first) {
+          sc[nt][e] *= factor[nt][e & 1];
+          if (kMasked && (int32_t)(e < 2 ? ka : kb) >= see[nt][e & 1] - (int32_t)first) {
             seen &= ~(1u << (4 * nt + e));
             sc[nt][e] = -INFINITY;
           }
           raise |= sc[nt][e] > top[nt][e & 1] + 8.0f;
         }
       if (__any_sync(0xffffffffu, raise)) {
+        float widest = 0.0f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) widest = fmaxf(widest, fmaxf(step[j][0], step[j][1]));
+#pragma unroll
+        for (int m = 4; m < 32; m <<= 1) widest = fmaxf(widest, __shfl_xor_sync(0xffffffffu, widest, m));
+        // the next power of two (an infinite step stays above every cap: its products are no numbers anyway)
+        const uint32_t bits = (__float_as_uint(fminf(widest, kMostCap)) + 0x007fffffu) & 0xff800000u;
+        const float cap_new = fmaxf(cap, __uint_as_float(bits)), shrink = cap / cap_new;
+        cap = cap_new;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -386,14 +410,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
             m = fmaxf(m, top[nt][e]);
-            const float f = exp2_approx(top[nt][e] - m);
+            const float f = exp2_approx(top[nt][e] - m), fo = f * shrink;
             top[nt][e] = m;
             lsum[nt][e] *= f;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
               osum[nt][j][e] *= f;
 #pragma unroll
-              for (int r = 0; r < 4; ++r) { o[nt][j][r][e] *= f; o[nt][j][r][e + 2] *= f; }
+              for (int r = 0; r < 4; ++r) { o[nt][j][r][e] *= fo; o[nt][j][r][e + 2] *= fo; }
             }
           }
       }
@@ -406,55 +430,77 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       }
 
       // ---- output ---------------------------------------------------------------------------------------------------------
-      const uint8_t* const values = tile + 9 * D;
-      const uint32_t* const value_pair = reinterpret_cast<const uint32_t*>(values + 8 * D);
+      const float times = __uint_as_float((260u << 23) - __float_as_uint(cap));           // 64 / cap, a power of two
       const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const uint32_t pa = value_pair[ka * J + j], pb = value_pair[kb * J + j];
-        const float step_a = from_bits16<TYPE>(pa >> 16), step_b = from_bits16<TYPE>(pb >> 16);
-        const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pa & 0xffffu)), mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pb & 0xffffu));
+        const float step_a = step[j][0] * times, step_b = step[j][1] * times;
         uint32_t bh[NT][2], bl[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float w[4] = {sc[nt][0] * step_a, sc[nt][1] * step_a, sc[nt][2] * step_b, sc[nt][3] * step_b};
-          float z[4] = {sc[nt][0] * mid_a, sc[nt][1] * mid_a, sc[nt][2] * mid_b, sc[nt][3] * mid_b};
-          if (masked) {                                     // what a row does not see may hold anything: no product with it
+          if (kMasked) {                                    // what a row does not see may hold anything: no product with it
+            float z[4] = {sc[nt][0] * mid[j][0], sc[nt][1] * mid[j][0], sc[nt][2] * mid[j][1], sc[nt][3] * mid[j][1]};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (!(seen >> (4 * nt + e) & 1u)) w[e] = z[e] = 0.0f;
+            osum[nt][j][0] += z[0] + z[2];
+            osum[nt][j][1] += z[1] + z[3];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) osum[nt][j][e & 1] = fmaf(sc[nt][e], mid[j][e >> 1], osum[nt][j][e & 1]);
           }
-          osum[nt][j][0] += z[0] + z[2];
-          osum[nt][j][1] += z[1] + z[3];
-          const uint32_t h0 = pack16<QSGD_TYPE_BF16>(w[0], w[1]), h1 = pack16<QSGD_TYPE_BF16>(w[2], w[3]);
-          const uint32_t l0 = pack16<QSGD_TYPE_BF16>(w[0] - __uint_as_float(h0 << 16), w[1] - __uint_as_float(h0 & 0xffff0000u));
-          const uint32_t l1 = pack16<QSGD_TYPE_BF16>(w[2] - __uint_as_float(h1 << 16), w[3] - __uint_as_float(h1 & 0xffff0000u));
+          const uint32_t h0 = pack16<QSGD_TYPE_F16>(w[0], w[1]), h1 = pack16<QSGD_TYPE_F16>(w[2], w[3]);
           bh[nt][0] = transpose8x8(h0);
           bh[nt][1] = transpose8x8(h1);
-          bl[nt][0] = transpose8x8(l0);
-          bl[nt][1] = transpose8x8(l1);
+          if (TYPE == QSGD_TYPE_F16) {
+            bl[nt][0] = transpose8x8(pack16<QSGD_TYPE_F16>(w[0] - from_bits16<QSGD_TYPE_F16>(h0 & 0xffffu), w[1] - from_bits16<QSGD_TYPE_F16>(h0 >> 16)));
+            bl[nt][1] = transpose8x8(pack16<QSGD_TYPE_F16>(w[2] - from_bits16<QSGD_TYPE_F16>(h1 & 0xffffu), w[3] - from_bits16<QSGD_TYPE_F16>(h1 >> 16)));
+          }
         }
         const uint8_t* const codes = values + j * 512 + 4 * g;
         const uint32_t c0 = *reinterpret_cast<const uint32_t*>(codes + va * 32), c1 = *reinterpret_cast<const uint32_t*>(codes + vb * 32);
         const uint32_t c2 = *reinterpret_cast<const uint32_t*>(codes + (va + 8) * 32), c3 = *reinterpret_cast<const uint32_t*>(codes + (vb + 8) * 32);
-        const uint32_t lo01 = __byte_perm(c0, c1, 0x5410), hi01 = __byte_perm(c0, c1, 0x7632);
-        const uint32_t lo23 = __byte_perm(c2, c3, 0x5410), hi23 = __byte_perm(c2, c3, 0x7632);
+        uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
+        unpack(__byte_perm(c0, c1, 0x5410), lo01); unpack(__byte_perm(c0, c1, 0x7632), hi01);
+        unpack(__byte_perm(c2, c3, 0x5410), lo23); unpack(__byte_perm(c2, c3, 0x7632), hi23);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {                       // rows: coordinates 64 j + 8 g + r, and those + 4
-          const uint32_t a[4] = {value_operand(lo01, r), value_operand(hi01, r), value_operand(lo23, r), value_operand(hi23, r)};
+          const uint32_t a[4] = {lo01[r], hi01[r], lo23[r], hi23[r]};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            mma16816<QSGD_TYPE_BF16>(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
-            mma16816<QSGD_TYPE_BF16>(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
+            mma16816(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
+            if (TYPE == QSGD_TYPE_F16) mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
           }
         }
       }
+    };
+
+#pragma unroll 1
+    for (uint32_t i = 0; i < count; ++i) {
+      {
+        const uint32_t parity = (phases >> stage) & 1u;
+        phases ^= 1u << stage;
+        uint32_t polls = 0;
+        while (!mbar_try(bar_u32 + 8 * stage, parity))
+          if (++polls >= kPolls) { timed_out = true; break; }
+      }
+      const uint32_t first = (my0 + kWarps * i) * kCacheTile;
+      const uint8_t* const tile = ring + stage * S::kTileBytes;
+      if ((int64_t)first + kCacheTile > see_all) take_tile(Constant<true>(), tile, first);     // some row does not see the whole tile
+      else take_tile(Constant<false>(), tile, first);
       __syncwarp();                                         // the stage's readers are done
-      issue(i + S::kStages);
+      const uint32_t next = i + S::kStages;
+      if (next < count) {
+        if ((next & 31u) == 0) source = next + lane < count ? look_up(next + lane) : nullptr;
+        if (lane == (next & 31u)) copy_tile(ring_u32 + stage * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * stage);
+      }
+      if (++stage == S::kStages) stage = 0;
     }
 
     // ---- the warps' parts are joined ----------------------------------------------------------------------------------------
     float* const mine = reinterpret_cast<float*>(ring);
+    const float held = cap * (1.0f / 64.0f);                // undoes the power of two in o
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -470,9 +516,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll
           for (int m = 4; m < 32; m <<= 1) z += __shfl_xor_sync(0xffffffffu, z, m);
           float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
-          *reinterpret_cast<float4*>(at) = make_float4(o[nt][j][0][e] + z, o[nt][j][1][e] + z, o[nt][j][2][e] + z, o[nt][j][3][e] + z);
-          *reinterpret_cast<float4*>(at + 4) =
-              make_float4(o[nt][j][0][e + 2] + z, o[nt][j][1][e + 2] + z, o[nt][j][2][e + 2] + z, o[nt][j][3][e + 2] + z);
+          float v[8];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) { v[r] = fmaf(o[nt][j][r][e], held, z); v[r + 4] = fmaf(o[nt][j][r][e + 2], held, z); }
+          *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
         }
       }
     __syncthreads();
