@@ -405,8 +405,9 @@ int qsgd_cache_read(const qsgd_cache* cache, const qsgd_cache_rows* rows, void* 
  *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q . k_t),  lse = ln sum_t p_t
  * over what the cache stands for. A row that sees no token (an empty sequence, or a row in front of the first
  * token) gives 0 and -infinity.
- *   q, out       [rows][q_heads][head_dim] as k and v above; scores, sums and the output are kept in fp32,
- *                p in 16 bits of fraction, the output is rounded to the type once
+ *   q, out       [rows][q_heads][head_dim] as k and v above; scores, sums and the output are kept in fp32, p_t * step
+ *                in 11 bits of fraction (22 for F16), the output is rounded to the type once. Where a sequence is split over the GPU
+ *                follows from all lengths of the call, so the same call gives the same bits, another batch around a sequence perhaps not.
  *   lse          [rows][q_heads] fp32, contiguous, or NULL
  *   workspace    qsgd_cache_attend_workspace_bytes() of scratch, 16-byte aligned. Every part that is read was
  *                written by the same call, so nothing needs clearing; calls that overlap on the GPU need one each.

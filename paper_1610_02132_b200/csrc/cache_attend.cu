@@ -16,11 +16,13 @@
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
-// What bounds it: with up to 8 rows a key head, HBM: 9/8 * head_dim bytes a token and head, each read once, against about 150
-// integer and 24 tensor instructions per 16 tokens. So everything is arranged around the stream of tiles. The tiles of all (sequence, key
-// head, row tile) segments form one line of units; CTA i takes the i-th of equal stretches of it, whatever the lengths are, and warp w of a CTA every
-// eighth tile of a piece, through a ring of its own that bulk copies fill. A piece that is a whole segment is written out; the
-// others leave (m, sum, o) in the workspace, at most two a CTA, and a second kernel joins them, a CTA for each boundary and row.
+// What bounds it: with up to 8 rows a key head, HBM: 9/8 * head_dim bytes a token and head, each read once, against about 100
+// integer and 16 tensor instructions per 16 tokens. So everything is arranged around the stream of tiles. The tiles of all (sequence, key
+// head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
+// takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
+// written out by its warp; what spans warps of a CTA is joined in shared memory; what spans CTAs leaves (m, sum, o) in the workspace,
+// at most two parts a CTA, and a second kernel joins those. (With tiles dealt out to the eight warps of a CTA, which met at the end of each
+// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us: a CTA had up to 40 segments one after another.)
 #include "cache.cuh"
 
 namespace qsgd {
@@ -29,7 +31,8 @@ namespace {
 
 constexpr uint32_t kWarps = 8, kThreads = 32 * kWarps;
 constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
-constexpr uint32_t kLeastChunk = kWarps;  // units of a stretch: a tile for each warp
+constexpr uint32_t kLeastStretch = 4;     // units of a warp's stretch at least
+constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kPolls = 1u << 22;
 constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;     // 2^-120, 2^126
@@ -38,12 +41,15 @@ constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that
 template <bool V>
 struct Constant { static constexpr bool value = V; };
 
-struct JoinInfo {                         // of the piece that a CTA begins with, written by every CTA of every call
-  uint32_t parts;                         // CTAs from `first` on hold a part of the segment; 0: nothing to join at this boundary
-  uint32_t first, first_slot;             // the segment's first part
-  uint32_t head, row0, rows;              // first row (query * group + head in group) of the row tile, rows in it
+struct Rows {                             // of a segment: which rows of which sequence
+  uint32_t head, row0, rows;              // key head, first row (query * group + head in group), number of rows
   uint32_t start;                         // first query row of the sequence
-  uint32_t unused;
+};
+
+struct JoinInfo {                         // of the segment that a CTA's stretch begins inside of, written by every CTA of every call
+  Rows rows;
+  uint32_t parts, first;                  // CTAs from `first` on hold a part each; 0: another CTA says so, or there is none
+  uint32_t unused[2];
 };
 
 struct AttendParams {
@@ -127,7 +133,7 @@ __device__ __forceinline__ Sequence sequence_at(const AttendParams& p, uint32_t 
   q.tiles = (uint32_t)((s.length + kCacheTile - 1) / kCacheTile);
   if (q.tiles == 0) q.tiles = 1;          // nothing to attend to: a unit that writes the empty result
   q.row_tiles = (s.n * p.group + ROWS - 1) / ROWS;
-  q.units = (uint64_t)p.c.heads * q.row_tiles * q.tiles;
+  q.units = (uint64_t)p.c.heads * q.row_tiles * (q.tiles + kSegmentCost);
   return q;
 }
 
@@ -138,12 +144,25 @@ struct Shape {
   // Ring stages of a warp: about 9 KB of tiles in flight at NT = 1 (two CTAs an SM: 150 KB), and room for the warp's part of the join.
   static constexpr uint32_t kStages = D == 64 ? 8 : D == 128 ? 4 : 3;
   static constexpr uint32_t kRing = kStages * kTileBytes;
-  static constexpr uint32_t kRowFloats = D + 8;                             // of the join: rows shifted by 8 banks
+  static constexpr uint32_t kRowFloats = D + 8;                             // of a part: rows shifted by 8 banks
   static constexpr uint32_t kPart = kRows * kRowFloats * 4;
-  static constexpr uint32_t kPerWarp = ((kRing > kPart ? kRing : kPart) + 127) / 128 * 128;
+  static constexpr uint32_t kRingSpace = ((kRing > kPart ? kRing : kPart) + 127) / 128 * 128;
+  // A warp's memory: the ring, whose place its last part takes, and the part of the segment that its stretch begins inside of.
+  static constexpr uint32_t kPerWarp = kRingSpace + (kPart + 127) / 128 * 128;
   static constexpr uint32_t kSmem = kWarps * kPerWarp;
   static constexpr int kCtas = D <= 128 && NT == 1 ? 2 : 1;
 };
+
+// Where a row of a segment goes, and its logarithm of the sum.
+__device__ __forceinline__ uint16_t* out_row(const AttendParams& p, const Rows& s, uint32_t r, uint64_t* lse_at) {
+  const uint32_t query = (s.row0 + r) / p.group, hh = s.head * p.group + (s.row0 + r) - query * p.group;
+  const uint64_t row = (uint64_t)s.start + query;
+  *lse_at = row * p.q_heads + hh;
+  return p.out + row * p.out_token + (uint64_t)hh * p.out_head;
+}
+// A row that saw no token has no maximum and no sum.
+__device__ __forceinline__ bool saw(float m, float l) { return m > kNoMax || !(l == 0.0f); }
+__device__ __forceinline__ float log_sum(float m, float l) { return saw(m, l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
 
 template <int TYPE, int D, int NT>
 __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_attend_kernel(const __grid_constant__ AttendParams p) {
@@ -152,9 +171,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t bars[kWarps][S::kStages];
   __shared__ uint64_t scan[kWarps];
-  __shared__ uint64_t found_base;
-  __shared__ uint32_t found_b;
-  __shared__ float part_m[kWarps][R], part_l[kWarps][R];
+  __shared__ uint64_t found_base[kWarps];
+  __shared__ uint32_t found_b[kWarps];
+  __shared__ float part_m[2][kWarps][R], part_l[2][kWarps][R];
+  __shared__ Rows part_rows[2][kWarps];
+  __shared__ uint32_t part_open[2][kWarps];                 // 0: no part; 1: the segment ends inside the warp's stretch; 2: it goes on
+  __shared__ uint64_t head_begin, head_end;                 // of the segment that the CTA's stretch begins inside of, on the line of units
 
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, t = lane & 3u;
   uint8_t* const ring = smem + warp * S::kPerWarp;
@@ -163,11 +185,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll
     for (uint32_t s = 0; s < S::kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_u32 + 8 * s) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    part_open[0][warp] = part_open[1][warp] = 0;
   }
   __syncwarp();
   chain_wait();
 
-  // ---- this CTA's stretch of the line of units, and the sequence that it begins in -------------------------------------
+  // ---- the warps' stretches of the line of units, and the sequences that they begin in -----------------------------------
   uint64_t total = 0;
   for (uint32_t b = tid; b < p.c.sequences; b += kThreads) total += sequence_at<R>(p, b).units;
 #pragma unroll
@@ -177,15 +200,16 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
   total = 0;
 #pragma unroll
   for (uint32_t w = 0; w < kWarps; ++w) total += scan[w];
-  uint64_t chunk = (total + gridDim.x - 1) / gridDim.x;
-  if (chunk < kLeastChunk) chunk = kLeastChunk;
-  const uint64_t u0 = blockIdx.x * chunk, u1 = u0 + chunk < total ? u0 + chunk : total;
-  if (u0 >= total) {
+  uint64_t stretch = (total + (uint64_t)gridDim.x * kWarps - 1) / ((uint64_t)gridDim.x * kWarps);
+  if (stretch < kLeastStretch) stretch = kLeastStretch;
+  const uint64_t cta0 = (uint64_t)blockIdx.x * kWarps * stretch;
+  if (cta0 >= total) {
     if (tid == 0) p.join[blockIdx.x].parts = 0;
     return;
   }
   uint64_t base = 0;
-  for (uint32_t b0 = 0;; b0 += kThreads) {                 // ends: u0 < total
+  const uint64_t last_start = cta0 + (kWarps - 1) * stretch < total ? cta0 + (kWarps - 1) * stretch : total - 1;
+  for (uint32_t b0 = 0;; b0 += kThreads) {                 // ends: last_start < total
     const uint64_t mine = b0 + tid < p.c.sequences ? sequence_at<R>(p, b0 + tid).units : 0;
     uint64_t sum = mine;
 #pragma unroll
@@ -203,26 +227,42 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       all += scan[w];
     }
     here += sum - mine;
-    if (here <= u0 && u0 < here + mine) { found_base = here; found_b = b0 + tid; }
+    if (mine && here < cta0 + kWarps * stretch && here + mine > cta0) {
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) {
+        const uint64_t at = cta0 + w * stretch;
+        if (here <= at && at < here + mine) { found_base[w] = here; found_b[w] = b0 + tid; }
+      }
+    }
     base += all;
-    if (base > u0) break;
+    if (base > last_start) break;
   }
   __syncthreads();
 
-  Sequence seq = sequence_at<R>(p, found_b);
-  uint64_t seq_base = found_base;
+  const uint64_t u0 = cta0 + warp * stretch, u1 = u0 + stretch < total ? u0 + stretch : total;
+  Sequence seq{};
+  uint64_t seq_base = 0;
+  if (u0 < u1) {
+    seq = sequence_at<R>(p, found_b[warp]);
+    seq_base = found_base[warp];
+  }
   uint32_t phases = 0;                                      // bit s: parity of the next wait on stage s
   bool timed_out = false;
 
+#pragma unroll 1
   for (uint64_t u = u0; u < u1;) {
     while (u >= seq_base + seq.units) {                     // (a sequence without rows has no units)
       seq_base += seq.units;
       seq = sequence_at<R>(p, seq.b + 1);
     }
     const uint64_t off = u - seq_base;
-    const uint64_t segment = off / seq.tiles;
-    const uint32_t tile0 = (uint32_t)(off - segment * seq.tiles);
-    const uint32_t tile1 = u1 - u < seq.tiles - tile0 ? tile0 + (uint32_t)(u1 - u) : seq.tiles;
+    const uint32_t span = seq.tiles + kSegmentCost;         // units of a segment: its cost, then its tiles
+    const uint64_t segment = off / span;
+    const uint32_t x0 = (uint32_t)(off - segment * span), x1 = u1 - u < span - x0 ? x0 + (uint32_t)(u1 - u) : span;
+    const uint32_t tile0 = x0 > kSegmentCost ? x0 - kSegmentCost : 0u, tile1 = x1 > kSegmentCost ? x1 - kSegmentCost : 0u;
+    const uint64_t begin = u - x0 + kSegmentCost;           // its first tile on the line
+    u += x1 - x0;
+    if (tile0 == tile1) continue;                           // the stretch ends in front of its tiles
     const uint32_t head = (uint32_t)(segment / seq.row_tiles), row_tile = (uint32_t)(segment - (uint64_t)head * seq.row_tiles);
     const uint32_t row0 = row_tile * R, rows_all = seq.n * p.group;
     const uint32_t rows = rows_all - row0 < (uint32_t)R ? rows_all - row0 : (uint32_t)R;
@@ -299,8 +339,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     const int64_t see_any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
     uint32_t tile_end = see_any <= 0 ? 0u : (uint32_t)((see_any + kCacheTile - 1) / kCacheTile);
     if (tile_end > tile1) tile_end = tile1;
-    const uint32_t my0 = tile0 + warp;
-    const uint32_t count = my0 < tile_end ? (tile_end - my0 + kWarps - 1) / kWarps : 0u;      // tiles of this warp
+    const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
 
     float o[NT][J][4][4], lsum[NT][2], osum[NT][J][2], top[NT][2];
 #pragma unroll
@@ -318,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     // ---- the warp's tiles ----------------------------------------------------------------------------------------------
     // Lane l knows where tiles l, l + 32, ... of the warp lie, and starts their copies.
     auto look_up = [&](uint32_t i) -> const uint8_t* {
-      const uint32_t tile = my0 + kWarps * i, page = tile / p.c.page_tiles;
+      const uint32_t tile = tile0 + i, page = tile / p.c.page_tiles;
       int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
       if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
       return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
@@ -485,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         while (!mbar_try(bar_u32 + 8 * stage, parity))
           if (++polls >= kPolls) { timed_out = true; break; }
       }
-      const uint32_t first = (my0 + kWarps * i) * kCacheTile;
+      const uint32_t first = (tile0 + i) * kCacheTile;
       const uint8_t* const tile = ring + stage * S::kTileBytes;
       if ((int64_t)first + kCacheTile > see_all) take_tile(Constant<true>(), tile, first);     // some row does not see the whole tile
       else take_tile(Constant<false>(), tile, first);
@@ -498,8 +537,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       if (++stage == S::kStages) stage = 0;
     }
 
-    // ---- the warps' parts are joined ----------------------------------------------------------------------------------------
-    float* const mine = reinterpret_cast<float*>(ring);
+    // ---- the segment's rows, or a part of them -----------------------------------------------------------------------------
+    const bool from_front = tile0 == 0, to_end = tile1 == seq.tiles;
+    const uint32_t slot = from_front ? 1u : 0u;             // a part without the segment's front is the stretch's first, one with it the last
+    const Rows which{head, row0, rows, seq.start};
+    float* const mine = reinterpret_cast<float*>(slot ? ring : ring + S::kRingSpace);
     const float held = cap * (1.0f / 64.0f);                // undoes the power of two in o
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -509,65 +551,92 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         float l = lsum[nt][e];
 #pragma unroll
         for (int m = 4; m < 32; m <<= 1) l += __shfl_xor_sync(0xffffffffu, l, m);
-        if (g == 0) { part_m[warp][r] = top[nt][e]; part_l[warp][r] = l; }
+        uint64_t lse_at = 0;
+        uint16_t* out = nullptr;
+        float over = 0.0f;
+        if (from_front && to_end) {
+          if (r < rows) {
+            out = out_row(p, which, r, &lse_at);
+            if (p.lse && g == 0) p.lse[lse_at] = log_sum(top[nt][e], l);
+            over = saw(top[nt][e], l) ? 1.0f / l : 0.0f;
+          }
+        } else if (g == 0) {
+          part_m[slot][warp][r] = top[nt][e];
+          part_l[slot][warp][r] = l;
+        }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           float z = osum[nt][j][e];
 #pragma unroll
           for (int m = 4; m < 32; m <<= 1) z += __shfl_xor_sync(0xffffffffu, z, m);
-          float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
           float v[8];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) { v[r] = fmaf(o[nt][j][r][e], held, z); v[r + 4] = fmaf(o[nt][j][r][e + 2], held, z); }
-          *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
-          *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+          for (int i = 0; i < 4; ++i) { v[i] = fmaf(o[nt][j][i][e], held, z); v[i + 4] = fmaf(o[nt][j][i][e + 2], held, z); }
+          if (out) {
+            *reinterpret_cast<uint4*>(out + 64 * j + 8 * g) =
+                make_uint4(pack16<TYPE>(v[0] * over, v[1] * over), pack16<TYPE>(v[2] * over, v[3] * over), pack16<TYPE>(v[4] * over, v[5] * over),
+                           pack16<TYPE>(v[6] * over, v[7] * over));
+          } else if (!(from_front && to_end)) {
+            float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
+            *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+          }
         }
       }
-    __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == seq.tiles;
-    float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + (u == u0 ? 0 : 1)) * part_floats(R, D);
-    for (uint32_t i = tid; i < rows * (D / 4); i += kThreads) {
+    if (!(from_front && to_end) && lane == 0) {
+      part_rows[slot][warp] = which;
+      part_open[slot][warp] = to_end ? 1u : 2u;
+      if (warp == 0 && slot == 0) { head_begin = begin; head_end = begin + seq.tiles; }
+    }
+  }
+  if (timed_out) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+
+  // ---- what spans warps: joined, and written out where it ends in this CTA -------------------------------------------------
+  __syncthreads();
+  JoinInfo info{};
+#pragma unroll 1
+  for (uint32_t k = 0; k <= kWarps; ++k) {                  // parts that begin in front of the CTA, then those that begin in warp k - 1
+    const uint32_t slot = k ? 1u : 0u, w0 = k ? k - 1 : 0u;
+    if (part_open[slot][w0] == 0) continue;
+    uint32_t w1 = w0;                                       // last warp that has some of the segment
+    bool goes_on = part_open[slot][w0] == 2;
+    while (goes_on && w1 + 1 < kWarps) goes_on = part_open[0][++w1] == 2;
+    const Rows which = part_rows[slot][w0];
+    const bool out_here = k != 0 && !goes_on;
+    float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
+    for (uint32_t i = tid; i < which.rows * (D / 4); i += kThreads) {
       const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
-      float m = kNoMax, l = 0.0f;
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) m = fmaxf(m, part_m[w][r]);
-      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) {
-        const float f = exp2_approx(part_m[w][r] - m);
-        const float4 v = *reinterpret_cast<const float4*>(smem + w * S::kPerWarp + (r * S::kRowFloats + 4 * d4) * 4);
-        l = fmaf(f, part_l[w][r], l);
-        sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+      float m = part_m[slot][w0][r], l = part_l[slot][w0][r];
+      float4 sum = *reinterpret_cast<const float4*>(smem + w0 * S::kPerWarp + (slot ? 0 : S::kRingSpace) + (r * S::kRowFloats + 4 * d4) * 4);
+      for (uint32_t w = w0 + 1; w <= w1; ++w) {
+        const float wm = part_m[0][w][r], high = fmaxf(m, wm), f = exp2_approx(m - high), e = exp2_approx(wm - high);
+        const float4 v = *reinterpret_cast<const float4*>(smem + w * S::kPerWarp + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4);
+        m = high;
+        l = fmaf(e, part_l[0][w][r], f * l);
+        sum.x = fmaf(e, v.x, f * sum.x); sum.y = fmaf(e, v.y, f * sum.y); sum.z = fmaf(e, v.z, f * sum.z); sum.w = fmaf(e, v.w, f * sum.w);
       }
-      if (whole) {
-        const uint32_t query = (row0 + r) / p.group, hh = head * p.group + (row0 + r) - query * p.group;
-        const uint64_t row = seq.start + query;
-        const bool sees = seq.length - (int64_t)(seq.n - 1 - query) > 0;
-        const float f = sees ? 1.0f / l : 0.0f;
-        *reinterpret_cast<uint2*>(p.out + row * p.out_token + (uint64_t)hh * p.out_head + 4 * d4) =
-            sees ? make_uint2(pack16<TYPE>(sum.x * f, sum.y * f), pack16<TYPE>(sum.z * f, sum.w * f)) : make_uint2(0u, 0u);
-        if (p.lse && d4 == 0) p.lse[row * p.q_heads + hh] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      if (out_here) {
+        uint64_t lse_at;
+        uint16_t* const out = out_row(p, which, r, &lse_at);
+        const float over = saw(m, l) ? 1.0f / l : 0.0f;
+        *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
+        if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
       } else {
         *reinterpret_cast<float4*>(part + r * D + 4 * d4) = sum;
         if (d4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
       }
     }
-    if (u == u0 && tid == 0) {
-      JoinInfo j{0, 0, 0, head, row0, rows, seq.start, 0};
-      const uint64_t begin = u - tile0, end = begin + seq.tiles;            // the segment on the line of units
-      if (tile0 && begin / chunk == blockIdx.x - 1) {       // this CTA's start is the first boundary inside the segment
-        j.first = blockIdx.x - 1;
-        j.first_slot = begin == (uint64_t)(blockIdx.x - 1) * chunk ? 0u : 1u;
-        j.parts = (uint32_t)((end - 1) / chunk) - j.first + 1;
+    if (k == 0) {
+      const uint64_t per_cta = kWarps * stretch;
+      const uint32_t first = (uint32_t)(head_begin / per_cta);
+      if (first + 1 == blockIdx.x) {                        // this CTA's start is the first such boundary inside the segment
+        info.rows = which;
+        info.first = first;
+        info.parts = (uint32_t)((head_end - 1) / per_cta) - first + 1;
       }
-      p.join[blockIdx.x] = j;
     }
-    // Bulk copies write where these reads were: order the two kinds of access before the next piece's first copy.
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
-    u += tile1 - tile0;
   }
-  if (timed_out) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+  if (tid == 0) p.join[blockIdx.x] = info;
 }
 
 // Parts of a segment that several CTAs hold, one row to a CTA: a warp to every eighth part, each D / 32 coordinates a lane.
@@ -579,12 +648,12 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_const
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, r = blockIdx.x / n, cta = blockIdx.x - r * n;
   chain_wait();
   const JoinInfo j = p.join[cta];
-  if (j.parts == 0 || r >= j.rows) return;
+  if (j.parts == 0 || r >= j.rows.rows) return;
   float m = kNoMax, l = 0.0f, o[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) o[i] = 0.0f;
   for (uint32_t k = warp; k < j.parts; k += kWarps) {
-    const float* part = p.parts + ((uint64_t)(j.first + k) * 2 + (k == 0 ? j.first_slot : 0u)) * part_floats(R, D);
+    const float* part = p.parts + ((uint64_t)(j.first + k) * 2 + (k == 0 ? 1u : 0u)) * part_floats(R, D);
     const float pm = part[R * D + r], pl = part[R * D + R + r], top = fmaxf(m, pm), f = exp2_approx(m - top), e = exp2_approx(pm - top);
     l = fmaf(e, pl, l * f);
 #pragma unroll
@@ -607,11 +676,10 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_const
       l = fmaf(f, part_l[w], l);
       v = fmaf(f, sum[w][threadIdx.x], v);
     }
-    const uint32_t query = (j.row0 + r) / p.group, hh = j.head * p.group + (j.row0 + r) - query * p.group;
-    const uint64_t row = j.start + query;
-    const bool sees = m > kNoMax || !(l == 0.0f);           // no token: no maximum and no sum
-    p.out[row * p.out_token + (uint64_t)hh * p.out_head + threadIdx.x] = sees ? (uint16_t)to_bits16<TYPE>(v / l) : (uint16_t)0;
-    if (p.lse && threadIdx.x == 0) p.lse[row * p.q_heads + hh] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    uint64_t lse_at;
+    uint16_t* const out = out_row(p, j.rows, r, &lse_at);
+    out[threadIdx.x] = (uint16_t)to_bits16<TYPE>(saw(m, l) ? v / l : 0.0f);
+    if (p.lse && threadIdx.x == 0) p.lse[lse_at] = log_sum(m, l);
   }
 }
 

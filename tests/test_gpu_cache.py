@@ -299,7 +299,9 @@ def test_places_that_the_cache_has_not(what):
             Q.qsgd_cache_write(f.cache, f.table, f.len, k * 0, v * 0, status, starts=starts)
         assert int(status.item()) == Q.DEV_PAGE, call
     rows = [] if what == "starts" else [0, 2]
-    assert torch.equal(out[rows], good[rows]) and torch.equal(k[rows], good_k[rows])
+    # (where a sequence is split follows from all lengths: two results differ by a rounding each, of the type and of p * step, here below 2^-2)
+    assert torch.allclose(out[rows].float(), good[rows].float(), rtol=2 * 2.0 ** -8, atol=2 * 2.0 ** -11 * 8 * 0.25)
+    assert torch.equal(k[rows], good_k[rows])
     touched = (f.cache.data != before).flatten(1).any(1).nonzero().flatten().tolist()
     assert set(touched) <= {int(p) for p in f.table_host.flatten() if p >= 0}
 
