@@ -3,16 +3,18 @@
 // For a query row q (one head of one query), with keys k_t = lo + step * c_t (a group g of 64 coordinates has its own pair):
 //   s_t = sum_g step_tg * (q_g . c_tg) + lo_tg * sum(q_g),   p_t = 2^(a s_t - m),   a = scale * log2(e),
 //   o   = (sum_t p_t v_t) / sum_t p_t,    sum_t p_t v_tg = sum_t (p_t step_tg) (c_tg - 8) + sum_t p_t (lo_tg + 8 step_tg).
-// The codes go to the tensor cores as they are, centred (c - 8 is exact in fp16), and the pairs are applied in fp32:
-//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp32 sums). A row of q is multiplied by a power of
-//            two that puts its largest number at 8 to 16: 16-bit numbers of either type fit fp16 then, but for what lies 2^-17 and more below
-//            the largest, which loses no more than fp32 sums do.
+// The codes go to the tensor cores as they are and the pairs are applied in fp32:
+//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp16 operands, fp32 sums). A row of q is multiplied by a
+//            power of two that puts its largest number at 2^11: 16-bit numbers of either type fit fp16 then, but for what lies 2^-21 and more
+//            below the largest, which loses no more than fp32 sums do.
 //   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two that puts the largest step so far at 64
 //            (p may reach 2^8). For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
 //            For fp16 p * step goes as the sum of two fp16 numbers, since one would put as much error into the output as rounding it does.
-// Unpacking: a nibble under the exponent of 1024 or of 64 is 1024 + c or 64 + c where it stands, so four pairs of codes take four
-// logical operations and one shift, and a subtraction each on the otherwise idle multiply pipe. (With bf16 operands, whose seven bits of fraction
-// need every nibble moved into place, and p in two bf16 numbers: 143 us against 4 fewer shifts per word and half the products here.)
+//            Every tile's -8 sum(p step) is added by a product with a constant operand: these sums run over the whole sequence, and without it
+//            8 sum(p step) would grow until what is left of the rounded sums, after taking it off at the end, is its error.
+// A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
+// and one shift; the powers of two are undone in q, and in the output's scale at the end. (Nibbles under the exponent of 1024 or of 64 and a
+// subtraction each: 101 us against %s for 64 sequences of 100 to 8000 tokens, 8 heads of 128; bf16 operands: 143.)
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
@@ -103,18 +105,27 @@ __device__ __forceinline__ float exp2_approx(float v) {
   return r;
 }
 
-// The codes of a word, less 8: pair s holds nibble s of either half.
-__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
+// The codes of a word as fp16 pairs, pair s = nibble s of either half: c * 2^-24 for even s, c * 2^-20 for odd ones.
 __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
   const uint32_t v = w >> 8;
-  c[0] = sub_f16x2((w & 0x000f000fu) | 0x64006400u, 0x64086408u);          // 1024 + c, less 1032
-  c[1] = sub_f16x2((w & 0x00f000f0u) | 0x54005400u, 0x54805480u);          // 64 + c, less 72
-  c[2] = sub_f16x2((v & 0x000f000fu) | 0x64006400u, 0x64086408u);
-  c[3] = sub_f16x2((v & 0x00f000f0u) | 0x54005400u, 0x54805480u);
+  c[0] = w & 0x000f000fu;
+  c[1] = w & 0x00f000f0u;
+  c[2] = v & 0x000f000fu;
+  c[3] = v & 0x00f000f0u;
+}
+
+template <int J>
+__device__ __forceinline__ void load_pairs(const uint32_t* at, uint32_t (&v)[J]) {      // at: on a boundary of J words if that is a power of two
+  if constexpr (J == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(at);
+    v[0] = x.x; v[1] = x.y;
+  } else if constexpr (J == 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(at);
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < J; ++j) v[j] = at[j];
+  }
 }
 
 // One sequence on the line of units.
@@ -246,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     seq = sequence_at<R>(p, found_b[warp]);
     seq_base = found_base[warp];
   }
-  uint32_t phases = 0;                                      // bit s: parity of the next wait on stage s
+  uint32_t stage = 0, parity = 0;                           // of the next wait; the ring goes on from segment to segment
   bool timed_out = false;
 
 #pragma unroll 1
@@ -298,13 +309,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         }
       top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 1));
       top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 2));
-      // 2^(3 - e) for a largest number of [2^e, 2^(e + 1)); nothing to scale in a row of zeros, infinities or NaN
+      // 2^(11 - e) for a largest number of [2^e, 2^(e + 1)); nothing to scale in a row of zeros, infinities or NaN
       const int32_t e = (int32_t)(__float_as_uint(top_q) >> 23) - 127;
-      int32_t up = 3 - e;
+      int32_t up = 11 - e;
       if (up > 120) up = top_q > 0.0f ? 120 : 0;
       if (e == 128) up = 0;
       const float times = __uint_as_float((uint32_t)(127 + up) << 23);
-      const float back = p.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+      const float back = p.scale_log2 * 16777216.0f * __uint_as_float((uint32_t)(127 - up) << 23);        // 2^24: see unpack
       factor[nt][0] = __shfl_sync(0xffffffffu, back, 8 * t);
       factor[nt][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
@@ -319,11 +330,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll
           for (int i = 0; i < 4; ++i) {                     // coordinates i and i + 4 of each word of eight
             sum += x[i] + x[i + 4];
-            qf[nt][j][i][h] = pack16<QSGD_TYPE_F16>(x[i], x[i + 4]);
+            qf[nt][j][i][h] = pack16<QSGD_TYPE_F16>(i & 1 ? x[i] * 0.0625f : x[i], i & 1 ? x[i + 4] * 0.0625f : x[i + 4]);
           }
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        sum *= 5.9604644775390625e-08f;                     // 2^-24, as the codes
         qsum[nt][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
         qsum[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
@@ -335,10 +347,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       }
     }
     // Tokens that the first row sees (all rows see them) and that the last row sees.
-    const int64_t see_all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group);
-    const int64_t see_any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
-    uint32_t tile_end = see_any <= 0 ? 0u : (uint32_t)((see_any + kCacheTile - 1) / kCacheTile);
+    const int64_t all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group), any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
+    const uint32_t see_all = all > 0 ? (uint32_t)all : 0u, see_any = any > 0 ? (uint32_t)any : 0u;
+    uint32_t tile_end = (see_any + kCacheTile - 1) / kCacheTile;
     if (tile_end > tile1) tile_end = tile1;
+    const uint32_t clear = see_all / kCacheTile;            // tiles in front of this one are seen whole by every row
     const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
 
     float o[NT][J][4][4], lsum[NT][2], osum[NT][J][2], top[NT][2];
@@ -364,23 +377,25 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     };
     const uint8_t* source = lane < count ? look_up(lane) : nullptr;
 #pragma unroll 1
-    for (uint32_t i = 0; i < S::kStages && i < count; ++i)
-      if (lane == i) copy_tile(ring_u32 + i * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * i);
+    for (uint32_t i = 0; i < S::kStages && i < count; ++i) {
+      const uint32_t at = stage + i < S::kStages ? stage + i : stage + i - S::kStages;
+      if (lane == i) copy_tile(ring_u32 + at * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * at);
+    }
 
     float cap = kLeastCap;                                  // power of two that no step so far exceeds
-    uint32_t stage = 0;
     auto take_tile = [&](auto masked_, const uint8_t* const tile, const uint32_t first) {
       constexpr bool kMasked = decltype(masked_)::value;
       const uint32_t ka = token_of(g), kb = ka + 8;
       float sc[NT][4];                                      // scores: tokens ka, ka, kb, kb; rows 2t, 2t + 1, 2t, 2t + 1
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
-      const uint32_t* const key_pair = reinterpret_cast<const uint32_t*>(tile + 8 * D);
+      uint32_t pair_a[J], pair_b[J];
+      load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + ka * J, pair_a);
+      load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + kb * J, pair_b);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const uint2 ca = *reinterpret_cast<const uint2*>(tile + (j * 16 + ka) * 32 + 8 * t);
         const uint2 cb = *reinterpret_cast<const uint2*>(tile + (j * 16 + kb) * 32 + 8 * t);
-        const uint32_t pa = key_pair[ka * J + j], pb = key_pair[kb * J + j];
         float acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
@@ -392,30 +407,32 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma16816(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
         }
-        const float step_a = from_bits16<TYPE>(pa >> 16), step_b = from_bits16<TYPE>(pb >> 16);
-        const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pa & 0xffffu)), mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pb & 0xffffu));
+        const float step_a = from_bits16<TYPE>(pair_a[j] >> 16), step_b = from_bits16<TYPE>(pair_b[j] >> 16);
+        const float lo_a = from_bits16<TYPE>(pair_a[j] & 0xffffu), lo_b = from_bits16<TYPE>(pair_b[j] & 0xffffu);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            sc[nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? mid_a : mid_b, qsum[nt][j][e & 1], sc[nt][e]));
+            sc[nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? lo_a : lo_b, qsum[nt][j][e & 1], sc[nt][e]));
       }
 
       // ---- the pairs of the values ----------------------------------------------------------------------------------------
       const uint8_t* const values = tile + 9 * D;
-      const uint32_t* const value_pair = reinterpret_cast<const uint32_t*>(values + 8 * D);
-      float step[J][2], mid[J][2];
-      bool raise = false;
+      load_pairs<J>(reinterpret_cast<const uint32_t*>(values + 8 * D) + ka * J, pair_a);
+      load_pairs<J>(reinterpret_cast<const uint32_t*>(values + 8 * D) + kb * J, pair_b);
+      float step[J][2], mid[J][2], widest = 0.0f;
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t pv = value_pair[(h ? kb : ka) * J + j];
+          const uint32_t pv = h ? pair_b[j] : pair_a[j];
           step[j][h] = from_bits16<TYPE>(pv >> 16);
           mid[j][h] = fmaf(8.0f, step[j][h], from_bits16<TYPE>(pv & 0xffffu));
-          if (kMasked && (int64_t)first + (h ? kb : ka) >= see_any) step[j][h] = mid[j][h] = 0.0f;      // was never written, perhaps
-          raise |= step[j][h] > cap;
+          if (kMasked && first + (h ? kb : ka) >= see_any) step[j][h] = mid[j][h] = 0.0f;      // was never written, perhaps
         }
+        widest = fmaxf(widest, fmaxf(step[j][0], step[j][1]));
+      }
+      bool raise = widest > cap;
 
       // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
       uint32_t seen = 0xffffffffu;                                          // bit 4 * nt + e
@@ -428,12 +445,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
             seen &= ~(1u << (4 * nt + e));
             sc[nt][e] = -INFINITY;
           }
-          raise |= sc[nt][e] > top[nt][e & 1] + 8.0f;
         }
-      if (__any_sync(0xffffffffu, raise)) {
-        float widest = 0.0f;
 #pragma unroll
-        for (int j = 0; j < J; ++j) widest = fmaxf(widest, fmaxf(step[j][0], step[j][1]));
+      for (int nt = 0; nt < NT; ++nt) {
+        raise |= fmaxf(sc[nt][0], sc[nt][2]) > top[nt][0] + 8.0f;
+        raise |= fmaxf(sc[nt][1], sc[nt][3]) > top[nt][1] + 8.0f;
+      }
+      if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int m = 4; m < 32; m <<= 1) widest = fmaxf(widest, __shfl_xor_sync(0xffffffffu, widest, m));
         // the next power of two (an infinite step stays above every cap: its products are no numbers anyway)
@@ -471,6 +489,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       // ---- output ---------------------------------------------------------------------------------------------------------
       const float times = __uint_as_float((260u << 23) - __float_as_uint(cap));           // 64 / cap, a power of two
       const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
+      const uint32_t eight_even[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};         // -8 * 2^-24
+      const uint32_t eight_odd[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};          // -8 * 2^-20
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const float step_a = step[j][0] * times, step_b = step[j][1] * times;
@@ -509,7 +529,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             mma16816(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
-            if (TYPE == QSGD_TYPE_F16) mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
+            mma16816(o[nt][j][r], r & 1 ? eight_odd : eight_even, bh[nt][0], bh[nt][1]);
+            if (TYPE == QSGD_TYPE_F16) {
+              mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
+              mma16816(o[nt][j][r], r & 1 ? eight_odd : eight_even, bl[nt][0], bl[nt][1]);
+            }
           }
         }
       }
@@ -518,15 +542,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
 #pragma unroll 1
     for (uint32_t i = 0; i < count; ++i) {
       {
-        const uint32_t parity = (phases >> stage) & 1u;
-        phases ^= 1u << stage;
         uint32_t polls = 0;
         while (!mbar_try(bar_u32 + 8 * stage, parity))
           if (++polls >= kPolls) { timed_out = true; break; }
       }
       const uint32_t first = (tile0 + i) * kCacheTile;
       const uint8_t* const tile = ring + stage * S::kTileBytes;
-      if ((int64_t)first + kCacheTile > see_all) take_tile(Constant<true>(), tile, first);     // some row does not see the whole tile
+      if (tile0 + i >= clear) take_tile(Constant<true>(), tile, first);     // some row does not see the whole tile
       else take_tile(Constant<false>(), tile, first);
       __syncwarp();                                         // the stage's readers are done
       const uint32_t next = i + S::kStages;
@@ -534,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         if ((next & 31u) == 0) source = next + lane < count ? look_up(next + lane) : nullptr;
         if (lane == (next & 31u)) copy_tile(ring_u32 + stage * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * stage);
       }
-      if (++stage == S::kStages) stage = 0;
+      if (++stage == S::kStages) { stage = 0; parity ^= 1u; }
     }
 
     // ---- the segment's rows, or a part of them -----------------------------------------------------------------------------
@@ -571,7 +593,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
           for (int m = 4; m < 32; m <<= 1) z += __shfl_xor_sync(0xffffffffu, z, m);
           float v[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { v[i] = fmaf(o[nt][j][i][e], held, z); v[i + 4] = fmaf(o[nt][j][i][e + 2], held, z); }
+          for (int i = 0; i < 4; ++i) {
+            v[i] = fmaf(o[nt][j][i][e] * (i & 1 ? 1048576.0f : 16777216.0f), held, z);
+            v[i + 4] = fmaf(o[nt][j][i][e + 2] * (i & 1 ? 1048576.0f : 16777216.0f), held, z);
+          }
           if (out) {
             *reinterpret_cast<uint4*>(out + 64 * j + 8 * g) =
                 make_uint4(pack16<TYPE>(v[0] * over, v[1] * over), pack16<TYPE>(v[2] * over, v[3] * over), pack16<TYPE>(v[4] * over, v[5] * over),
