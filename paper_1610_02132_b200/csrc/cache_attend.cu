@@ -114,6 +114,20 @@ __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
   c[3] = v & 0x00f000f0u;
 }
 
+// The same less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
+__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack_centred(uint32_t w, uint32_t (&c)[4]) {
+  unpack(w, c);
+  c[0] = add_f16x2(c[0], 0x80088008u);
+  c[1] = add_f16x2(c[1], 0x80808080u);
+  c[2] = add_f16x2(c[2], 0x80088008u);
+  c[3] = add_f16x2(c[3], 0x80808080u);
+}
+
 template <int J>
 __device__ __forceinline__ void load_pairs(const uint32_t* at, uint32_t (&v)[J]) {      // at: on a boundary of J words if that is a power of two
   if constexpr (J == 2) {
@@ -489,8 +503,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       // ---- output ---------------------------------------------------------------------------------------------------------
       const float times = __uint_as_float((260u << 23) - __float_as_uint(cap));           // 64 / cap, a power of two
       const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
-      const uint32_t eight_even[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};         // -8 * 2^-24
-      const uint32_t eight_odd[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};          // -8 * 2^-20
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const float step_a = step[j][0] * times, step_b = step[j][1] * times;
@@ -521,18 +533,16 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         const uint32_t c0 = *reinterpret_cast<const uint32_t*>(codes + va * 32), c1 = *reinterpret_cast<const uint32_t*>(codes + vb * 32);
         const uint32_t c2 = *reinterpret_cast<const uint32_t*>(codes + (va + 8) * 32), c3 = *reinterpret_cast<const uint32_t*>(codes + (vb + 8) * 32);
         uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
-        unpack(__byte_perm(c0, c1, 0x5410), lo01); unpack(__byte_perm(c0, c1, 0x7632), hi01);
-        unpack(__byte_perm(c2, c3, 0x5410), lo23); unpack(__byte_perm(c2, c3, 0x7632), hi23);
+        unpack_centred(__byte_perm(c0, c1, 0x5410), lo01); unpack_centred(__byte_perm(c0, c1, 0x7632), hi01);
+        unpack_centred(__byte_perm(c2, c3, 0x5410), lo23); unpack_centred(__byte_perm(c2, c3, 0x7632), hi23);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {                       // rows: coordinates 64 j + 8 g + r, and those + 4
           const uint32_t a[4] = {lo01[r], hi01[r], lo23[r], hi23[r]};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             mma16816(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
-            mma16816(o[nt][j][r], r & 1 ? eight_odd : eight_even, bh[nt][0], bh[nt][1]);
             if (TYPE == QSGD_TYPE_F16) {
               mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
-              mma16816(o[nt][j][r], r & 1 ? eight_odd : eight_even, bl[nt][0], bl[nt][1]);
             }
           }
         }
