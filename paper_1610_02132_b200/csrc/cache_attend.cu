@@ -75,17 +75,38 @@ __device__ __forceinline__ uint32_t token_of(uint32_t r) { return (0x57463120u >
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+// Waits for a phase, at most kPolls times as long as the hardware suspends a thread that tries; false if that was not enough.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
+      "mov.u32 n, 0;\n\t"
+      "again:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra done;\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.lt.u32 p, n, %3;\n\t"
+      "@p bra again;\n\t"
+      "setp.ne.u32 p, n, n;\n\t"
+      "done:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "n"(kPolls) : "memory");
   return ok != 0;
 }
 
-__device__ __forceinline__ void copy_tile(uint32_t dst, const uint8_t* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar) : "memory");
+// One lane's copies of one or two tiles into a stage, two places one behind the other.
+__device__ __forceinline__ void copy_tiles(bool mine, uint32_t dst, const uint8_t* src0, const uint8_t* src1, uint32_t tile_bytes, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 d, n;\n\t"
+      "setp.ne.u32 p, %0, 0;\n\t"
+      "setp.ne.and.u64 q, %3, 0, p;\n\t"
+      "add.u32 d, %1, %4;\n\t"
+      "selp.u32 n, %4, 0, q;\n\t"
+      "add.u32 n, n, %4;\n\t"
+      "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%5], n;\n\t"
+      "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%1], [%2], %4, [%5];\n\t"
+      "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [d], [%3], %4, [%5];\n\t}"
+      ::"r"((uint32_t)mine), "r"(dst), "l"(src0), "l"(src1), "r"(tile_bytes), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -113,6 +134,10 @@ __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
   c[2] = v & 0x000f000fu;
   c[3] = v & 0x00f000f0u;
 }
+
+// The largest pair (as a number) whose step is not above a power of two.
+template <int TYPE>
+__device__ __forceinline__ uint32_t cap_bits(float cap) { return to_bits16<TYPE>(cap) << 16 | 0xffffu; }
 
 // The same less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
 __device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
@@ -166,9 +191,9 @@ template <int TYPE, int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT, kGroups = D / 64;
   static constexpr uint32_t kTileBytes = 18 * D;
-  // Ring stages of a warp: about 9 KB of tiles in flight at NT = 1 (two CTAs an SM: 150 KB), and room for the warp's part of the join.
-  static constexpr uint32_t kStages = D == 64 ? 8 : D == 128 ? 4 : 3;
-  static constexpr uint32_t kRing = kStages * kTileBytes;
+  // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (two CTAs an SM: 150 KB), and room for the warp's part of the join.
+  static constexpr uint32_t kStages = D == 64 ? 4 : 2;
+  static constexpr uint32_t kRing = kStages * 2 * kTileBytes;
   static constexpr uint32_t kRowFloats = D + 8;                             // of a part: rows shifted by 8 banks
   static constexpr uint32_t kPart = kRows * kRowFloats * 4;
   static constexpr uint32_t kRingSpace = ((kRing > kPart ? kRing : kPart) + 127) / 128 * 128;
@@ -362,11 +387,21 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     }
     // Tokens that the first row sees (all rows see them) and that the last row sees.
     const int64_t all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group), any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
-    const uint32_t see_all = all > 0 ? (uint32_t)all : 0u, see_any = any > 0 ? (uint32_t)any : 0u;
+    const uint32_t see_all = all > 0 ? (uint32_t)all : 0u;
+    uint32_t see_any = any > 0 ? (uint32_t)any : 0u;
     uint32_t tile_end = (see_any + kCacheTile - 1) / kCacheTile;
     if (tile_end > tile1) tile_end = tile1;
-    const uint32_t clear = see_all / kCacheTile;            // tiles in front of this one are seen whole by every row
     const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
+    const uint32_t clear = see_all / kCacheTile > tile0 ? see_all / kCacheTile - tile0 : 0u;      // tiles that every row sees whole
+    const uint32_t plain = clear < count ? clear : count;
+    // What lies behind the warp's tiles is not there to see, whatever the rows' own bounds are.
+    const uint32_t bound = tile_end * kCacheTile;
+    if (see_any > bound) see_any = bound;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if ((uint32_t)see[nt][e] > bound) see[nt][e] = (int32_t)bound;
 
     float o[NT][J][4][4], lsum[NT][2], osum[NT][J][2], top[NT][2];
 #pragma unroll
@@ -381,102 +416,111 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       top[nt][0] = top[nt][1] = kNoMax;
     }
 
-    // ---- the warp's tiles ----------------------------------------------------------------------------------------------
-    // Lane l knows where tiles l, l + 32, ... of the warp lie, and starts their copies.
+    // ---- the warp's tiles, two at a time -------------------------------------------------------------------------------
+    // Lane l knows where pairs l, l + 32, ... of the warp's tiles lie, and starts their copies.
+    const uint32_t pairs = (count + 1) / 2;
     auto look_up = [&](uint32_t i) -> const uint8_t* {
+      if (i >= count) return nullptr;
       const uint32_t tile = tile0 + i, page = tile / p.c.page_tiles;
       int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
       if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
       return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
     };
-    const uint8_t* source = lane < count ? look_up(lane) : nullptr;
+    const uint8_t *source0 = look_up(2 * lane), *source1 = look_up(2 * lane + 1);
 #pragma unroll 1
-    for (uint32_t i = 0; i < S::kStages && i < count; ++i) {
+    for (uint32_t i = 0; i < S::kStages && i < pairs; ++i) {
       const uint32_t at = stage + i < S::kStages ? stage + i : stage + i - S::kStages;
-      if (lane == i) copy_tile(ring_u32 + at * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * at);
+      copy_tiles(lane == i, ring_u32 + at * 2 * S::kTileBytes, source0, source1, S::kTileBytes, bar_u32 + 8 * at);
     }
 
     float cap = kLeastCap;                                  // power of two that no step so far exceeds
-    auto take_tile = [&](auto masked_, const uint8_t* const tile, const uint32_t first) {
+    uint32_t cap_pair = cap_bits<TYPE>(kLeastCap);          // the largest pair whose step does not
+    auto take_tiles = [&](auto masked_, const uint8_t* const tiles, const uint32_t first) {
       constexpr bool kMasked = decltype(masked_)::value;
       const uint32_t ka = token_of(g), kb = ka + 8;
-      float sc[NT][4];                                      // scores: tokens ka, ka, kb, kb; rows 2t, 2t + 1, 2t, 2t + 1
+      float sc[2][NT][4];                                   // scores of each tile: tokens ka, ka, kb, kb; rows 2t, 2t + 1, 2t, 2t + 1
+      uint32_t pair[2][2][J];                               // of the values: tokens ka, kb
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
-      uint32_t pair_a[J], pair_b[J];
-      load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + ka * J, pair_a);
-      load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + kb * J, pair_b);
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* const tile = tiles + h * S::kTileBytes;
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const uint2 ca = *reinterpret_cast<const uint2*>(tile + (j * 16 + ka) * 32 + 8 * t);
-        const uint2 cb = *reinterpret_cast<const uint2*>(tile + (j * 16 + kb) * 32 + 8 * t);
-        float acc[NT][4];
+        for (int nt = 0; nt < NT; ++nt) sc[h][nt][0] = sc[h][nt][1] = sc[h][nt][2] = sc[h][nt][3] = 0.0f;
+        uint32_t pair_a[J], pair_b[J];
+        load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + ka * J, pair_a);
+        load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 8 * D) + kb * J, pair_b);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
-        uint32_t ax[4], ay[4], bx[4], by[4];
-        unpack(ca.x, ax); unpack(ca.y, ay); unpack(cb.x, bx); unpack(cb.y, by);
+        for (int j = 0; j < J; ++j) {
+          const uint2 ca = *reinterpret_cast<const uint2*>(tile + (j * 16 + ka) * 32 + 8 * t);
+          const uint2 cb = *reinterpret_cast<const uint2*>(tile + (j * 16 + kb) * 32 + 8 * t);
+          float acc[NT][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t a[4] = {ax[e], bx[e], ay[e], by[e]};
+          for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
+          uint32_t ax[4], ay[4], bx[4], by[4];
+          unpack(ca.x, ax); unpack(ca.y, ay); unpack(cb.x, bx); unpack(cb.y, by);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t a[4] = {ax[e], bx[e], ay[e], by[e]};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816(acc[nt], a, qf[nt][j][e][0], qf[nt][j][e][1]);
+          }
+          const float step_a = from_bits16<TYPE>(pair_a[j] >> 16), step_b = from_bits16<TYPE>(pair_b[j] >> 16);
+          const float lo_a = from_bits16<TYPE>(pair_a[j] & 0xffffu), lo_b = from_bits16<TYPE>(pair_b[j] & 0xffffu);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sc[h][nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? lo_a : lo_b, qsum[nt][j][e & 1], sc[h][nt][e]));
         }
-        const float step_a = from_bits16<TYPE>(pair_a[j] >> 16), step_b = from_bits16<TYPE>(pair_b[j] >> 16);
-        const float lo_a = from_bits16<TYPE>(pair_a[j] & 0xffffu), lo_b = from_bits16<TYPE>(pair_b[j] & 0xffffu);
+        load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 17 * D) + ka * J, pair[h][0]);
+        load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 17 * D) + kb * J, pair[h][1]);
+      }
+
+      // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
+      uint32_t seen = 0xffffffffu;                                          // bit 4 * (NT * h + nt) + e
+      uint32_t widest = 0;                                                  // steps are not negative: pairs order like their upper halves
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sc[nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? lo_a : lo_b, qsum[nt][j][e & 1], sc[nt][e]));
-      }
-
-      // ---- the pairs of the values ----------------------------------------------------------------------------------------
-      const uint8_t* const values = tile + 9 * D;
-      load_pairs<J>(reinterpret_cast<const uint32_t*>(values + 8 * D) + ka * J, pair_a);
-      load_pairs<J>(reinterpret_cast<const uint32_t*>(values + 8 * D) + kb * J, pair_b);
-      float step[J][2], mid[J][2], widest = 0.0f;
+          for (int e = 0; e < 4; ++e) {
+            sc[h][nt][e] *= factor[nt][e & 1];
+            if (kMasked && (int32_t)(16 * h + (e < 2 ? ka : kb)) >= see[nt][e & 1] - (int32_t)first) {
+              seen &= ~(1u << (4 * (NT * h + nt) + e));
+              sc[h][nt][e] = -INFINITY;
+            }
+          }
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
+        for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t pv = h ? pair_b[j] : pair_a[j];
-          step[j][h] = from_bits16<TYPE>(pv >> 16);
-          mid[j][h] = fmaf(8.0f, step[j][h], from_bits16<TYPE>(pv & 0xffffu));
-          if (kMasked && first + (h ? kb : ka) >= see_any) step[j][h] = mid[j][h] = 0.0f;      // was never written, perhaps
-        }
-        widest = fmaxf(widest, fmaxf(step[j][0], step[j][1]));
+          for (int x = 0; x < 2; ++x) {
+            if (kMasked && first + 16 * h + (x ? kb : ka) >= see_any) pair[h][x][j] = 0;      // was never written, perhaps
+            widest = pair[h][x][j] > widest ? pair[h][x][j] : widest;
+          }
       }
-      bool raise = widest > cap;
-
-      // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
-      uint32_t seen = 0xffffffffu;                                          // bit 4 * nt + e
+      bool raise = widest > cap_pair;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[nt][e] *= factor[nt][e & 1];
-          if (kMasked && (int32_t)(e < 2 ? ka : kb) >= see[nt][e & 1] - (int32_t)first) {
-            seen &= ~(1u << (4 * nt + e));
-            sc[nt][e] = -INFINITY;
-          }
-        }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        raise |= fmaxf(sc[nt][0], sc[nt][2]) > top[nt][0] + 8.0f;
-        raise |= fmaxf(sc[nt][1], sc[nt][3]) > top[nt][1] + 8.0f;
-      }
+        for (int e = 0; e < 2; ++e)
+          raise |= fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2])) > top[nt][e] + 8.0f;
       if (__any_sync(0xffffffffu, raise)) {
+        float step = 0.0f;                                  // (a step that is no number is passed over: its products are none anyway)
 #pragma unroll
-        for (int m = 4; m < 32; m <<= 1) widest = fmaxf(widest, __shfl_xor_sync(0xffffffffu, widest, m));
-        // the next power of two (an infinite step stays above every cap: its products are no numbers anyway)
-        const uint32_t bits = (__float_as_uint(fminf(widest, kMostCap)) + 0x007fffffu) & 0xff800000u;
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) step = fmaxf(step, from_bits16<TYPE>(pair[x >> 1][x & 1][j] >> 16));
+#pragma unroll
+        for (int m = 4; m < 32; m <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, m));
+        const uint32_t bits = (__float_as_uint(fminf(step, kMostCap)) + 0x007fffffu) & 0xff800000u;      // the next power of two
         const float cap_new = fmaxf(cap, __uint_as_float(bits)), shrink = cap / cap_new;
         cap = cap_new;
+        cap_pair = cap_bits<TYPE>(cap);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float m = fmaxf(sc[nt][e], sc[nt][e + 2]);
+            float m = fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2]));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -493,56 +537,64 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
           }
       }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[nt][e] = exp2_approx(sc[nt][e] - top[nt][e & 1]);
-        lsum[nt][0] += sc[nt][0] + sc[nt][2];
-        lsum[nt][1] += sc[nt][1] + sc[nt][3];
-      }
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[h][nt][e] = exp2_approx(sc[h][nt][e] - top[nt][e & 1]);
+          lsum[nt][0] += sc[h][nt][0] + sc[h][nt][2];
+          lsum[nt][1] += sc[h][nt][1] + sc[h][nt][3];
+        }
 
       // ---- output ---------------------------------------------------------------------------------------------------------
       const float times = __uint_as_float((260u << 23) - __float_as_uint(cap));           // 64 / cap, a power of two
       const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const float step_a = step[j][0] * times, step_b = step[j][1] * times;
-        uint32_t bh[NT][2], bl[NT][2];
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* const values = tiles + h * S::kTileBytes + 9 * D;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float w[4] = {sc[nt][0] * step_a, sc[nt][1] * step_a, sc[nt][2] * step_b, sc[nt][3] * step_b};
-          if (kMasked) {                                    // what a row does not see may hold anything: no product with it
-            float z[4] = {sc[nt][0] * mid[j][0], sc[nt][1] * mid[j][0], sc[nt][2] * mid[j][1], sc[nt][3] * mid[j][1]};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!(seen >> (4 * nt + e) & 1u)) w[e] = z[e] = 0.0f;
-            osum[nt][j][0] += z[0] + z[2];
-            osum[nt][j][1] += z[1] + z[3];
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) osum[nt][j][e & 1] = fmaf(sc[nt][e], mid[j][e >> 1], osum[nt][j][e & 1]);
-          }
-          const uint32_t h0 = pack16<QSGD_TYPE_F16>(w[0], w[1]), h1 = pack16<QSGD_TYPE_F16>(w[2], w[3]);
-          bh[nt][0] = transpose8x8(h0);
-          bh[nt][1] = transpose8x8(h1);
-          if (TYPE == QSGD_TYPE_F16) {
-            bl[nt][0] = transpose8x8(pack16<QSGD_TYPE_F16>(w[0] - from_bits16<QSGD_TYPE_F16>(h0 & 0xffffu), w[1] - from_bits16<QSGD_TYPE_F16>(h0 >> 16)));
-            bl[nt][1] = transpose8x8(pack16<QSGD_TYPE_F16>(w[2] - from_bits16<QSGD_TYPE_F16>(h1 & 0xffffu), w[3] - from_bits16<QSGD_TYPE_F16>(h1 >> 16)));
-          }
-        }
-        const uint8_t* const codes = values + j * 512 + 4 * g;
-        const uint32_t c0 = *reinterpret_cast<const uint32_t*>(codes + va * 32), c1 = *reinterpret_cast<const uint32_t*>(codes + vb * 32);
-        const uint32_t c2 = *reinterpret_cast<const uint32_t*>(codes + (va + 8) * 32), c3 = *reinterpret_cast<const uint32_t*>(codes + (vb + 8) * 32);
-        uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
-        unpack_centred(__byte_perm(c0, c1, 0x5410), lo01); unpack_centred(__byte_perm(c0, c1, 0x7632), hi01);
-        unpack_centred(__byte_perm(c2, c3, 0x5410), lo23); unpack_centred(__byte_perm(c2, c3, 0x7632), hi23);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {                       // rows: coordinates 64 j + 8 g + r, and those + 4
-          const uint32_t a[4] = {lo01[r], hi01[r], lo23[r], hi23[r]};
+        for (int j = 0; j < J; ++j) {
+          const float step_a = from_bits16<TYPE>(pair[h][0][j] >> 16), step_b = from_bits16<TYPE>(pair[h][1][j] >> 16);
+          const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pair[h][0][j] & 0xffffu));
+          const float mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pair[h][1][j] & 0xffffu));
+          const float times_a = step_a * times, times_b = step_b * times;
+          uint32_t bh[NT][2], bl[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            mma16816(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
+            const float* const pr = sc[h][nt];
+            float w[4] = {pr[0] * times_a, pr[1] * times_a, pr[2] * times_b, pr[3] * times_b};
+            if (kMasked) {                                  // what a row does not see may hold anything: no product with it
+              float z[4] = {pr[0] * mid_a, pr[1] * mid_a, pr[2] * mid_b, pr[3] * mid_b};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (!(seen >> (4 * (NT * h + nt) + e) & 1u)) w[e] = z[e] = 0.0f;
+              osum[nt][j][0] += z[0] + z[2];
+              osum[nt][j][1] += z[1] + z[3];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) osum[nt][j][e & 1] = fmaf(pr[e], e < 2 ? mid_a : mid_b, osum[nt][j][e & 1]);
+            }
+            const uint32_t h0 = pack16<QSGD_TYPE_F16>(w[0], w[1]), h1 = pack16<QSGD_TYPE_F16>(w[2], w[3]);
+            bh[nt][0] = transpose8x8(h0);
+            bh[nt][1] = transpose8x8(h1);
             if (TYPE == QSGD_TYPE_F16) {
-              mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
+              bl[nt][0] = transpose8x8(pack16<QSGD_TYPE_F16>(w[0] - from_bits16<QSGD_TYPE_F16>(h0 & 0xffffu), w[1] - from_bits16<QSGD_TYPE_F16>(h0 >> 16)));
+              bl[nt][1] = transpose8x8(pack16<QSGD_TYPE_F16>(w[2] - from_bits16<QSGD_TYPE_F16>(h1 & 0xffffu), w[3] - from_bits16<QSGD_TYPE_F16>(h1 >> 16)));
+            }
+          }
+          const uint8_t* const codes = values + j * 512 + 4 * g;
+          const uint32_t c0 = *reinterpret_cast<const uint32_t*>(codes + va * 32), c1 = *reinterpret_cast<const uint32_t*>(codes + vb * 32);
+          const uint32_t c2 = *reinterpret_cast<const uint32_t*>(codes + (va + 8) * 32), c3 = *reinterpret_cast<const uint32_t*>(codes + (vb + 8) * 32);
+          uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
+          unpack_centred(__byte_perm(c0, c1, 0x5410), lo01); unpack_centred(__byte_perm(c0, c1, 0x7632), hi01);
+          unpack_centred(__byte_perm(c2, c3, 0x5410), lo23); unpack_centred(__byte_perm(c2, c3, 0x7632), hi23);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {                     // rows: coordinates 64 j + 8 g + r, and those + 4
+            const uint32_t a[4] = {lo01[r], hi01[r], lo23[r], hi23[r]};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma16816(o[nt][j][r], a, bh[nt][0], bh[nt][1]);
+              if (TYPE == QSGD_TYPE_F16) mma16816(o[nt][j][r], a, bl[nt][0], bl[nt][1]);
             }
           }
         }
@@ -550,21 +602,18 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     };
 
 #pragma unroll 1
-    for (uint32_t i = 0; i < count; ++i) {
-      {
-        uint32_t polls = 0;
-        while (!mbar_try(bar_u32 + 8 * stage, parity))
-          if (++polls >= kPolls) { timed_out = true; break; }
-      }
-      const uint32_t first = (tile0 + i) * kCacheTile;
-      const uint8_t* const tile = ring + stage * S::kTileBytes;
-      if (tile0 + i >= clear) take_tile(Constant<true>(), tile, first);     // some row does not see the whole tile
-      else take_tile(Constant<false>(), tile, first);
+    for (uint32_t i = 0; i < pairs; ++i) {
+      if (!mbar_wait(bar_u32 + 8 * stage, parity)) timed_out = true;
+      const uint32_t first = (tile0 + 2 * i) * kCacheTile;
+      const uint8_t* const tiles = ring + stage * 2 * S::kTileBytes;
+      // Some row does not see both tiles whole, or the second one lies behind the warp's stretch (and holds what was there before).
+      if (2 * i + 2 > plain) take_tiles(Constant<true>(), tiles, first);
+      else take_tiles(Constant<false>(), tiles, first);
       __syncwarp();                                         // the stage's readers are done
       const uint32_t next = i + S::kStages;
-      if (next < count) {
-        if ((next & 31u) == 0) source = next + lane < count ? look_up(next + lane) : nullptr;
-        if (lane == (next & 31u)) copy_tile(ring_u32 + stage * S::kTileBytes, source, S::kTileBytes, bar_u32 + 8 * stage);
+      if (next < pairs) {
+        if ((next & 31u) == 0) { source0 = look_up(2 * (next + lane)); source1 = look_up(2 * (next + lane) + 1); }
+        copy_tiles(lane == (next & 31u), ring_u32 + stage * 2 * S::kTileBytes, source0, source1, S::kTileBytes, bar_u32 + 8 * stage);
       }
       if (++stage == S::kStages) { stage = 0; parity ^= 1u; }
     }
