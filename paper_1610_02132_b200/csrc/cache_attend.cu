@@ -203,6 +203,10 @@ struct Shape {
   static constexpr int kCtas = D <= 128 && NT == 1 ? 2 : 1;
 };
 
+__device__ __forceinline__ uint64_t divide(uint64_t a, uint32_t b) {      // nearly always in 32 bits, a fraction of the latency
+  return a >> 32 ? a / b : (uint64_t)((uint32_t)a / b);
+}
+
 // Where a row of a segment goes, and its logarithm of the sum.
 __device__ __forceinline__ uint16_t* out_row(const AttendParams& p, const Rows& s, uint32_t r, uint64_t* lse_at) {
   const uint32_t query = (s.row0 + r) / p.group, hh = s.head * p.group + (s.row0 + r) - query * p.group;
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
   total = 0;
 #pragma unroll
   for (uint32_t w = 0; w < kWarps; ++w) total += scan[w];
-  uint64_t stretch = (total + (uint64_t)gridDim.x * kWarps - 1) / ((uint64_t)gridDim.x * kWarps);
+  uint64_t stretch = divide(total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
   if (stretch < kLeastStretch) stretch = kLeastStretch;
   const uint64_t cta0 = (uint64_t)blockIdx.x * kWarps * stretch;
   if (cta0 >= total) {
@@ -307,15 +311,42 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     }
     const uint64_t off = u - seq_base;
     const uint32_t span = seq.tiles + kSegmentCost;         // units of a segment: its cost, then its tiles
-    const uint64_t segment = off / span;
+    const uint64_t segment = divide(off, span);
     const uint32_t x0 = (uint32_t)(off - segment * span), x1 = u1 - u < span - x0 ? x0 + (uint32_t)(u1 - u) : span;
     const uint32_t tile0 = x0 > kSegmentCost ? x0 - kSegmentCost : 0u, tile1 = x1 > kSegmentCost ? x1 - kSegmentCost : 0u;
     const uint64_t begin = u - x0 + kSegmentCost;           // its first tile on the line
     u += x1 - x0;
     if (tile0 == tile1) continue;                           // the stretch ends in front of its tiles
-    const uint32_t head = (uint32_t)(segment / seq.row_tiles), row_tile = (uint32_t)(segment - (uint64_t)head * seq.row_tiles);
+    const uint32_t head = (uint32_t)divide(segment, seq.row_tiles), row_tile = (uint32_t)(segment - (uint64_t)head * seq.row_tiles);
     const uint32_t row0 = row_tile * R, rows_all = seq.n * p.group;
     const uint32_t rows = rows_all - row0 < (uint32_t)R ? rows_all - row0 : (uint32_t)R;
+
+    // Tokens that the first row sees (all rows see them) and that the last row sees.
+    const int64_t all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group), any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
+    const uint32_t see_all = all > 0 ? (uint32_t)all : 0u;
+    uint32_t see_any = any > 0 ? (uint32_t)any : 0u;
+    uint32_t tile_end = (see_any + kCacheTile - 1) / kCacheTile;
+    if (tile_end > tile1) tile_end = tile1;
+    const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
+    const uint32_t clear = see_all / kCacheTile > tile0 ? see_all / kCacheTile - tile0 : 0u;      // tiles that every row sees whole
+    const uint32_t plain = clear < count ? clear : count;
+    // ---- the warp's first copies: everything else of a segment's beginning goes on while they fly ---------------------------
+    // Lane l knows where pairs l, l + 32, ... of the warp's tiles lie, and starts their copies.
+    const uint32_t pairs = (count + 1) / 2;
+    auto look_up = [&](uint32_t i) -> const uint8_t* {
+      if (i >= count) return nullptr;
+      const uint32_t tile = tile0 + i, page = tile / p.c.page_tiles;
+      int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
+      if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
+      return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
+    };
+    const uint8_t *source0 = look_up(2 * lane), *source1 = look_up(2 * lane + 1);
+#pragma unroll 1
+    for (uint32_t i = 0; i < S::kStages && i < pairs; ++i) {
+      const uint32_t at = stage + i < S::kStages ? stage + i : stage + i - S::kStages;
+      copy_tiles(lane == i, ring_u32 + at * 2 * S::kTileBytes, source0, source1, S::kTileBytes, bar_u32 + 8 * at);
+    }
+
 
     // ---- queries: operands, sums of each group, and how far each row sees ------------------------------------------------
     uint32_t qf[NT][J][4][2];
@@ -385,15 +416,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
         see[nt][e2] = far > 0 ? (int32_t)far : 0;
       }
     }
-    // Tokens that the first row sees (all rows see them) and that the last row sees.
-    const int64_t all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group), any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
-    const uint32_t see_all = all > 0 ? (uint32_t)all : 0u;
-    uint32_t see_any = any > 0 ? (uint32_t)any : 0u;
-    uint32_t tile_end = (see_any + kCacheTile - 1) / kCacheTile;
-    if (tile_end > tile1) tile_end = tile1;
-    const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
-    const uint32_t clear = see_all / kCacheTile > tile0 ? see_all / kCacheTile - tile0 : 0u;      // tiles that every row sees whole
-    const uint32_t plain = clear < count ? clear : count;
     // What lies behind the warp's tiles is not there to see, whatever the rows' own bounds are.
     const uint32_t bound = tile_end * kCacheTile;
     if (see_any > bound) see_any = bound;
@@ -417,22 +439,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     }
 
     // ---- the warp's tiles, two at a time -------------------------------------------------------------------------------
-    // Lane l knows where pairs l, l + 32, ... of the warp's tiles lie, and starts their copies.
-    const uint32_t pairs = (count + 1) / 2;
-    auto look_up = [&](uint32_t i) -> const uint8_t* {
-      if (i >= count) return nullptr;
-      const uint32_t tile = tile0 + i, page = tile / p.c.page_tiles;
-      int32_t at = __ldg(p.c.table + (uint64_t)seq.b * p.c.table_stride + page);
-      if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
-      return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTileBytes;
-    };
-    const uint8_t *source0 = look_up(2 * lane), *source1 = look_up(2 * lane + 1);
-#pragma unroll 1
-    for (uint32_t i = 0; i < S::kStages && i < pairs; ++i) {
-      const uint32_t at = stage + i < S::kStages ? stage + i : stage + i - S::kStages;
-      copy_tiles(lane == i, ring_u32 + at * 2 * S::kTileBytes, source0, source1, S::kTileBytes, bar_u32 + 8 * at);
-    }
-
     float cap = kLeastCap;                                  // power of two that no step so far exceeds
     uint32_t cap_pair = cap_bits<TYPE>(kLeastCap);          // the largest pair whose step does not
     auto take_tiles = [&](auto masked_, const uint8_t* const tiles, const uint32_t first) {
