@@ -434,6 +434,7 @@ int qsgd_cache_attend(const qsgd_cache* cache, const qsgd_cache_rows* rows, cons
  *   strides      in elements. Rows that begin on 16-byte boundaries (base and stride multiples of 16 bytes) are read by bulk
  *                copies; others are taken too, more slowly
  *   bias         [n] fp32 or NULL
+ *   status_dev   one u32, OR-ed with QSGD_DEV_TIMEOUT if a bounded wait inside a kernel gave up (out is unspecified then); or NULL
  *
  * qsgd_linear_i8: the two in one call, for activations that are quantised on the way (x W^T). workspace:
  * qsgd_linear_i8_workspace_bytes() of scratch, 16-byte aligned, nothing to clear; calls that overlap on the GPU need one each.
@@ -442,11 +443,11 @@ int qsgd_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row
                        uint64_t codes_stride, float* scale, qsgd_stream_t stream);
 int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, const int8_t* b, uint64_t b_stride,
                    const float* b_scale, const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out,
-                   uint64_t out_stride, int type, qsgd_stream_t stream);
+                   uint64_t out_stride, int type, uint32_t* status_dev, qsgd_stream_t stream);
 size_t qsgd_linear_i8_workspace_bytes(uint64_t m, uint32_t cols);
 int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w, uint64_t w_stride, const float* w_scale,
                    const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int out_type,
-                   void* workspace, qsgd_stream_t stream);
+                   void* workspace, uint32_t* status_dev, qsgd_stream_t stream);
 
 /*
  * Per-kernel timing (measurement aid; the paper has no counterpart). While enabled, every

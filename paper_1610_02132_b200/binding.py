@@ -130,11 +130,11 @@ def lib():
         L.qsgd_cache_attend.restype = C.c_int
         L.qsgd_quantize_rows.argtypes = [vp, u64, u32, u64, C.c_int, vp, u64, vp, vp]
         L.qsgd_quantize_rows.restype = C.c_int
-        L.qsgd_matmul_i8.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp]
+        L.qsgd_matmul_i8.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp, vp]
         L.qsgd_matmul_i8.restype = C.c_int
         L.qsgd_linear_i8_workspace_bytes.argtypes = [u64, u32]
         L.qsgd_linear_i8_workspace_bytes.restype = sz
-        L.qsgd_linear_i8.argtypes = [vp, u64, C.c_int, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp, vp]
+        L.qsgd_linear_i8.argtypes = [vp, u64, C.c_int, vp, u64, vp, vp, u64, u64, u32, vp, u64, C.c_int, vp, vp, vp]
         L.qsgd_linear_i8.restype = C.c_int
         L.qsgd_set_launch_chaining.argtypes = [C.c_int]
         L.qsgd_set_launch_chaining.restype = C.c_int
@@ -396,18 +396,18 @@ def qsgd_quantize_rows(x, codes, scale, stream=None):
     _check(_native.quantize_rows(x, codes, scale, stream))
 
 
-def qsgd_matmul_i8(a, a_scale, b, b_scale, out, bias=None, stream=None):
+def qsgd_matmul_i8(a, a_scale, b, b_scale, out, bias=None, stream=None, status_dev=None):
     """out <- (a b^T) * a_scale[:, None] * b_scale + bias, for int8 a and b; the sum is exact."""
-    _check(_native.matmul_i8(a, a_scale, b, b_scale, out, bias, stream))
+    _check(_native.matmul_i8(a, a_scale, b, b_scale, out, bias, status_dev, stream))
 
 
 def qsgd_linear_i8_workspace_bytes(rows, cols):
     return int(lib().qsgd_linear_i8_workspace_bytes(rows, cols))
 
 
-def qsgd_linear_i8(x, w, w_scale, out, workspace, bias=None, stream=None):
+def qsgd_linear_i8(x, w, w_scale, out, workspace, bias=None, stream=None, status_dev=None):
     """out <- x w^T + bias with the rows of x quantised on the way; w and w_scale as qsgd_quantize_rows leaves them."""
-    _check(_native.linear_i8(x, w, w_scale, out, workspace, bias, stream))
+    _check(_native.linear_i8(x, w, w_scale, out, workspace, bias, status_dev, stream))
 
 
 def quantize_rows_alloc(x, stream=None):

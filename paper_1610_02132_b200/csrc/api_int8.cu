@@ -31,7 +31,8 @@ int qsgd_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row
 }
 
 int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, const int8_t* b, uint64_t b_stride, const float* b_scale,
-                   const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int type, qsgd_stream_t stream) {
+                   const float* bias, uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int type, uint32_t* status_dev,
+                   qsgd_stream_t stream) {
   if (!type_taken(type)) return QSGD_ERR_TYPE;
   if (cols < 1 || cols > kMostCols || m > 0x7fffffffull || n > 0x7fffffffull || a_stride >> 40 || b_stride >> 40 || out_stride >> 40)
     return QSGD_ERR_SHAPE;
@@ -40,7 +41,7 @@ int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, con
   if (!a || !b || !a_scale || !b_scale || !out) return QSGD_ERR_NULL;
   if (!on(a_scale, 4) || !on(b_scale, 4) || !on(bias, 4) || !on(out, size_of(type))) return QSGD_ERR_ALIGN;
   const MatmulArgs args{a, b, a_scale, b_scale, bias, out, m > 1 ? a_stride : padded_cols(cols), n > 1 ? b_stride : padded_cols(cols),
-                        out_stride, (uint32_t)m, (uint32_t)n, cols, type};
+                        out_stride, (uint32_t)m, (uint32_t)n, cols, type, status_dev};
   return launch_matmul_i8(args, static_cast<cudaStream_t>(stream));
 }
 
@@ -50,7 +51,8 @@ size_t qsgd_linear_i8_workspace_bytes(uint64_t m, uint32_t cols) {
 }
 
 int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w, uint64_t w_stride, const float* w_scale, const float* bias,
-                   uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int out_type, void* workspace, qsgd_stream_t stream) {
+                   uint64_t m, uint64_t n, uint32_t cols, void* out, uint64_t out_stride, int out_type, void* workspace,
+                   uint32_t* status_dev, qsgd_stream_t stream) {
   if (!type_taken(x_type) || !type_taken(out_type)) return QSGD_ERR_TYPE;
   if (cols < 1 || cols > kMostCols || m > 0x7fffffffull || n > 0x7fffffffull || x_stride >> 40 || w_stride >> 40 || out_stride >> 40)
     return QSGD_ERR_SHAPE;
@@ -62,7 +64,7 @@ int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w
   float* scale = reinterpret_cast<float*>(codes + m * padded_cols(cols));
   const int st = qsgd_quantize_rows(x, m, cols, x_stride, x_type, codes, padded_cols(cols), scale, stream);
   if (st) return st;
-  return qsgd_matmul_i8(codes, padded_cols(cols), scale, w, w_stride, w_scale, bias, m, n, cols, out, out_stride, out_type, stream);
+  return qsgd_matmul_i8(codes, padded_cols(cols), scale, w, w_stride, w_scale, bias, m, n, cols, out, out_stride, out_type, status_dev, stream);
 }
 
 }  // extern "C"

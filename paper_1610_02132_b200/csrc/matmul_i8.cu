@@ -1,0 +1,334 @@
+// Product in 8-bit integers for many rows: out[m][n] = (a_m . b_n) a_scale b_scale + bias on the fifth-generation tensor cores.
+//
+// Tiles of 128 x BN of the output, each summed over K by tcgen05.mma (kind::i8, exact 32-bit sums in tensor memory). A persistent CTA per SM:
+// one thread keeps a ring of stages (128 columns of 128 rows of a and BN rows of b, 128-byte swizzle) filled by TMA, which puts zeros where a or b
+// end; one thread issues the products; four warps take finished sums out of tensor memory, scale them and store them, while the next tile's
+// products run into the other half of tensor memory.
+//
+// All waits are bounded. One that runs out raises a flag in shared memory, at which every role leaves its loop; the CTA then waits for the
+// copies and products in flight (bounded again), frees its tensor memory and returns with QSGD_DEV_TIMEOUT in the status word, if there is one.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "int8.cuh"
+
+namespace qsgd {
+
+namespace {
+
+constexpr uint32_t kBM = 128, kBK = 128, kStages = 4, kThreads = 192, kEpilogueWarps = 4;
+constexpr uint32_t kPolls = 1u << 22;
+
+struct GemmParams {
+  MatmulArgs p;
+  uint32_t m_tiles, n_tiles, k_steps;
+  bool vector_out;             // rows of out begin on 16-byte boundaries
+};
+
+template <uint32_t BN>
+struct Shape {
+  static constexpr uint32_t kA = kBM * kBK, kB = BN * kBK, kStage = kA + kB;
+  static constexpr uint32_t kSmem = kStages * kStage + 1024;               // stages on 1024-byte boundaries
+  static constexpr uint32_t kColumns = 2 * BN;                              // of tensor memory: two tiles of sums
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// False when the wait ran out or another role's has.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+  for (uint32_t i = 0; i < kPolls; ++i) {
+    if (mbar_try(bar, parity)) return true;
+    if ((i & 63u) == 63u && *given_up) return false;
+  }
+  *given_up = 1;
+  return false;
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t x, uint32_t y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Shared-memory descriptor of a tile whose rows are 128 bytes, 128-byte swizzle: 8 rows are 1024 bytes apart.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
+  return ((uint64_t)0x40004040u << 32) | (1u << 16) | ((addr >> 4) & 0x3fffu);
+}
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+               "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t at, int32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+      "%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+        "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+        "=r"(v[31])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// Tiles in an order that keeps those at work together close: columns of up to 16 row tiles.
+__device__ __forceinline__ void tile_at(const GemmParams& g, uint32_t i, uint32_t* m, uint32_t* n) {
+  constexpr uint32_t kBand = 16;
+  const uint32_t per_band = kBand * g.n_tiles, band = i / per_band, rest = i - band * per_band;
+  const uint32_t first = band * kBand, rows = g.m_tiles - first < kBand ? g.m_tiles - first : kBand;
+  *n = rest / rows;
+  *m = first + (rest - *n * rows);
+}
+
+template <int TYPE>
+struct Out;
+template <>
+struct Out<QSGD_TYPE_F32> {
+  typedef float T;
+  static __device__ __forceinline__ T one(float v) { return v; }
+};
+template <>
+struct Out<QSGD_TYPE_F16> {
+  typedef __half T;
+  static __device__ __forceinline__ T one(float v) { return __float2half_rn(v); }
+};
+template <>
+struct Out<QSGD_TYPE_BF16> {
+  typedef __nv_bfloat16 T;
+  static __device__ __forceinline__ T one(float v) { return __float2bfloat16_rn(v); }
+};
+
+// 16 bytes of output from the values at v.
+template <int TYPE>
+__device__ __forceinline__ uint4 pack_out(const float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TYPE == QSGD_TYPE_F32) w[i] = __float_as_uint(v[i]);
+    else if constexpr (TYPE == QSGD_TYPE_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <uint32_t BN, int TYPE>
+__global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                               const __grid_constant__ GemmParams g) {
+  using S = Shape<BN>;
+  typedef typename Out<TYPE>::T T;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
+  __shared__ uint32_t tmem_base, given_up;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), sums_full0 = smem_u32(sums_full), sums_empty0 = smem_u32(sums_empty);
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (uint32_t s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+#pragma unroll
+    for (uint32_t s = 0; s < 2; ++s) { mbar_init(sums_full0 + 8 * s, 1); mbar_init(sums_empty0 + 8 * s, kEpilogueWarps); }
+    given_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0)
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(S::kColumns) : "memory");
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_base;
+  chain_wait();
+
+  const uint32_t tiles = g.m_tiles * g.n_tiles;
+  if (warp == 0) {                                          // ---- fills the ring ------------------------------------------------
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool fine = true;
+      for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x) {
+        uint32_t m, n;
+        tile_at(g, i, &m, &n);
+        for (uint32_t k = 0; k < g.k_steps; ++k, ++it) {
+          const uint32_t s = it % kStages, round = it / kStages;
+          if (round && !mbar_wait(empty0 + 8 * s, (round - 1) & 1u, &given_up)) { fine = false; break; }
+          const uint32_t at = stages + s * S::kStage;
+          mbar_expect(full0 + 8 * s, S::kStage);
+          tma_load(at, &map_a, k * kBK, m * kBM, full0 + 8 * s);
+          tma_load(at + S::kA, &map_b, k * kBK, n * BN, full0 + 8 * s);
+        }
+      }
+      // What is in flight lands before the CTA's shared memory goes away.
+      for (uint32_t s = 0; s < kStages && s < it && !fine; ++s) {
+        const uint32_t last = (it - 1 - s) / kStages;       // the round of stage s' = (it - 1 - s) % kStages that was filled last
+        for (uint32_t t = 0; t < kPolls && !mbar_try(full0 + 8 * ((it - 1 - s) % kStages), last & 1u); ++t) {}
+      }
+    }
+  } else if (warp == 1) {                                   // ---- issues the products -------------------------------------------
+    if (lane == 0) {
+      constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((BN >> 3) << 17) | ((kBM >> 4) << 24);     // s32 += s8 * s8
+      uint32_t it = 0, done = 0;
+      bool fine = true;
+      for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x, ++done) {
+        const uint32_t half = done & 1u, use = done >> 1;
+        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, &given_up)) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (uint32_t k = 0; k < g.k_steps; ++k, ++it) {
+          const uint32_t s = it % kStages;
+          if (!mbar_wait(full0 + 8 * s, (it / kStages) & 1u, &given_up)) { fine = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t a = tile_desc(stages + s * S::kStage), b = tile_desc(stages + s * S::kStage + S::kA);
+#pragma unroll
+          for (uint32_t x = 0; x < kBK / 32; ++x) mma_i8(tmem + half * BN, a + 2 * x, b + 2 * x, idesc, k != 0 || x != 0);
+          tc_commit(empty0 + 8 * s);
+        }
+        if (fine) tc_commit(sums_full0 + 8 * half);
+      }
+      // Products in flight are done before tensor memory is freed: after a wait that ran out, the last commit is waited for here.
+      if (!fine && it) {
+        const uint32_t last = it - 1;
+        for (uint32_t t = 0; t < kPolls && !mbar_try(empty0 + 8 * (last % kStages), (last / kStages) & 1u); ++t) {}
+      }
+    }
+  } else {                                                  // ---- takes the sums out --------------------------------------------
+    const uint32_t quarter = warp & 3u;                     // of tensor memory's lanes: a warp reaches those of its number modulo 4
+    uint32_t done = 0;
+    for (uint32_t i = blockIdx.x; i < tiles; i += gridDim.x, ++done) {
+      uint32_t m, n;
+      tile_at(g, i, &m, &n);
+      const uint32_t half = done & 1u;
+      const bool fine = __all_sync(0xffffffffu, mbar_wait(sums_full0 + 8 * half, (done >> 1) & 1u, &given_up));
+      if (!fine) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t row = m * kBM + 32 * quarter + lane;
+      const bool live = row < g.p.m;
+      const float a_scale = live ? __ldg(g.p.a_scale + row) : 0.0f;
+      T* const out = static_cast<T*>(g.p.out) + (uint64_t)row * g.p.out_stride;
+#pragma unroll 1
+      for (uint32_t c = 0; c < BN; c += 32) {
+        int32_t v[32];
+        tmem_load32(tmem + half * BN + c + ((32 * quarter) << 16), v);
+        const uint32_t col = n * BN + c;
+        if (live && col < g.p.n) {
+          float y[32];
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            const uint32_t at = col + x < g.p.n ? col + x : g.p.n - 1;
+            y[x] = scaled_sum(v[x], a_scale, __ldg(g.p.b_scale + at), g.p.bias ? __ldg(g.p.bias + at) : 0.0f);
+          }
+          if (g.vector_out && col + 32 <= g.p.n) {
+            constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+            for (int x = 0; x < 32; x += kPer) *reinterpret_cast<uint4*>(out + col + x) = pack_out<TYPE>(y + x);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (col + x < g.p.n) out[col + x] = Out<TYPE>::one(y[x]);
+          }
+        }
+        __syncwarp();                                       // the next read of tensor memory is of the whole warp
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sums_empty0 + 8 * half);
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 0) {
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns));
+  }
+  if (threadIdx.x == 0 && given_up && g.p.status) atomicOr(g.p.status, QSGD_DEV_TIMEOUT);
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode_tiled(EncodeTiled* out) {
+  static std::atomic<void*> known{nullptr};
+  void* fn = known.load(std::memory_order_acquire);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return (int)e;
+    if (found != cudaDriverEntryPointSuccess || !fn) return (int)cudaErrorNotSupported;
+    known.store(fn, std::memory_order_release);
+  }
+  *out = reinterpret_cast<EncodeTiled>(fn);
+  return 0;
+}
+
+// Rows of int8 in boxes of 128 columns x `box` rows.
+int make_map(CUtensorMap* map, const int8_t* base, uint32_t cols, uint32_t rows, uint64_t stride, uint32_t box) {
+  EncodeTiled encode;
+  const int st = encode_tiled(&encode);
+  if (st) return st;
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
+  const cuuint32_t boxes[2] = {kBK, box}, ones[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? 0 : (int)cudaErrorInvalidValue;
+}
+
+template <uint32_t BN, int TYPE>
+int launch(const MatmulArgs& p, cudaStream_t stream) {
+  using S = Shape<BN>;
+  static KernelSite site;
+  int sms = 0, occ = 0;
+  int st = site.lookup(matmul_i8_kernel<BN, TYPE>, kThreads, S::kSmem, &sms, &occ);
+  if (st) return st;
+  CUtensorMap a, b;
+  st = make_map(&a, p.a, p.k, p.m, p.a_stride, kBM);
+  if (!st) st = make_map(&b, p.b, p.k, p.n, p.b_stride, BN);
+  if (st) return st;
+  GemmParams g;
+  g.p = p;
+  g.m_tiles = (p.m + kBM - 1) / kBM;
+  g.n_tiles = (p.n + BN - 1) / BN;
+  g.k_steps = (p.k + kBK - 1) / kBK;
+  g.vector_out = ((reinterpret_cast<uintptr_t>(p.out) | p.out_stride * (TYPE == QSGD_TYPE_F32 ? 4 : 2)) & 15u) == 0;
+  const uint64_t tiles = (uint64_t)g.m_tiles * g.n_tiles;
+  ScopedKernel sk(kKernMatmulI8, stream);
+  return (int)launch_chained(matmul_i8_kernel<BN, TYPE>, (uint32_t)(tiles < (uint64_t)sms ? tiles : (uint64_t)sms), kThreads, S::kSmem, stream, a, b, g);
+}
+
+template <int TYPE>
+int launch_typed(const MatmulArgs& p, cudaStream_t stream) {
+  return launch<256, TYPE>(p, stream);
+}
+
+}  // namespace
+
+bool matmul_i8_many_takes(const MatmulArgs& p) {
+  // TMA: rows on 16-byte boundaries. Tiles are counted in 32 bits.
+  const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | p.a_stride | p.b_stride) & 15u) == 0;
+  const uint64_t tiles = (uint64_t)((p.m + kBM - 1) / kBM) * ((p.n + 127) / 128);
+  return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > 64;
+}
+
+int launch_matmul_i8_many(const MatmulArgs& p, cudaStream_t stream) {
+  switch (p.type) {
+    case QSGD_TYPE_F32: return launch_typed<QSGD_TYPE_F32>(p, stream);
+    case QSGD_TYPE_F16: return launch_typed<QSGD_TYPE_F16>(p, stream);
+    default: return launch_typed<QSGD_TYPE_BF16>(p, stream);
+  }
+}
+
+}  // namespace qsgd

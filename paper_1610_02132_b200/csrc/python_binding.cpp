@@ -502,29 +502,30 @@ struct ProductCall {
   }
 };
 
-// matmul_i8(a, a_scale, b, b_scale, out, bias or None, stream)
+// matmul_i8(a, a_scale, b, b_scale, out, bias or None, status or None, stream)
 PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  QSGD_ARGS(7)
+  QSGD_ARGS(8)
   QSGD_TRY
   const c10::Device device = device_of(a[0], "a");
   const at::Tensor& x = strided(a[0], "a", at::kChar, 2, device);
   const at::Tensor& x_scale = whole(a[1], "a_scale", at::kFloat, 1, device);
   sized(x_scale, "a_scale", 0, x.size(0));
   const ProductCall c(a[2], a[3], a[4], a[5], x, "b", "b_scale", device);
-  const qsgd_stream_t stream = stream_on(a[6], device);
+  uint32_t* status = a[6] == Py_None ? nullptr : static_cast<uint32_t*>(whole(a[6], "status_dev", at::kInt, 1, device).data_ptr());
+  const qsgd_stream_t stream = stream_on(a[7], device);
   const c10::cuda::CUDAGuard guard(device);
   return unlocked([&] {
     return qsgd_matmul_i8(x.const_data_ptr<int8_t>(), stride_of(x, 0), x_scale.const_data_ptr<float>(), c.b.const_data_ptr<int8_t>(),
                           stride_of(c.b, 0), c.scale.const_data_ptr<float>(), c.bias, static_cast<uint64_t>(x.size(0)),
                           static_cast<uint64_t>(c.b.size(0)), static_cast<uint32_t>(x.size(1)), c.out.data_ptr(), stride_of(c.out, 0), c.type,
-                          stream);
+                          status, stream);
   });
   QSGD_CATCH
 }
 
-// linear_i8(x, w, w_scale, out, workspace, bias or None, stream)
+// linear_i8(x, w, w_scale, out, workspace, bias or None, status or None, stream)
 PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  QSGD_ARGS(7)
+  QSGD_ARGS(8)
   QSGD_TRY
   const c10::Device device = device_of(a[0], "x");
   const c10::ScalarType kind = THPVariable_Unpack(a[0]).scalar_type();
@@ -534,12 +535,14 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const at::Tensor& ws = whole(a[4], "workspace", at::kByte, 1, device);
   const size_t need = qsgd_linear_i8_workspace_bytes(static_cast<uint64_t>(x.size(0)), static_cast<uint32_t>(x.size(1)));
   if (ws.nbytes() < need) refuse("%s must have %lld bytes", "workspace", static_cast<long long>(need));
-  const qsgd_stream_t stream = stream_on(a[6], device);
+  uint32_t* status = a[6] == Py_None ? nullptr : static_cast<uint32_t*>(whole(a[6], "status_dev", at::kInt, 1, device).data_ptr());
+  const qsgd_stream_t stream = stream_on(a[7], device);
   const c10::cuda::CUDAGuard guard(device);
   return unlocked([&] {
     return qsgd_linear_i8(x.const_data_ptr(), stride_of(x, 0), x_type, c.b.const_data_ptr<int8_t>(), stride_of(c.b, 0),
                           c.scale.const_data_ptr<float>(), c.bias, static_cast<uint64_t>(x.size(0)), static_cast<uint64_t>(c.b.size(0)),
-                          static_cast<uint32_t>(x.size(1)), c.out.data_ptr(), stride_of(c.out, 0), c.type, ws.data_ptr(), stream);
+                          static_cast<uint32_t>(x.size(1)), c.out.data_ptr(), stride_of(c.out, 0), c.type, ws.data_ptr(), status,
+                          stream);
   });
   QSGD_CATCH
 }

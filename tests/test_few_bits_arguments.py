@@ -77,9 +77,9 @@ def test_nothing_to_do_launches_nothing():
     assert attend(r=rows(sequences=0)) == 0
     L = Q.binding.lib()
     assert L.qsgd_quantize_rows(None, 0, 64, 64, BF16, None, 64, None, None) == 0
-    assert L.qsgd_matmul_i8(None, 64, None, None, 64, None, None, 0, 5, 64, None, 5, F32, None) == 0
-    assert L.qsgd_matmul_i8(None, 64, None, None, 64, None, None, 5, 0, 64, None, 5, F32, None) == 0
-    assert L.qsgd_linear_i8(None, 64, F32, None, 64, None, None, 0, 5, 64, None, 5, F32, None, None) == 0
+    assert L.qsgd_matmul_i8(None, 64, None, None, 64, None, None, 0, 5, 64, None, 5, F32, None, None) == 0
+    assert L.qsgd_matmul_i8(None, 64, None, None, 64, None, None, 5, 0, 64, None, 5, F32, None, None) == 0
+    assert L.qsgd_linear_i8(None, 64, F32, None, 64, None, None, 0, 5, 64, None, 5, F32, None, None, None) == 0
 
 
 def test_workspace_sizes():
@@ -101,13 +101,13 @@ def test_products_refused():
     assert rows_(x=None) == rows_(codes=None) == rows_(scale=None) == NULL
     assert rows_(x=4097) == rows_(x=4098, type=F32) == rows_(scale=4098) == ALIGN
     mm = lambda a=4096, sa=4096, b=4096, sb=4096, bias=None, m=3, n=5, cols=64, out=4096, os=5, type=F32, stride=64: \
-        L.qsgd_matmul_i8(a, stride, sa, b, 64, sb, bias, m, n, cols, out, os, type, None)
+        L.qsgd_matmul_i8(a, stride, sa, b, 64, sb, bias, m, n, cols, out, os, type, None, None)
     assert mm(type=-1) == TYPE
     assert mm(cols=0) == mm(cols=131072) == mm(m=2 ** 31) == mm(n=2 ** 31) == mm(os=4) == mm(stride=2 ** 40) == SHAPE
     assert mm(a=None) == mm(b=None) == mm(sa=None) == mm(sb=None) == mm(out=None) == NULL
     assert mm(sa=4097) == mm(sb=4098) == mm(bias=4098) == mm(out=4098) == ALIGN
     lin = lambda x=4096, xt=BF16, w=4096, sw=4096, m=3, n=5, cols=64, out=4096, os=5, type=F32, ws=4096: \
-        L.qsgd_linear_i8(x, 64, xt, w, 64, sw, None, m, n, cols, out, os, type, ws, None)
+        L.qsgd_linear_i8(x, 64, xt, w, 64, sw, None, m, n, cols, out, os, type, ws, None, None)
     assert lin(xt=9) == lin(type=9) == TYPE
     assert lin(cols=0) == lin(m=2 ** 31) == lin(os=4) == SHAPE
     assert lin(x=None) == lin(w=None) == lin(sw=None) == lin(out=None) == lin(ws=None) == NULL
