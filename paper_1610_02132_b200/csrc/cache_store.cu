@@ -6,9 +6,10 @@
 // and the codes are taken against the rounded step, so a value is never further than step / 2 from what is held for it.
 //
 // Both directions move 2 * head_dim * 2 dense bytes and 9/8 * head_dim held bytes a token and head and compute little: HBM
-// bounds them. Eight lanes share a group (16 dense bytes and one word of codes each), so a warp's accesses to either side are whole sectors. Where
-// a row lies in the cache takes a search in `starts` and two dependent reads; a CTA looks that up for up to 32 rows at once, a lane to a
-// row, before it moves any of them.
+// bounds them, once the conversions stay off the slow conversion pipe (codes become floats, and floats codes, by adding 2^23). Eight lanes
+// share a group (16 dense bytes and one word of codes each), a warp's four teams four neighbouring rows, so its accesses to either side are whole
+// sectors; a team goes along its row's heads with all groups of a head in flight. Where a row lies in the cache takes a search in `starts` and two
+// dependent reads; a CTA looks that up for up to 32 rows at once, a lane to a row, before it moves any of them.
 #include <float.h>
 
 #include "cache.cuh"
@@ -24,8 +25,7 @@ struct StoreArgs {
   const uint16_t* k;
   const uint16_t* v;
   uint64_t k_token, k_head, v_token, v_head;
-  uint32_t rows_shift;          // log2 of the rows a CTA takes at a time
-  uint32_t head_dim;
+  uint32_t rows_shift;          // log2 of the rows a CTA takes
 };
 
 constexpr uint64_t kNowhere = ~0ull, kBefore = ~0ull - 1;
@@ -47,33 +47,27 @@ __device__ uint64_t place_of(const CacheView& c, uint32_t r, uint32_t tile_bytes
   return (uint64_t)at * c.page_stride + (uint64_t)(tile - page * c.page_tiles) * tile_bytes + (uint32_t)(pos % kCacheTile);
 }
 
-// What a lane of a team holds of a group: unit u of a CTA's rows, the row fastest.
-struct Unit {
-  uint64_t at;
-  uint32_t row, head, half, group;
+constexpr float kTwo23 = 8388608.0f;
+
+// A team's way along its row: where it lies on either side, and the sides first, first + step, ... of its heads (keys, then values, of each)
+struct Way {
+  uint64_t at, row;
+  uint32_t side, step;
+  uint8_t* held;               // of head 0: the lane's word of key codes; pairs lie `pair` bytes further
+  uint32_t pair;
 };
-__device__ __forceinline__ Unit unit_of(const StoreArgs& a, const uint64_t* place, uint32_t u) {
-  Unit t;
-  const uint32_t groups = a.head_dim / kCacheGroup;
-  t.row = u & ((1u << a.rows_shift) - 1u);
-  uint32_t rest = u >> a.rows_shift;
-  t.half = rest & 1u;
-  rest >>= 1;
-  t.head = rest / groups;
-  t.group = rest - t.head * groups;
-  t.at = place[t.row];
-  return t;
-}
-__device__ __forceinline__ uint64_t dense_at(const StoreArgs& a, const Unit& t, uint32_t r, uint32_t lane8) {
-  return (uint64_t)r * (t.half ? a.v_token : a.k_token) + (uint64_t)t.head * (t.half ? a.v_head : a.k_head) + t.group * kCacheGroup +
-         lane8 * 8;
-}
-// Addresses of the lane's word of codes and of the group's pair.
-__device__ __forceinline__ void held_at(const StoreArgs& a, const Unit& t, uint32_t lane8, uint32_t** word, uint32_t** pair) {
-  const uint32_t slot = (uint32_t)t.at & (kCacheTile - 1u), D = a.head_dim;
-  uint8_t* p = a.c.data + (t.at - slot) + (uint64_t)t.head * a.c.head_stride + t.half * 9 * D;
-  *word = reinterpret_cast<uint32_t*>(p + (t.group * kCacheTile + slot) * 32 + lane8 * 4);
-  *pair = reinterpret_cast<uint32_t*>(p + 8 * D + (slot * (D / kCacheGroup) + t.group) * 4);
+template <int J>
+__device__ __forceinline__ Way way_of(const StoreArgs& a, const uint64_t* place, uint64_t first) {
+  const uint32_t team = threadIdx.x / 8, lane8 = threadIdx.x % 8, r = team & ((1u << a.rows_shift) - 1u);
+  Way w;
+  w.at = place[r];
+  w.row = first + r;
+  w.side = team >> a.rows_shift;
+  w.step = kTeams >> a.rows_shift;
+  const uint32_t slot = (uint32_t)w.at & (kCacheTile - 1u);
+  w.held = a.c.data + (w.at - slot) + slot * 32 + lane8 * 4;
+  w.pair = J * 512 + slot * J * 4 - slot * 32 - lane8 * 4;
+  return w;
 }
 
 // A row is looked up in one sequence only: that every sequence's rows ascend inside the call's is looked at here, by all CTAs together.
@@ -86,115 +80,168 @@ __device__ void check_starts(const CacheView& c) {
   }
 }
 
+// Smaller and larger of two pairs of numbers; not a number where one of them is none.
 template <int TYPE>
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (TYPE == QSGD_TYPE_BF16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (TYPE == QSGD_TYPE_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// Codes and pair of a team's group; all lanes of the warp take part.
+template <int TYPE>
+__device__ __forceinline__ void quantize_group(const uint4& raw, uint32_t* codes_out, uint32_t* pair_out) {
+  uint32_t small = min2<TYPE>(min2<TYPE>(raw.x, raw.y), min2<TYPE>(raw.z, raw.w));
+  uint32_t large = max2<TYPE>(max2<TYPE>(raw.x, raw.y), max2<TYPE>(raw.z, raw.w));
+#pragma unroll
+  for (int m = 1; m < 8; m <<= 1) {
+    small = min2<TYPE>(small, __shfl_xor_sync(0xffffffffu, small, m));
+    large = max2<TYPE>(large, __shfl_xor_sync(0xffffffffu, large, m));
+  }
+  small = min2<TYPE>(small, __byte_perm(small, small, 0x1032));
+  large = max2<TYPE>(large, __byte_perm(large, large, 0x1032));
+  const float lo = from_bits16<TYPE>(small & 0xffffu) + 0.0f;               // -0 becomes +0: the pair's bits do not depend on the order
+  const float hi = from_bits16<TYPE>(large & 0xffffu);
+  // The span as the sum of two numbers, so that step is the smallest number with 15 * step (exact in fp32) at least as large, not one near it.
+  const float span = hi - lo, back = span - hi, rest = (hi - (span - back)) - (lo + back);
+  const bool fine = fabsf(span) <= FLT_MAX;                 // not with an infinity or what is no number among the values
+  uint32_t step_bits = to_bits16<TYPE>(span * (1.0f / 15.0f));
+  const float near = 15.0f * from_bits16<TYPE>(step_bits), below = 15.0f * from_bits16<TYPE>(step_bits - 1u);
+  if (near < span || (near == span && rest > 0.0f)) ++step_bits;
+  else if (step_bits && (below > span || (below == span && rest <= 0.0f))) --step_bits;
+  if (span < 15.0f * 1.1754943508222875e-38f) step_bits = 0;                // step below the smallest normal fp32: every code is 0
+  // Slightly too large on purpose (the approximation is off by 2^-23 at most): a quotient is rounded to its nearest code or to one too high, never
+  // too low. The remainder, exact in one fused operation, tells the two apart.
+  const float step = from_bits16<TYPE>(step_bits), inverse = step > 0.0f ? reciprocal(step) * (1.0f + 0x1p-21f) : 0.0f;
+  const float half = step > 0.0f ? -0.5f * step : -INFINITY;                // without a step no value leaves code 0
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const float d = from_bits16<TYPE>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu) - lo;
+    const float t = fmaf(d, inverse, kTwo23);               // 2^23 + the quotient, rounded to a whole number
+    const float r = fmaf(kTwo23 - t, step, d);
+    codes = codes * 16u + (__float_as_uint(t) - (r <= half ? 1u : 0u));
+  }
+  codes -= 0xfb000000u;                                     // the exponents of the 2^23, as far as they lie in 32 bits
+  uint32_t pair = to_bits16<TYPE>(lo) | step_bits << 16;
+  if (!fine) { codes = 0; pair = TYPE == QSGD_TYPE_BF16 ? 0x7fc07fc0u : 0x7e007e00u; }         // reads back as NaN
+  *codes_out = codes;
+  *pair_out = pair;
+}
+
+template <int TYPE, int J>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ StoreArgs a) {
   __shared__ uint64_t place[kMostRows];
-  const uint32_t team = threadIdx.x / 8, lane8 = threadIdx.x % 8, rows = 1u << a.rows_shift;
-  const uint32_t units = (a.head_dim / kCacheGroup * a.c.heads * 2) << a.rows_shift;
+  const uint32_t lane8 = threadIdx.x % 8;
+  const uint64_t first = (uint64_t)blockIdx.x << a.rows_shift;
   chain_wait();
-  for (uint64_t first = (uint64_t)blockIdx.x << a.rows_shift; first < a.c.rows; first += (uint64_t)gridDim.x << a.rows_shift) {
-    if (threadIdx.x < rows) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 18 * a.head_dim);
-    __syncthreads();
-    // (all lanes of a warp go round together: the shuffles below are of the whole warp)
-    for (uint32_t u0 = 0; u0 < units; u0 += kTeams) {
-      const uint32_t u = u0 + team;
-      Unit t = unit_of(a, place, u < units ? u : 0u);
-      if (u >= units) t.at = kNowhere;
-      const bool live = t.at < kBefore;
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (live) raw = __ldg(reinterpret_cast<const uint4*>((t.half ? a.v : a.k) + dense_at(a, t, (uint32_t)first + t.row, lane8)));
-      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-      float x[8];
+  if (threadIdx.x < 1u << a.rows_shift) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 1152 * J);
+  __syncthreads();
+  const Way w = way_of<J>(a, place, first);
+  const bool live = w.at < kBefore;
+  const uint16_t* const k = a.k + w.row * a.k_token + lane8 * 8;
+  const uint16_t* const v = a.v + w.row * a.v_token + lane8 * 8;
+  // (the lanes of a warp go round together: the shuffles are of the whole warp)
+  const uint32_t sides = 2 * a.c.heads, rounds = (sides + w.step - 1) / w.step;
+  constexpr int kAhead = J <= 2 ? 2 : 1;                    // sides whose reads are in flight together
+#pragma unroll 1
+  for (uint32_t i0 = 0; i0 < rounds; i0 += kAhead) {
+    uint4 raw[kAhead][J];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { x[2 * i] = from_bits16<TYPE>(w[i] & 0xffffu); x[2 * i + 1] = from_bits16<TYPE>(w[i] >> 16); }
-      float lo = x[0], hi = x[0];
-      bool fine = fabsf(x[0]) <= FLT_MAX;
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t side = w.side + (i0 + i) * w.step, head = side >> 1, h = side & 1u;
+      const uint16_t* const src = h ? v + head * a.v_head : k + head * a.k_head;
 #pragma unroll
-      for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); fine &= fabsf(x[i]) <= FLT_MAX; }
+      for (int j = 0; j < J; ++j)
+        raw[i][j] = live && side < sides ? __ldg(reinterpret_cast<const uint4*>(src + j * kCacheGroup)) : make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
-      for (int m = 1; m < 8; m <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
-      }
-      const uint32_t votes = __ballot_sync(0xffffffffu, fine);
-      fine = ((votes >> (threadIdx.x & 24u)) & 0xffu) == 0xffu;
-      lo += 0.0f;                                           // -0 becomes +0: the pair's bits do not depend on the order
-      fine &= hi - lo <= FLT_MAX;
-      // The span in 64 bits (exact but for wildly different exponents), so that step is the smallest number in reach, not one near it.
-      const double span = (double)hi - (double)lo;
-      uint32_t step_bits = to_bits16<TYPE>((float)span * (1.0f / 15.0f));
-      if (15.0 * (double)from_bits16<TYPE>(step_bits) < span) ++step_bits;
-      else if (step_bits && 15.0 * (double)from_bits16<TYPE>(step_bits - 1u) >= span) --step_bits;
-      if (span < 15.0 * 1.1754943508222875e-38) step_bits = 0;      // step below the smallest normal fp32: every code is 0
-      const float step = from_bits16<TYPE>(step_bits), inverse = step > 0.0f ? 1.0f / step : 0.0f;
-      const float half = step > 0.0f ? 0.5f * step : INFINITY;           // without a step no value leaves code 0
-      uint32_t codes = 0;
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t side = w.side + (i0 + i) * w.step, head = side >> 1, h = side & 1u;
+      uint8_t* const at = w.held + (uint64_t)head * a.c.head_stride + h * 576 * J;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d = x[i] - lo;
-        float c = rintf(d * inverse);
-        // The quotient's last places may have crossed a border: the remainder, exact in one fused operation, says so.
-        const float r = fmaf(-c, step, d);
-        if (r > half) c += 1.0f;
-        if (r <= -half && c > 0.0f) c -= 1.0f;
-        codes |= (uint32_t)fminf(c, 15.0f) << (4 * i);
-      }
-      uint32_t pair = to_bits16<TYPE>(lo) | step_bits << 16;
-      if (!fine) { codes = 0; pair = TYPE == QSGD_TYPE_BF16 ? 0x7fc07fc0u : 0x7e007e00u; }     // reads back as NaN
-      if (live) {
-        uint32_t *word_at, *pair_at;
-        held_at(a, t, lane8, &word_at, &pair_at);
-        *word_at = codes;
-        if (lane8 == 0) *pair_at = pair;
+      for (int j = 0; j < J; ++j) {
+        uint32_t codes, pair;
+        quantize_group<TYPE>(raw[i][j], &codes, &pair);
+        if (live && side < sides) {
+          *reinterpret_cast<uint32_t*>(at + j * 512) = codes;
+          if (lane8 == 0) *reinterpret_cast<uint32_t*>(at + w.pair + j * 4) = pair;
+        }
       }
     }
-    __syncthreads();
   }
   check_starts(a.c);
 }
 
+// Eight values of the group's type from a word of codes.
 template <int TYPE>
+__device__ __forceinline__ uint4 expand(uint32_t word, uint32_t pair) {
+  const float lo = from_bits16<TYPE>(pair & 0xffffu), step = from_bits16<TYPE>(pair >> 16);
+  const uint32_t even = word & 0x0f0f0f0fu, odd = (word >> 4) & 0x0f0f0f0fu;
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {                             // step * code is exact in fp32: one rounding there, one to the type
+    const float c0 = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 + j)) - kTwo23;         // 2^23 + code, less 2^23
+    const float c1 = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 + j)) - kTwo23;
+    o[j] = pack16<TYPE>(fmaf(step, c0, lo), fmaf(step, c1, lo));
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+template <int TYPE, int J>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ StoreArgs a) {
   __shared__ uint64_t place[kMostRows];
-  const uint32_t team = threadIdx.x / 8, lane8 = threadIdx.x % 8, rows = 1u << a.rows_shift;
-  const uint32_t units = (a.head_dim / kCacheGroup * a.c.heads * 2) << a.rows_shift;
+  const uint32_t lane8 = threadIdx.x % 8;
+  const uint64_t first = (uint64_t)blockIdx.x << a.rows_shift;
   chain_wait();
-  for (uint64_t first = (uint64_t)blockIdx.x << a.rows_shift; first < a.c.rows; first += (uint64_t)gridDim.x << a.rows_shift) {
-    if (threadIdx.x < rows) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 18 * a.head_dim);
-    __syncthreads();
-    constexpr int kAhead = 4;                               // units whose reads are in flight together
-    for (uint32_t u0 = team; u0 < units; u0 += kAhead * kTeams) {
-      uint32_t word[kAhead], pair[kAhead];
+  if (threadIdx.x < 1u << a.rows_shift) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 1152 * J);
+  __syncthreads();
+  const Way w = way_of<J>(a, place, first);
+  if (w.at != kNowhere) {
+    uint16_t* const k = const_cast<uint16_t*>(a.k) + w.row * a.k_token + lane8 * 8;
+    uint16_t* const v = const_cast<uint16_t*>(a.v) + w.row * a.v_token + lane8 * 8;
+    const uint32_t sides = 2 * a.c.heads;
+    constexpr int kAhead = 8 / J;                           // sides whose reads are in flight together
+#pragma unroll 1
+    for (uint32_t side0 = w.side; side0 < sides; side0 += kAhead * w.step) {
+      uint32_t word[kAhead][J], pair[kAhead][J];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const uint32_t u = u0 + i * kTeams;
-        word[i] = pair[i] = 0;
-        if (u < units) {
-          const Unit t = unit_of(a, place, u);
-          if (t.at < kBefore) {
-            uint32_t *word_at, *pair_at;
-            held_at(a, t, lane8, &word_at, &pair_at);
-            word[i] = __ldg(word_at);
-            pair[i] = __ldg(pair_at);
+        const uint32_t side = side0 + i * w.step, head = side >> 1, h = side & 1u;
+        const uint8_t* const at = w.held + (uint64_t)head * a.c.head_stride + h * 576 * J;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          word[i][j] = pair[i][j] = 0;                      // in front of the first token: zeros
+          if (w.at != kBefore && side < sides) {
+            word[i][j] = __ldg(reinterpret_cast<const uint32_t*>(at + j * 512));
+            pair[i][j] = __ldg(reinterpret_cast<const uint32_t*>(at + w.pair + j * 4));
           }
         }
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const uint32_t u = u0 + i * kTeams;
-        if (u >= units) break;
-        const Unit t = unit_of(a, place, u);
-        if (t.at == kNowhere) continue;
-        const float lo = from_bits16<TYPE>(pair[i] & 0xffffu), step = from_bits16<TYPE>(pair[i] >> 16);
-        uint32_t o[4];
+        const uint32_t side = side0 + i * w.step, head = side >> 1, h = side & 1u;
+        if (side < sides) {
+          uint16_t* const dst = h ? v + head * a.v_head : k + head * a.k_head;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)                         // step * code is exact in fp32: one rounding there, one to the type
-          o[j] = pack16<TYPE>(fmaf(step, (float)((word[i] >> (8 * j)) & 15u), lo), fmaf(step, (float)((word[i] >> (8 * j + 4)) & 15u), lo));
-        *reinterpret_cast<uint4*>(const_cast<uint16_t*>(t.half ? a.v : a.k) + dense_at(a, t, (uint32_t)first + t.row, lane8)) =
-            make_uint4(o[0], o[1], o[2], o[3]);
+          for (int j = 0; j < J; ++j) *reinterpret_cast<uint4*>(dst + j * kCacheGroup) = expand<TYPE>(word[i][j], pair[i][j]);
+        }
       }
     }
-    __syncthreads();
   }
   check_starts(a.c);
 }
@@ -204,31 +251,46 @@ int launch_store(Kernel kern, KernelSite& site, KernelId id, StoreArgs& a, cudaS
   int sms = 0, occ = 0;
   const int st = site.lookup(kern, kThreads, 0, &sms, &occ);
   if (st) return st;
-  // As many rows to a CTA as leave every resident CTA some: one row at a time where there are few.
-  const uint64_t ctas = (uint64_t)sms * occ;
+  // As many rows to a CTA as keep its teams busy, and more, up to 32, as long as four CTAs are left to every place: then the last ones to
+  // run make up little of the time.
+  const uint64_t places = (uint64_t)sms * occ;
   a.rows_shift = 0;
-  while (a.rows_shift < 5 && (a.c.rows >> (a.rows_shift + 1)) >= ctas) ++a.rows_shift;
+  while (a.rows_shift < 5 && kTeams >> a.rows_shift > 2 * a.c.heads) ++a.rows_shift;
+  while (a.rows_shift < 5 && (a.c.rows >> (a.rows_shift + 1)) >= 4 * places) ++a.rows_shift;
   const uint64_t blocks = ((uint64_t)a.c.rows + (1u << a.rows_shift) - 1) >> a.rows_shift;
   ScopedKernel sk(id, stream);
-  return (int)launch_chained(kern, (uint32_t)(blocks < ctas ? blocks : ctas), kThreads, 0, stream, a);
+  return (int)launch_chained(kern, (uint32_t)blocks, kThreads, 0, stream, a);
+}
+
+template <int TYPE, int J>
+int launch_way(StoreArgs& a, bool write, cudaStream_t stream) {
+  static KernelSite site[2];
+  if (write) return launch_store(cache_write_kernel<TYPE, J>, site[0], kKernCacheWrite, a, stream);
+  return launch_store(cache_read_kernel<TYPE, J>, site[1], kKernCacheRead, a, stream);
+}
+
+template <int TYPE>
+int launch_dim(StoreArgs& a, uint32_t head_dim, bool write, cudaStream_t stream) {
+  switch (head_dim / kCacheGroup) {
+    case 1: return launch_way<TYPE, 1>(a, write, stream);
+    case 2: return launch_way<TYPE, 2>(a, write, stream);
+    case 3: return launch_way<TYPE, 3>(a, write, stream);
+    default: return launch_way<TYPE, 4>(a, write, stream);
+  }
 }
 
 }  // namespace
 
 int launch_cache_write(const CacheView& view, uint32_t head_dim, int type, const void* k, uint64_t k_token, uint64_t k_head,
                        const void* v, uint64_t v_token, uint64_t v_head, cudaStream_t stream) {
-  StoreArgs a{view, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_token, k_head, v_token, v_head, 0, head_dim};
-  static KernelSite site[2];
-  if (type == QSGD_TYPE_BF16) return launch_store(cache_write_kernel<QSGD_TYPE_BF16>, site[0], kKernCacheWrite, a, stream);
-  return launch_store(cache_write_kernel<QSGD_TYPE_F16>, site[1], kKernCacheWrite, a, stream);
+  StoreArgs a{view, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_token, k_head, v_token, v_head, 0};
+  return type == QSGD_TYPE_BF16 ? launch_dim<QSGD_TYPE_BF16>(a, head_dim, true, stream) : launch_dim<QSGD_TYPE_F16>(a, head_dim, true, stream);
 }
 
 int launch_cache_read(const CacheView& view, uint32_t head_dim, int type, void* k, uint64_t k_token, uint64_t k_head, void* v,
                       uint64_t v_token, uint64_t v_head, cudaStream_t stream) {
-  StoreArgs a{view, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_token, k_head, v_token, v_head, 0, head_dim};
-  static KernelSite site[2];
-  if (type == QSGD_TYPE_BF16) return launch_store(cache_read_kernel<QSGD_TYPE_BF16>, site[0], kKernCacheRead, a, stream);
-  return launch_store(cache_read_kernel<QSGD_TYPE_F16>, site[1], kKernCacheRead, a, stream);
+  StoreArgs a{view, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_token, k_head, v_token, v_head, 0};
+  return type == QSGD_TYPE_BF16 ? launch_dim<QSGD_TYPE_BF16>(a, head_dim, false, stream) : launch_dim<QSGD_TYPE_F16>(a, head_dim, false, stream);
 }
 
 }  // namespace qsgd
