@@ -6,10 +6,11 @@
 // and the codes are taken against the rounded step, so a value is never further than step / 2 from what is held for it.
 //
 // Both directions move 2 * head_dim * 2 dense bytes and 9/8 * head_dim held bytes a token and head and compute little: HBM
-// bounds them, once the conversions stay off the slow conversion pipe (codes become floats, and floats codes, by adding 2^23). Eight lanes
-// share a group (16 dense bytes and one word of codes each), a warp's four teams four neighbouring rows, so its accesses to either side are whole
-// sectors; a team goes along its row's heads with all groups of a head in flight. Where a row lies in the cache takes a search in `starts` and two
-// dependent reads; a CTA looks that up for up to 32 rows at once, a lane to a row, before it moves any of them.
+// bounds them, once the conversions stay off the slow conversion pipe (codes become floats, and floats codes, by adding 2^23) and nobody waits for
+// places: where a row lies in the cache takes a search in `starts` and two dependent reads, and a ninth warp looks that up for the next rows
+// of its CTA while the others move the present ones (without it 55 against %s us for 15.6 K tokens of 8 heads of 128, written and read back).
+// Eight lanes share a group (16 dense bytes and one word of codes each), a warp's four teams neighbouring rows or heads; a team goes along its row's
+// keys, or values, head by head.
 #include <float.h>
 
 #include "cache.cuh"
@@ -18,14 +19,14 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kThreads = 256, kTeams = kThreads / 8, kMostRows = 32;
+constexpr uint32_t kMovers = 256, kThreads = kMovers + 32, kTeams = kMovers / 8, kMostShift = 4;
 
 struct StoreArgs {
   CacheView c;
   const uint16_t* k;
   const uint16_t* v;
   uint64_t k_token, k_head, v_token, v_head;
-  uint32_t rows_shift;          // log2 of the rows a CTA takes
+  uint32_t rows_shift;          // log2 of the rows that a CTA takes at a time
 };
 
 constexpr uint64_t kNowhere = ~0ull, kBefore = ~0ull - 1;
@@ -49,24 +50,53 @@ __device__ uint64_t place_of(const CacheView& c, uint32_t r, uint32_t tile_bytes
 
 constexpr float kTwo23 = 8388608.0f;
 
-// A team's way along its row: where it lies on either side, and the sides first, first + step, ... of its heads (keys, then values, of each)
+// Goes through the CTA's rows, 1 << rows_shift at a time: `move` by all movers with the rows' places, while the ninth warp looks up the next.
+template <int J, typename Move>
+__device__ __forceinline__ void for_rows(const StoreArgs& a, Move&& move) {
+  __shared__ uint64_t place[2][1u << kMostShift];
+  const uint32_t rows = 1u << a.rows_shift;
+  const uint64_t stride = (uint64_t)gridDim.x << a.rows_shift;
+  const bool scout = threadIdx.x >= kMovers;
+  const uint32_t i = threadIdx.x - kMovers;
+  uint64_t first = (uint64_t)blockIdx.x << a.rows_shift;
+  if (scout && i < rows) place[0][i] = first + i < a.c.rows ? place_of(a.c, (uint32_t)(first + i), 1152 * J) : kNowhere;
+  __syncthreads();
+  for (uint32_t turn = 0; first < a.c.rows; first += stride, turn ^= 1u) {
+    if (scout) {
+      const uint64_t next = first + stride + i;
+      if (i < rows) place[turn ^ 1u][i] = next < a.c.rows ? place_of(a.c, (uint32_t)next, 1152 * J) : kNowhere;
+    } else {
+      move(place[turn], first);
+    }
+    __syncthreads();
+  }
+}
+
+// A team's way along its row: the heads first, first + step, ... of the keys or of the values.
 struct Way {
-  uint64_t at, row;
-  uint32_t side, step;
-  uint8_t* held;               // of head 0: the lane's word of key codes; pairs lie `pair` bytes further
+  uint64_t at;                 // the row's place
+  uint32_t head, step;
+  uint8_t* held;               // of `head`: the lane's word of codes; pairs lie `pair` bytes further
+  uint64_t held_step;
   uint32_t pair;
+  const uint16_t* dense;
+  uint64_t dense_step;
 };
 template <int J>
 __device__ __forceinline__ Way way_of(const StoreArgs& a, const uint64_t* place, uint64_t first) {
   const uint32_t team = threadIdx.x / 8, lane8 = threadIdx.x % 8, r = team & ((1u << a.rows_shift) - 1u);
+  const uint32_t side = team >> a.rows_shift;               // the last bit of it: keys or values (two teams at least to a row)
   Way w;
   w.at = place[r];
-  w.row = first + r;
-  w.side = team >> a.rows_shift;
-  w.step = kTeams >> a.rows_shift;
+  w.head = side >> 1;
+  w.step = kTeams >> (a.rows_shift + 1);
   const uint32_t slot = (uint32_t)w.at & (kCacheTile - 1u);
-  w.held = a.c.data + (w.at - slot) + slot * 32 + lane8 * 4;
+  w.held = a.c.data + (w.at - slot) + (uint64_t)w.head * a.c.head_stride + (side & 1u) * 576 * J + slot * 32 + lane8 * 4;
+  w.held_step = (uint64_t)w.step * a.c.head_stride;
   w.pair = J * 512 + slot * J * 4 - slot * 32 - lane8 * 4;
+  const uint64_t row = first + r;
+  w.dense = (side & 1u ? a.v + row * a.v_token + (uint64_t)w.head * a.v_head : a.k + row * a.k_token + (uint64_t)w.head * a.k_head) + lane8 * 8;
+  w.dense_step = (uint64_t)w.step * (side & 1u ? a.v_head : a.k_head);
   return w;
 }
 
@@ -144,46 +174,42 @@ __device__ __forceinline__ void quantize_group(const uint4& raw, uint32_t* codes
 }
 
 template <int TYPE, int J>
-__global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ StoreArgs a) {
-  __shared__ uint64_t place[kMostRows];
+__global__ void __launch_bounds__(kThreads, 3) cache_write_kernel(const __grid_constant__ StoreArgs a) {
   const uint32_t lane8 = threadIdx.x % 8;
-  const uint64_t first = (uint64_t)blockIdx.x << a.rows_shift;
   chain_wait();
-  if (threadIdx.x < 1u << a.rows_shift) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 1152 * J);
-  __syncthreads();
-  const Way w = way_of<J>(a, place, first);
-  const bool live = w.at < kBefore;
-  const uint16_t* const k = a.k + w.row * a.k_token + lane8 * 8;
-  const uint16_t* const v = a.v + w.row * a.v_token + lane8 * 8;
-  // (the lanes of a warp go round together: the shuffles are of the whole warp)
-  const uint32_t sides = 2 * a.c.heads, rounds = (sides + w.step - 1) / w.step;
-  constexpr int kAhead = J <= 2 ? 2 : 1;                    // sides whose reads are in flight together
+  for_rows<J>(a, [&](const uint64_t* place, uint64_t first) {
+    Way w = way_of<J>(a, place, first);
+    const uint32_t heads = w.at < kBefore ? a.c.heads : 0u;
+    // (the lanes of a warp go round together: the shuffles are of the whole warp)
+    const uint32_t rounds = (a.c.heads + w.step - 1) / w.step;
+    constexpr int kAhead = J <= 2 ? 2 : 1;                  // heads whose reads are in flight together
 #pragma unroll 1
-  for (uint32_t i0 = 0; i0 < rounds; i0 += kAhead) {
-    uint4 raw[kAhead][J];
+    for (uint32_t i0 = 0; i0 < rounds; i0 += kAhead) {
+      uint4 raw[kAhead][J];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint32_t side = w.side + (i0 + i) * w.step, head = side >> 1, h = side & 1u;
-      const uint16_t* const src = h ? v + head * a.v_head : k + head * a.k_head;
+      for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        raw[i][j] = live && side < sides ? __ldg(reinterpret_cast<const uint4*>(src + j * kCacheGroup)) : make_uint4(0, 0, 0, 0);
-    }
+        for (int j = 0; j < J; ++j)
+          raw[i][j] = w.head + i * w.step < heads ? __ldg(reinterpret_cast<const uint4*>(w.dense + i * w.dense_step + j * kCacheGroup))
+                                                  : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint32_t side = w.side + (i0 + i) * w.step, head = side >> 1, h = side & 1u;
-      uint8_t* const at = w.held + (uint64_t)head * a.c.head_stride + h * 576 * J;
+      for (int i = 0; i < kAhead; ++i) {
+        if (i0 + i >= rounds) break;
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        uint32_t codes, pair;
-        quantize_group<TYPE>(raw[i][j], &codes, &pair);
-        if (live && side < sides) {
-          *reinterpret_cast<uint32_t*>(at + j * 512) = codes;
-          if (lane8 == 0) *reinterpret_cast<uint32_t*>(at + w.pair + j * 4) = pair;
+        for (int j = 0; j < J; ++j) {
+          uint32_t codes, pair;
+          quantize_group<TYPE>(raw[i][j], &codes, &pair);
+          if (w.head + i * w.step < heads) {
+            *reinterpret_cast<uint32_t*>(w.held + i * w.held_step + j * 512) = codes;
+            if (lane8 == 0) *reinterpret_cast<uint32_t*>(w.held + i * w.held_step + w.pair + j * 4) = pair;
+          }
         }
       }
+      w.head += kAhead * w.step;
+      w.held += kAhead * w.held_step;
+      w.dense += kAhead * w.dense_step;
     }
-  }
+  });
   check_starts(a.c);
 }
 
@@ -203,46 +229,36 @@ __device__ __forceinline__ uint4 expand(uint32_t word, uint32_t pair) {
 }
 
 template <int TYPE, int J>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ StoreArgs a) {
-  __shared__ uint64_t place[kMostRows];
-  const uint32_t lane8 = threadIdx.x % 8;
-  const uint64_t first = (uint64_t)blockIdx.x << a.rows_shift;
+__global__ void __launch_bounds__(kThreads, 3) cache_read_kernel(const __grid_constant__ StoreArgs a) {
   chain_wait();
-  if (threadIdx.x < 1u << a.rows_shift) place[threadIdx.x] = place_of(a.c, (uint32_t)first + threadIdx.x, 1152 * J);
-  __syncthreads();
-  const Way w = way_of<J>(a, place, first);
-  if (w.at != kNowhere) {
-    uint16_t* const k = const_cast<uint16_t*>(a.k) + w.row * a.k_token + lane8 * 8;
-    uint16_t* const v = const_cast<uint16_t*>(a.v) + w.row * a.v_token + lane8 * 8;
-    const uint32_t sides = 2 * a.c.heads;
-    constexpr int kAhead = 8 / J;                           // sides whose reads are in flight together
+  for_rows<J>(a, [&](const uint64_t* place, uint64_t first) {
+    Way w = way_of<J>(a, place, first);
+    if (w.at == kNowhere) return;
+    constexpr int kAhead = 8 / J;                           // heads whose reads are in flight together
 #pragma unroll 1
-    for (uint32_t side0 = w.side; side0 < sides; side0 += kAhead * w.step) {
+    for (; w.head < a.c.heads; w.head += kAhead * w.step) {
       uint32_t word[kAhead][J], pair[kAhead][J];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const uint32_t side = side0 + i * w.step, head = side >> 1, h = side & 1u;
-        const uint8_t* const at = w.held + (uint64_t)head * a.c.head_stride + h * 576 * J;
+      for (int i = 0; i < kAhead; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           word[i][j] = pair[i][j] = 0;                      // in front of the first token: zeros
-          if (w.at != kBefore && side < sides) {
-            word[i][j] = __ldg(reinterpret_cast<const uint32_t*>(at + j * 512));
-            pair[i][j] = __ldg(reinterpret_cast<const uint32_t*>(at + w.pair + j * 4));
+          if (w.at != kBefore && w.head + i * w.step < a.c.heads) {
+            word[i][j] = __ldg(reinterpret_cast<const uint32_t*>(w.held + i * w.held_step + j * 512));
+            pair[i][j] = __ldg(reinterpret_cast<const uint32_t*>(w.held + i * w.held_step + w.pair + j * 4));
           }
         }
-      }
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const uint32_t side = side0 + i * w.step, head = side >> 1, h = side & 1u;
-        if (side < sides) {
-          uint16_t* const dst = h ? v + head * a.v_head : k + head * a.k_head;
+      for (int i = 0; i < kAhead; ++i)
+        if (w.head + i * w.step < a.c.heads) {
 #pragma unroll
-          for (int j = 0; j < J; ++j) *reinterpret_cast<uint4*>(dst + j * kCacheGroup) = expand<TYPE>(word[i][j], pair[i][j]);
+          for (int j = 0; j < J; ++j)
+            *reinterpret_cast<uint4*>(const_cast<uint16_t*>(w.dense) + i * w.dense_step + j * kCacheGroup) = expand<TYPE>(word[i][j], pair[i][j]);
         }
-      }
+      w.held += kAhead * w.held_step;
+      w.dense += kAhead * w.dense_step;
     }
-  }
+  });
   check_starts(a.c);
 }
 
@@ -251,15 +267,15 @@ int launch_store(Kernel kern, KernelSite& site, KernelId id, StoreArgs& a, cudaS
   int sms = 0, occ = 0;
   const int st = site.lookup(kern, kThreads, 0, &sms, &occ);
   if (st) return st;
-  // As many rows to a CTA as keep its teams busy, and more, up to 32, as long as four CTAs are left to every place: then the last ones to
-  // run make up little of the time.
+  // As many rows at a time as keep the teams busy, and more, up to 16, as long as every CTA goes round six times: then the last round, which
+  // not all take part in, makes up little of the time.
   const uint64_t places = (uint64_t)sms * occ;
   a.rows_shift = 0;
-  while (a.rows_shift < 5 && kTeams >> a.rows_shift > 2 * a.c.heads) ++a.rows_shift;
-  while (a.rows_shift < 5 && (a.c.rows >> (a.rows_shift + 1)) >= 4 * places) ++a.rows_shift;
+  while (a.rows_shift < kMostShift && kTeams >> a.rows_shift > 2 * a.c.heads) ++a.rows_shift;
+  while (a.rows_shift < kMostShift && (a.c.rows >> (a.rows_shift + 1)) >= 6 * places) ++a.rows_shift;
   const uint64_t blocks = ((uint64_t)a.c.rows + (1u << a.rows_shift) - 1) >> a.rows_shift;
   ScopedKernel sk(id, stream);
-  return (int)launch_chained(kern, (uint32_t)blocks, kThreads, 0, stream, a);
+  return (int)launch_chained(kern, (uint32_t)(blocks < places ? blocks : places), kThreads, 0, stream, a);
 }
 
 template <int TYPE, int J>
