@@ -9,8 +9,8 @@
 // bounds them, once the conversions stay off the slow conversion pipe (codes become floats, and floats codes, by adding 2^23) and nobody waits for
 // places: where a row lies in the cache takes a search in `starts` and two dependent reads, and a ninth warp looks that up for the next rows
 // of its CTA while the others move the present ones (without it 55 against %s us for 15.6 K tokens of 8 heads of 128, written and read back).
-// Eight lanes share a group (16 dense bytes and one word of codes each), a warp's four teams neighbouring rows or heads; a team goes along its row's
-// keys, or values, head by head.
+// Four lanes share a group (two times 16 dense bytes and two words of codes each: with eight lanes what a group takes once, its span and step,
+// was done twice as often), a warp's eight teams neighbouring rows or heads; a team goes along its row's keys, or values, head by head.
 #include <float.h>
 
 #include "cache.cuh"
@@ -19,7 +19,7 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kMovers = 256, kThreads = kMovers + 32, kTeams = kMovers / 8, kMostShift = 4;
+constexpr uint32_t kMovers = 256, kThreads = kMovers + 32, kLanes = 4, kTeams = kMovers / kLanes, kMostShift = 5;
 
 struct StoreArgs {
   CacheView c;
@@ -76,26 +76,26 @@ __device__ __forceinline__ void for_rows(const StoreArgs& a, Move&& move) {
 struct Way {
   uint64_t at;                 // the row's place
   uint32_t head, step;
-  uint8_t* held;               // of `head`: the lane's word of codes; pairs lie `pair` bytes further
+  uint8_t* held;               // of `head`: the lane's first word of codes, the other lies 16 bytes, the pairs `pair` bytes further
   uint64_t held_step;
   uint32_t pair;
-  const uint16_t* dense;
+  const uint16_t* dense;       // the lane's first eight numbers, the others lie 32 further
   uint64_t dense_step;
 };
 template <int J>
 __device__ __forceinline__ Way way_of(const StoreArgs& a, const uint64_t* place, uint64_t first) {
-  const uint32_t team = threadIdx.x / 8, lane8 = threadIdx.x % 8, r = team & ((1u << a.rows_shift) - 1u);
+  const uint32_t team = threadIdx.x / kLanes, lane4 = threadIdx.x % kLanes, r = team & ((1u << a.rows_shift) - 1u);
   const uint32_t side = team >> a.rows_shift;               // the last bit of it: keys or values (two teams at least to a row)
   Way w;
   w.at = place[r];
   w.head = side >> 1;
   w.step = kTeams >> (a.rows_shift + 1);
   const uint32_t slot = (uint32_t)w.at & (kCacheTile - 1u);
-  w.held = a.c.data + (w.at - slot) + (uint64_t)w.head * a.c.head_stride + (side & 1u) * 576 * J + slot * 32 + lane8 * 4;
+  w.held = a.c.data + (w.at - slot) + (uint64_t)w.head * a.c.head_stride + (side & 1u) * 576 * J + slot * 32 + lane4 * 4;
   w.held_step = (uint64_t)w.step * a.c.head_stride;
-  w.pair = J * 512 + slot * J * 4 - slot * 32 - lane8 * 4;
+  w.pair = J * 512 + slot * J * 4 - slot * 32 - lane4 * 4;
   const uint64_t row = first + r;
-  w.dense = (side & 1u ? a.v + row * a.v_token + (uint64_t)w.head * a.v_head : a.k + row * a.k_token + (uint64_t)w.head * a.k_head) + lane8 * 8;
+  w.dense = (side & 1u ? a.v + row * a.v_token + (uint64_t)w.head * a.v_head : a.k + row * a.k_token + (uint64_t)w.head * a.k_head) + lane4 * 8;
   w.dense_step = (uint64_t)w.step * (side & 1u ? a.v_head : a.k_head);
   return w;
 }
@@ -133,11 +133,13 @@ __device__ __forceinline__ float reciprocal(float v) {
 
 // Codes and pair of a team's group; all lanes of the warp take part.
 template <int TYPE>
-__device__ __forceinline__ void quantize_group(const uint4& raw, uint32_t* codes_out, uint32_t* pair_out) {
-  uint32_t small = min2<TYPE>(min2<TYPE>(raw.x, raw.y), min2<TYPE>(raw.z, raw.w));
-  uint32_t large = max2<TYPE>(max2<TYPE>(raw.x, raw.y), max2<TYPE>(raw.z, raw.w));
+__device__ __forceinline__ void quantize_group(const uint4 (&raw)[2], uint32_t (&codes_out)[2], uint32_t* pair_out) {
+  uint32_t small = min2<TYPE>(min2<TYPE>(min2<TYPE>(raw[0].x, raw[0].y), min2<TYPE>(raw[0].z, raw[0].w)),
+                              min2<TYPE>(min2<TYPE>(raw[1].x, raw[1].y), min2<TYPE>(raw[1].z, raw[1].w)));
+  uint32_t large = max2<TYPE>(max2<TYPE>(max2<TYPE>(raw[0].x, raw[0].y), max2<TYPE>(raw[0].z, raw[0].w)),
+                              max2<TYPE>(max2<TYPE>(raw[1].x, raw[1].y), max2<TYPE>(raw[1].z, raw[1].w)));
 #pragma unroll
-  for (int m = 1; m < 8; m <<= 1) {
+  for (int m = 1; m < (int)kLanes; m <<= 1) {
     small = min2<TYPE>(small, __shfl_xor_sync(0xffffffffu, small, m));
     large = max2<TYPE>(large, __shfl_xor_sync(0xffffffffu, large, m));
   }
@@ -157,57 +159,52 @@ __device__ __forceinline__ void quantize_group(const uint4& raw, uint32_t* codes
   // too low. The remainder, exact in one fused operation, tells the two apart.
   const float step = from_bits16<TYPE>(step_bits), inverse = step > 0.0f ? reciprocal(step) * (1.0f + 0x1p-21f) : 0.0f;
   const float half = step > 0.0f ? -0.5f * step : -INFINITY;                // without a step no value leaves code 0
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-  uint32_t codes = 0;
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    const float d = from_bits16<TYPE>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu) - lo;
-    const float t = fmaf(d, inverse, kTwo23);               // 2^23 + the quotient, rounded to a whole number
-    const float r = fmaf(kTwo23 - t, step, d);
-    codes = codes * 16u + (__float_as_uint(t) - (r <= half ? 1u : 0u));
+  for (int x = 0; x < 2; ++x) {
+    const uint32_t w[4] = {raw[x].x, raw[x].y, raw[x].z, raw[x].w};
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      const float d = from_bits16<TYPE>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu) - lo;
+      const float t = fmaf(d, inverse, kTwo23);             // 2^23 + the quotient, rounded to a whole number
+      const float r = fmaf(kTwo23 - t, step, d);
+      codes = codes * 16u + (__float_as_uint(t) - (r <= half ? 1u : 0u));
+    }
+    codes_out[x] = fine ? codes - 0xfb000000u : 0u;         // less the exponents of the 2^23, as far as they lie in 32 bits
   }
-  codes -= 0xfb000000u;                                     // the exponents of the 2^23, as far as they lie in 32 bits
-  uint32_t pair = to_bits16<TYPE>(lo) | step_bits << 16;
-  if (!fine) { codes = 0; pair = TYPE == QSGD_TYPE_BF16 ? 0x7fc07fc0u : 0x7e007e00u; }         // reads back as NaN
-  *codes_out = codes;
-  *pair_out = pair;
+  *pair_out = fine ? to_bits16<TYPE>(lo) | step_bits << 16 : TYPE == QSGD_TYPE_BF16 ? 0x7fc07fc0u : 0x7e007e00u;     // reads back as NaN
 }
 
 template <int TYPE, int J>
 __global__ void __launch_bounds__(kThreads, 3) cache_write_kernel(const __grid_constant__ StoreArgs a) {
-  const uint32_t lane8 = threadIdx.x % 8;
+  const uint32_t lane4 = threadIdx.x % kLanes;
   chain_wait();
   for_rows<J>(a, [&](const uint64_t* place, uint64_t first) {
     Way w = way_of<J>(a, place, first);
     const uint32_t heads = w.at < kBefore ? a.c.heads : 0u;
     // (the lanes of a warp go round together: the shuffles are of the whole warp)
     const uint32_t rounds = (a.c.heads + w.step - 1) / w.step;
-    constexpr int kAhead = J <= 2 ? 2 : 1;                  // heads whose reads are in flight together
 #pragma unroll 1
-    for (uint32_t i0 = 0; i0 < rounds; i0 += kAhead) {
-      uint4 raw[kAhead][J];
+    for (uint32_t i = 0; i < rounds; ++i) {
+      uint4 raw[J][2];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i)
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-          raw[i][j] = w.head + i * w.step < heads ? __ldg(reinterpret_cast<const uint4*>(w.dense + i * w.dense_step + j * kCacheGroup))
-                                                  : make_uint4(0, 0, 0, 0);
+        for (int x = 0; x < 2; ++x)
+          raw[j][x] = w.head < heads ? __ldg(reinterpret_cast<const uint4*>(w.dense + j * kCacheGroup + x * 32)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        if (i0 + i >= rounds) break;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-          uint32_t codes, pair;
-          quantize_group<TYPE>(raw[i][j], &codes, &pair);
-          if (w.head + i * w.step < heads) {
-            *reinterpret_cast<uint32_t*>(w.held + i * w.held_step + j * 512) = codes;
-            if (lane8 == 0) *reinterpret_cast<uint32_t*>(w.held + i * w.held_step + w.pair + j * 4) = pair;
-          }
+      for (int j = 0; j < J; ++j) {
+        uint32_t codes[2], pair;
+        quantize_group<TYPE>(raw[j], codes, &pair);
+        if (w.head < heads) {
+          *reinterpret_cast<uint32_t*>(w.held + j * 512) = codes[0];
+          *reinterpret_cast<uint32_t*>(w.held + j * 512 + 16) = codes[1];
+          if (lane4 == 0) *reinterpret_cast<uint32_t*>(w.held + w.pair + j * 4) = pair;
         }
       }
-      w.head += kAhead * w.step;
-      w.held += kAhead * w.held_step;
-      w.dense += kAhead * w.dense_step;
+      w.head += w.step;
+      w.held += w.held_step;
+      w.dense += w.dense_step;
     }
   });
   check_starts(a.c);
@@ -234,26 +231,30 @@ __global__ void __launch_bounds__(kThreads, 3) cache_read_kernel(const __grid_co
   for_rows<J>(a, [&](const uint64_t* place, uint64_t first) {
     Way w = way_of<J>(a, place, first);
     if (w.at == kNowhere) return;
-    constexpr int kAhead = 8 / J;                           // heads whose reads are in flight together
+    constexpr int kAhead = J <= 2 ? 4 / J : 1;              // heads whose reads are in flight together
 #pragma unroll 1
     for (; w.head < a.c.heads; w.head += kAhead * w.step) {
-      uint32_t word[kAhead][J], pair[kAhead][J];
+      uint32_t word[kAhead][J][2], pair[kAhead][J];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          word[i][j] = pair[i][j] = 0;                      // in front of the first token: zeros
+          word[i][j][0] = word[i][j][1] = pair[i][j] = 0;   // in front of the first token: zeros
           if (w.at != kBefore && w.head + i * w.step < a.c.heads) {
-            word[i][j] = __ldg(reinterpret_cast<const uint32_t*>(w.held + i * w.held_step + j * 512));
-            pair[i][j] = __ldg(reinterpret_cast<const uint32_t*>(w.held + i * w.held_step + w.pair + j * 4));
+            const uint8_t* const at = w.held + i * w.held_step;
+            word[i][j][0] = __ldg(reinterpret_cast<const uint32_t*>(at + j * 512));
+            word[i][j][1] = __ldg(reinterpret_cast<const uint32_t*>(at + j * 512 + 16));
+            pair[i][j] = __ldg(reinterpret_cast<const uint32_t*>(at + w.pair + j * 4));
           }
         }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
         if (w.head + i * w.step < a.c.heads) {
+          uint16_t* const to = const_cast<uint16_t*>(w.dense) + i * w.dense_step;
 #pragma unroll
           for (int j = 0; j < J; ++j)
-            *reinterpret_cast<uint4*>(const_cast<uint16_t*>(w.dense) + i * w.dense_step + j * kCacheGroup) = expand<TYPE>(word[i][j], pair[i][j]);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) *reinterpret_cast<uint4*>(to + j * kCacheGroup + x * 32) = expand<TYPE>(word[i][j][x], pair[i][j]);
         }
       w.held += kAhead * w.held_step;
       w.dense += kAhead * w.dense_step;
@@ -267,7 +268,7 @@ int launch_store(Kernel kern, KernelSite& site, KernelId id, StoreArgs& a, cudaS
   int sms = 0, occ = 0;
   const int st = site.lookup(kern, kThreads, 0, &sms, &occ);
   if (st) return st;
-  // As many rows at a time as keep the teams busy, and more, up to 16, as long as every CTA goes round six times: then the last round, which
+  // As many rows at a time as keep the teams busy, and more, up to 32, as long as every CTA goes round six times: then the last round, which
   // not all take part in, makes up little of the time.
   const uint64_t places = (uint64_t)sms * occ;
   a.rows_shift = 0;
