@@ -27,7 +27,7 @@ int qsgd_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row
   if (rows == 0) return QSGD_OK;
   if (!x || !codes || !scale) return QSGD_ERR_NULL;
   if (!on(x, size_of(type)) || !on(scale, 4)) return QSGD_ERR_ALIGN;
-  return launch_quantize_rows(x, rows, cols, row_stride, type, codes, codes_stride, scale, static_cast<cudaStream_t>(stream));
+  return launch_quantize_rows(x, rows, cols, row_stride, type, codes, codes_stride, scale, false, static_cast<cudaStream_t>(stream));
 }
 
 int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, const int8_t* b, uint64_t b_stride, const float* b_scale,
@@ -42,7 +42,7 @@ int qsgd_matmul_i8(const int8_t* a, uint64_t a_stride, const float* a_scale, con
   if (!on(a_scale, 4) || !on(b_scale, 4) || !on(bias, 4) || !on(out, size_of(type))) return QSGD_ERR_ALIGN;
   const MatmulArgs args{a, b, a_scale, b_scale, bias, out, m > 1 ? a_stride : padded_cols(cols), n > 1 ? b_stride : padded_cols(cols),
                         out_stride, (uint32_t)m, (uint32_t)n, cols, type, status_dev};
-  return launch_matmul_i8(args, static_cast<cudaStream_t>(stream));
+  return launch_matmul_i8(args, false, static_cast<cudaStream_t>(stream));
 }
 
 size_t qsgd_linear_i8_workspace_bytes(uint64_t m, uint32_t cols) {
@@ -62,9 +62,11 @@ int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w
   if (!on(workspace, 16) || !on(x, size_of(x_type)) || !on(w_scale, 4) || !on(bias, 4) || !on(out, size_of(out_type))) return QSGD_ERR_ALIGN;
   int8_t* codes = static_cast<int8_t*>(workspace);
   float* scale = reinterpret_cast<float*>(codes + m * padded_cols(cols));
-  const int st = qsgd_quantize_rows(x, m, cols, x_stride, x_type, codes, padded_cols(cols), scale, stream);
-  if (st) return st;
-  return qsgd_matmul_i8(codes, padded_cols(cols), scale, w, w_stride, w_scale, bias, m, n, cols, out, out_stride, out_type, status_dev, stream);
+  const MatmulArgs args{codes, w, scale, w_scale, bias, out, padded_cols(cols), n > 1 ? w_stride : padded_cols(cols), out_stride, (uint32_t)m,
+                        (uint32_t)n, cols, out_type, status_dev};
+  const bool few = !matmul_i8_many_takes(args) && m <= 64;
+  const int st = launch_quantize_rows(x, m, cols, x_stride, x_type, codes, padded_cols(cols), scale, few, static_cast<cudaStream_t>(stream));
+  return st ? st : launch_matmul_i8(args, few, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -6,7 +6,8 @@
 namespace qsgd {
 
 int launch_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row_stride, int type, int8_t* codes, uint64_t codes_stride,
-                         float* scale, cudaStream_t stream);
+                         float* scale, bool release, cudaStream_t stream);
+// release: the next kernel of the stream may start as soon as the kernels in front of this one are done. It waits for this one itself.
 
 struct MatmulArgs {
   const int8_t* a;
@@ -20,7 +21,8 @@ struct MatmulArgs {
   int type;
   uint32_t* status;           // or nullptr
 };
-int launch_matmul_i8(const MatmulArgs& args, cudaStream_t stream);
+// early: the kernel ahead is the one that writes a and its scales, launched with `release`; b, its scales and the bias are older.
+int launch_matmul_i8(const MatmulArgs& args, bool early, cudaStream_t stream);
 
 // For many rows (matmul_i8.cu): whether it takes a product, and the launch.
 bool matmul_i8_many_takes(const MatmulArgs& args);

@@ -22,6 +22,7 @@ struct RowsArgs {
   float* scale;
   uint64_t rows, row_stride, codes_stride;
   uint32_t cols;
+  bool release;
 };
 
 template <int TYPE>
@@ -91,6 +92,8 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_co
   __shared__ float warp_top[kThreads / 32];
   const uint32_t c0 = 8 * threadIdx.x;
   chain_wait();
+  // (The library's kernels else release no dependents: waiting CTAs slow running ones down. Here the running ones are a CTA to a row, 64 at most.)
+  if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = static_cast<const T*>(a.x) + r * a.row_stride;
     int8_t* out = a.codes + r * a.codes_stride;
@@ -161,8 +164,8 @@ int launch(const RowsArgs& a, cudaStream_t stream) {
 }  // namespace
 
 int launch_quantize_rows(const void* x, uint64_t rows, uint32_t cols, uint64_t row_stride, int type, int8_t* codes, uint64_t codes_stride,
-                         float* scale, cudaStream_t stream) {
-  const RowsArgs a{x, codes, scale, rows, row_stride, codes_stride, cols};
+                         float* scale, bool release, cudaStream_t stream) {
+  const RowsArgs a{x, codes, scale, rows, row_stride, codes_stride, cols, release};
   const uint64_t size = type == QSGD_TYPE_F32 ? 4 : 2;
   const bool vector = ((reinterpret_cast<uintptr_t>(x) | row_stride * size) & 15u) == 0 &&
                       ((reinterpret_cast<uintptr_t>(codes) | codes_stride) & 7u) == 0;
