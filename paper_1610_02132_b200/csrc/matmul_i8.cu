@@ -1,9 +1,13 @@
 // Product in 8-bit integers for many rows: out[m][n] = (a_m . b_n) a_scale b_scale + bias on the fifth-generation tensor cores.
 //
-// Tiles of 128 x BN of the output, each summed over K by tcgen05.mma (kind::i8, exact 32-bit sums in tensor memory). A persistent CTA per SM:
-// one thread keeps a ring of stages (128 columns of 128 rows of a and BN rows of b, 128-byte swizzle) filled by TMA, which puts zeros where a or b
+// Tiles of 128 x `width` of the output, each summed over K by tcgen05.mma (kind::i8, exact 32-bit sums in tensor memory). A persistent CTA per SM:
+// one thread keeps a ring of stages (128 columns of 128 rows of a and `width` rows of b, 128-byte swizzle) filled by TMA, which puts zeros where a or b
 // end; one thread issues the products; four warps take finished sums out of tensor memory, scale them and store them, while the next tile's
 // products run into the other half of tensor memory.
+//
+// The width is what leaves the SMs least idle (pick_width): 256 for large products, where it halves the traffic from L2 against 128; fewer columns,
+// so that there is a tile for every SM, where rows are few: the bytes of b are then what bounds a product, and a narrow tile's ring holds as many of
+// them in flight as a wide one's.
 //
 // All waits are bounded. One that runs out raises a flag in shared memory, at which every role leaves its loop; the CTA then waits for the
 // copies and products in flight (bounded again), frees its tensor memory and returns with QSGD_DEV_TIMEOUT in the status word, if there is one.
@@ -19,20 +23,31 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kBM = 128, kBK = 128, kStages = 4, kThreads = 192, kEpilogueWarps = 4;
+constexpr uint32_t kBM = 128, kBK = 128, kMostStages = 16, kThreads = 192, kEpilogueWarps = 4;
+constexpr uint32_t kMostWidth = 256, kLeastWidth = 32;
+constexpr uint32_t kRingBytes = 4 * (kBM + kMostWidth) * kBK;
+// Stages on 1024-byte boundaries. A stage holds no more rows of a than there are; the products read 128 all the same, whatever lies behind (sums of
+// rows that are not there go nowhere), so there is that much room behind the last stage.
+constexpr uint32_t kSmem = kRingBytes + kBM * kBK + 1024;
 constexpr uint32_t kPolls = 1u << 22;
+// Up to here matmul_i8_few.cu: 16 rows of 16384 x 4096 take 19.0 us there and 21.6 here, 32 rows 36.5 and 16.8 (4096 x 4096: 7.9 and 16, 16 rows).
+constexpr uint32_t kFewRows = 16;
 
 struct GemmParams {
   MatmulArgs p;
   uint32_t m_tiles, n_tiles, k_steps;
+  uint32_t width, stages;      // columns of a tile (a multiple of 16), stages of the ring
+  uint32_t a_bytes;            // of a stage's rows of a
   bool vector_out;             // rows of out begin on 16-byte boundaries
 };
 
-template <uint32_t BN>
-struct Shape {
-  static constexpr uint32_t kA = kBM * kBK, kB = BN * kBK, kStage = kA + kB;
-  static constexpr uint32_t kSmem = kStages * kStage + 1024;               // stages on 1024-byte boundaries
-  static constexpr uint32_t kColumns = 2 * BN;                              // of tensor memory: two tiles of sums
+// Position in a ring of stages.
+struct Ring {
+  uint32_t stage = 0, parity = 0, fills = 0;
+  __device__ __forceinline__ void next(uint32_t stages) {
+    ++fills;
+    if (++stage == stages) { stage = 0; parity ^= 1u; }
+  }
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -76,14 +91,11 @@ __device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint3
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
                "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at, int32_t (&v)[32]) {
+__device__ __forceinline__ void tmem_load16(uint32_t at, int32_t (&v)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
-      "%28,%29,%30,%31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
-        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
-        "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
-        "=r"(v[31])
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(at));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -128,27 +140,24 @@ __device__ __forceinline__ uint4 pack_out(const float* v) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <uint32_t BN, int TYPE>
+template <int TYPE>
 __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                const __grid_constant__ GemmParams g) {
-  using S = Shape<BN>;
   typedef typename Out<TYPE>::T T;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
+  __shared__ uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_empty[2];
   __shared__ uint32_t tmem_base, given_up;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-  const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u, stage_bytes = g.a_bytes + g.width * kBK;
   const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), sums_full0 = smem_u32(sums_full), sums_empty0 = smem_u32(sums_empty);
   if (threadIdx.x == 0) {
-#pragma unroll
-    for (uint32_t s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-#pragma unroll
+    for (uint32_t s = 0; s < g.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     for (uint32_t s = 0; s < 2; ++s) { mbar_init(sums_full0 + 8 * s, 1); mbar_init(sums_empty0 + 8 * s, kEpilogueWarps); }
     given_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 0)
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(S::kColumns) : "memory");
+  if (warp == 0)                                            // all of tensor memory: two tiles of up to 256 columns
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(2 * kMostWidth) : "memory");
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -158,50 +167,52 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   const uint32_t tiles = g.m_tiles * g.n_tiles;
   if (warp == 0) {                                          // ---- fills the ring ------------------------------------------------
     if (lane == 0) {
-      uint32_t it = 0;
+      Ring r;
       bool fine = true;
       for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x) {
         uint32_t m, n;
         tile_at(g, i, &m, &n);
-        for (uint32_t k = 0; k < g.k_steps; ++k, ++it) {
-          const uint32_t s = it % kStages, round = it / kStages;
-          if (round && !mbar_wait(empty0 + 8 * s, (round - 1) & 1u, &given_up)) { fine = false; break; }
-          const uint32_t at = stages + s * S::kStage;
-          mbar_expect(full0 + 8 * s, S::kStage);
-          tma_load(at, &map_a, k * kBK, m * kBM, full0 + 8 * s);
-          tma_load(at + S::kA, &map_b, k * kBK, n * BN, full0 + 8 * s);
+        for (uint32_t k = 0; k < g.k_steps; ++k) {
+          if (r.fills >= g.stages && !mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, &given_up)) { fine = false; break; }
+          const uint32_t at = ring0 + r.stage * stage_bytes, bar = full0 + 8 * r.stage;
+          mbar_expect(bar, stage_bytes);
+          tma_load(at, &map_a, k * kBK, m * kBM, bar);
+          tma_load(at + g.a_bytes, &map_b, k * kBK, n * g.width, bar);
+          r.next(g.stages);
         }
       }
-      // What is in flight lands before the CTA's shared memory goes away.
-      for (uint32_t s = 0; s < kStages && s < it && !fine; ++s) {
-        const uint32_t last = (it - 1 - s) / kStages;       // the round of stage s' = (it - 1 - s) % kStages that was filled last
-        for (uint32_t t = 0; t < kPolls && !mbar_try(full0 + 8 * ((it - 1 - s) % kStages), last & 1u); ++t) {}
+      // After a wait that ran out: what is in flight lands before the CTA's shared memory goes away.
+      for (uint32_t back = 1; !fine && back <= g.stages && back <= r.fills; ++back) {
+        const uint32_t fill = r.fills - back;
+        for (uint32_t t = 0; t < kPolls && !mbar_try(full0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
       }
     }
   } else if (warp == 1) {                                   // ---- issues the products -------------------------------------------
     if (lane == 0) {
-      constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((BN >> 3) << 17) | ((kBM >> 4) << 24);     // s32 += s8 * s8
-      uint32_t it = 0, done = 0;
+      const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((g.width >> 3) << 17) | ((kBM >> 4) << 24);     // s32 += s8 * s8
+      Ring r;
+      uint32_t done = 0;
       bool fine = true;
       for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x, ++done) {
         const uint32_t half = done & 1u, use = done >> 1;
-        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, &given_up)) break;
+        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, &given_up)) { fine = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (uint32_t k = 0; k < g.k_steps; ++k, ++it) {
-          const uint32_t s = it % kStages;
-          if (!mbar_wait(full0 + 8 * s, (it / kStages) & 1u, &given_up)) { fine = false; break; }
+        for (uint32_t k = 0; k < g.k_steps; ++k) {
+          if (!mbar_wait(full0 + 8 * r.stage, r.parity, &given_up)) { fine = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t a = tile_desc(stages + s * S::kStage), b = tile_desc(stages + s * S::kStage + S::kA);
+          const uint32_t at = ring0 + r.stage * stage_bytes;
+          const uint64_t a = tile_desc(at), b = tile_desc(at + g.a_bytes);
 #pragma unroll
-          for (uint32_t x = 0; x < kBK / 32; ++x) mma_i8(tmem + half * BN, a + 2 * x, b + 2 * x, idesc, k != 0 || x != 0);
-          tc_commit(empty0 + 8 * s);
+          for (uint32_t x = 0; x < kBK / 32; ++x) mma_i8(tmem + half * kMostWidth, a + 2 * x, b + 2 * x, idesc, k != 0 || x != 0);
+          tc_commit(empty0 + 8 * r.stage);
+          r.next(g.stages);
         }
         if (fine) tc_commit(sums_full0 + 8 * half);
       }
-      // Products in flight are done before tensor memory is freed: after a wait that ran out, the last commit is waited for here.
-      if (!fine && it) {
-        const uint32_t last = it - 1;
-        for (uint32_t t = 0; t < kPolls && !mbar_try(empty0 + 8 * (last % kStages), (last / kStages) & 1u); ++t) {}
+      // After a wait that ran out: products in flight are done before tensor memory is freed.
+      if (!fine && r.fills) {
+        const uint32_t fill = r.fills - 1;
+        for (uint32_t t = 0; t < kPolls && !mbar_try(empty0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
       }
     }
   } else {                                                  // ---- takes the sums out --------------------------------------------
@@ -218,29 +229,32 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
       const bool live = row < g.p.m;
       const float a_scale = live ? __ldg(g.p.a_scale + row) : 0.0f;
       T* const out = static_cast<T*>(g.p.out) + (uint64_t)row * g.p.out_stride;
-#pragma unroll 1
-      for (uint32_t c = 0; c < BN; c += 32) {
-        int32_t v[32];
-        tmem_load32(tmem + half * BN + c + ((32 * quarter) << 16), v);
-        const uint32_t col = n * BN + c;
-        if (live && col < g.p.n) {
-          float y[32];
+      if (m * kBM + 32 * quarter < g.p.m) {                 // (of the warp: some of its rows are there)
+#pragma unroll 2
+        for (uint32_t c = 0; c < g.width; c += 16) {
+          const uint32_t col = n * g.width + c;
+          if (col >= g.p.n) break;
+          int32_t v[16];
+          tmem_load16(tmem + half * kMostWidth + c + ((32 * quarter) << 16), v);
+          if (live) {
+            float y[16];
 #pragma unroll
-          for (int x = 0; x < 32; ++x) {
-            const uint32_t at = col + x < g.p.n ? col + x : g.p.n - 1;
-            y[x] = scaled_sum(v[x], a_scale, __ldg(g.p.b_scale + at), g.p.bias ? __ldg(g.p.bias + at) : 0.0f);
+            for (int x = 0; x < 16; ++x) {
+              const uint32_t at = col + x < g.p.n ? col + x : g.p.n - 1;
+              y[x] = scaled_sum(v[x], a_scale, __ldg(g.p.b_scale + at), g.p.bias ? __ldg(g.p.bias + at) : 0.0f);
+            }
+            if (g.vector_out && col + 16 <= g.p.n) {
+              constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+              for (int x = 0; x < 16; x += kPer) *reinterpret_cast<uint4*>(out + col + x) = pack_out<TYPE>(y + x);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 16; ++x)
+                if (col + x < g.p.n) out[col + x] = Out<TYPE>::one(y[x]);
+            }
           }
-          if (g.vector_out && col + 32 <= g.p.n) {
-            constexpr int kPer = 16 / sizeof(T);
-#pragma unroll
-            for (int x = 0; x < 32; x += kPer) *reinterpret_cast<uint4*>(out + col + x) = pack_out<TYPE>(y + x);
-          } else {
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (col + x < g.p.n) out[col + x] = Out<TYPE>::one(y[x]);
-          }
+          __syncwarp();                                     // the next read of tensor memory is of the whole warp
         }
-        __syncwarp();                                       // the next read of tensor memory is of the whole warp
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -253,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 0) {
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns));
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kMostWidth));
   }
   if (threadIdx.x == 0 && given_up && g.p.status) atomicOr(g.p.status, QSGD_DEV_TIMEOUT);
 }
@@ -287,31 +301,42 @@ int make_map(CUtensorMap* map, const int8_t* base, uint32_t cols, uint32_t rows,
   return r == CUDA_SUCCESS ? 0 : (int)cudaErrorInvalidValue;
 }
 
-template <uint32_t BN, int TYPE>
+// Columns of a tile. The tiles go round the SMs in rounds of equal length: a round takes as long as a tile has columns of b to bring in and to multiply
+// with, and a part for a's rows and the tile's beginning and end.
+uint32_t pick_width(uint32_t m_tiles, uint32_t a_rows, uint32_t n, uint32_t sms) {
+  uint32_t best = kMostWidth;
+  uint64_t least = ~0ull;
+  for (uint32_t w = kMostWidth; w >= kLeastWidth; w -= 16) {
+    const uint64_t tiles = (uint64_t)m_tiles * ((n + w - 1) / w), cost = (tiles + sms - 1) / sms * (w + a_rows / 2);
+    if (cost < least) { least = cost; best = w; }
+  }
+  return best;
+}
+
+template <int TYPE>
 int launch(const MatmulArgs& p, cudaStream_t stream) {
-  using S = Shape<BN>;
   static KernelSite site;
   int sms = 0, occ = 0;
-  int st = site.lookup(matmul_i8_kernel<BN, TYPE>, kThreads, S::kSmem, &sms, &occ);
-  if (st) return st;
-  CUtensorMap a, b;
-  st = make_map(&a, p.a, p.k, p.m, p.a_stride, kBM);
-  if (!st) st = make_map(&b, p.b, p.k, p.n, p.b_stride, BN);
+  int st = site.lookup(matmul_i8_kernel<TYPE>, kThreads, kSmem, &sms, &occ);
   if (st) return st;
   GemmParams g;
   g.p = p;
   g.m_tiles = (p.m + kBM - 1) / kBM;
-  g.n_tiles = (p.n + BN - 1) / BN;
+  const uint32_t a_rows = p.m < kBM ? (p.m + 7) / 8 * 8 : kBM;              // (8 rows of 128 bytes: the swizzle's period)
+  g.a_bytes = a_rows * kBK;
+  g.width = pick_width(g.m_tiles, a_rows, p.n, (uint32_t)sms);
+  g.n_tiles = (p.n + g.width - 1) / g.width;
   g.k_steps = (p.k + kBK - 1) / kBK;
+  g.stages = kRingBytes / (g.a_bytes + g.width * kBK);
+  if (g.stages > kMostStages) g.stages = kMostStages;
   g.vector_out = ((reinterpret_cast<uintptr_t>(p.out) | p.out_stride * (TYPE == QSGD_TYPE_F32 ? 4 : 2)) & 15u) == 0;
+  CUtensorMap a, b;
+  st = make_map(&a, p.a, p.k, p.m, p.a_stride, a_rows);
+  if (!st) st = make_map(&b, p.b, p.k, p.n, p.b_stride, g.width);
+  if (st) return st;
   const uint64_t tiles = (uint64_t)g.m_tiles * g.n_tiles;
   ScopedKernel sk(kKernMatmulI8, stream);
-  return (int)launch_chained(matmul_i8_kernel<BN, TYPE>, (uint32_t)(tiles < (uint64_t)sms ? tiles : (uint64_t)sms), kThreads, S::kSmem, stream, a, b, g);
-}
-
-template <int TYPE>
-int launch_typed(const MatmulArgs& p, cudaStream_t stream) {
-  return launch<256, TYPE>(p, stream);
+  return (int)launch_chained(matmul_i8_kernel<TYPE>, (uint32_t)(tiles < (uint64_t)sms ? tiles : (uint64_t)sms), kThreads, kSmem, stream, a, b, g);
 }
 
 }  // namespace
@@ -319,15 +344,15 @@ int launch_typed(const MatmulArgs& p, cudaStream_t stream) {
 bool matmul_i8_many_takes(const MatmulArgs& p) {
   // TMA: rows on 16-byte boundaries. Tiles are counted in 32 bits.
   const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | p.a_stride | p.b_stride) & 15u) == 0;
-  const uint64_t tiles = (uint64_t)((p.m + kBM - 1) / kBM) * ((p.n + 127) / 128);
-  return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > 64;
+  const uint64_t tiles = (uint64_t)((p.m + kBM - 1) / kBM) * ((p.n + kLeastWidth - 1) / kLeastWidth);
+  return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > kFewRows;
 }
 
 int launch_matmul_i8_many(const MatmulArgs& p, cudaStream_t stream) {
   switch (p.type) {
-    case QSGD_TYPE_F32: return launch_typed<QSGD_TYPE_F32>(p, stream);
-    case QSGD_TYPE_F16: return launch_typed<QSGD_TYPE_F16>(p, stream);
-    default: return launch_typed<QSGD_TYPE_BF16>(p, stream);
+    case QSGD_TYPE_F32: return launch<QSGD_TYPE_F32>(p, stream);
+    case QSGD_TYPE_F16: return launch<QSGD_TYPE_F16>(p, stream);
+    default: return launch<QSGD_TYPE_BF16>(p, stream);
   }
 }
 

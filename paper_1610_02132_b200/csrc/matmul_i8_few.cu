@@ -1,6 +1,6 @@
 // Product in 8-bit integers for few rows of a (and for rows that begin anywhere): out[m][n] = (a_m . b_n) a_scale b_scale + bias.
 //
-// Bytes of b bound it: each is read once and used for up to 64 rows of a. A CTA takes 16 rows of b (those of an m16n8k32 product) and its warps
+// Bytes of b bound it: each is read once for up to 16 rows of a (up to 64 where rows begin anywhere). A CTA takes 16 rows of b (those of an m16n8k32 product) and its warps
 // 64 columns of them in turn; a lane reads 16 bytes of two of its rows straight into registers, since the order of the columns inside a product does
 // not matter as long as both operands agree. The warps meet in shared memory; integer sums have no order. CTAs are small so that a GPU full of them
 // holds all the rows of b at once where they are not too many: 16384 rows are 1024 CTAs, 7 to an SM, and no second round is left half empty.
@@ -159,11 +159,10 @@ int launch_matmul_i8(const MatmulArgs& p, bool early, cudaStream_t stream) {
     q.a_scale += m0;
     q.out = static_cast<uint8_t*>(p.out) + (uint64_t)m0 * p.out_stride * (p.type == QSGD_TYPE_F32 ? 4 : 2);
     int st;
-    if (q.m <= 8) st = aligned ? launch<1, true>(q, early, stream) : launch<1, false>(q, early, stream);
-    else if (q.m <= 16) st = aligned ? launch<2, true>(q, early, stream) : launch<2, false>(q, early, stream);
-    else if (q.m <= 32) st = aligned ? launch<4, true>(q, early, stream) : launch<4, false>(q, early, stream);
-    else if (q.m <= 48) st = aligned ? launch<6, true>(q, early, stream) : launch<6, false>(q, early, stream);
-    else st = aligned ? launch<8, true>(q, early, stream) : launch<8, false>(q, early, stream);
+    if (aligned && q.m <= 16) st = q.m <= 8 ? launch<1, true>(q, early, stream) : launch<2, true>(q, early, stream);
+    else if (q.m <= 8) st = launch<1, false>(q, early, stream);
+    else if (q.m <= 32) st = launch<4, false>(q, early, stream);
+    else st = launch<8, false>(q, early, stream);
     if (st) return st;
     m0 += q.m;
     early = false;
