@@ -31,9 +31,11 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kWarps = 8, kThreads = 32 * kWarps;
+constexpr uint32_t kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
-constexpr uint32_t kLeastStretch = 4;     // units of a warp's stretch at least
+constexpr uint32_t kLeastStretch = 2;     // units of a warp's stretch at least, and of a CTA's
+constexpr uint32_t kLeastCta = 8;
+constexpr uint32_t kDirectTokens = 2048;  // longest sequence that may be given to one CTA
 constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kPolls = 1u << 22;
@@ -62,6 +64,7 @@ struct AttendParams {
   float* lse;
   uint32_t q_heads, group;
   float scale_log2;
+  bool direct;                            // a CTA to a segment: nothing spans CTAs
   JoinInfo* join;
   float* parts;                           // [CTA][2][rows * (dim + 2)]
 };
@@ -190,8 +193,11 @@ __device__ __forceinline__ Sequence sequence_at(const AttendParams& p, uint32_t 
 template <int TYPE, int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT, kGroups = D / 64;
+  // A CTA fills its SM: with 128 registers a thread 16 warps, else 8. (As two CTAs of 8, the second one's warps were given 18 % less of the SM's
+  // time than the first one's, and worked on alone at the end.)
+  static constexpr uint32_t kWarps = D <= 128 && NT == 1 ? 16 : 8, kThreads = 32 * kWarps;
   static constexpr uint32_t kTileBytes = 18 * D;
-  // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (two CTAs an SM: 150 KB), and room for the warp's part of the join.
+  // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (16 warps: 150 KB), and room for the warp's part of the join.
   static constexpr uint32_t kStages = D == 64 ? 4 : 2;
   static constexpr uint32_t kRing = kStages * 2 * kTileBytes;
   static constexpr uint32_t kRowFloats = D + 8;                             // of a part: rows shifted by 8 banks
@@ -200,7 +206,6 @@ struct Shape {
   // A warp's memory: the ring, whose place its last part takes, and the part of the segment that its stretch begins inside of.
   static constexpr uint32_t kPerWarp = kRingSpace + (kPart + 127) / 128 * 128;
   static constexpr uint32_t kSmem = kWarps * kPerWarp;
-  static constexpr int kCtas = D <= 128 && NT == 1 ? 2 : 1;
 };
 
 __device__ __forceinline__ uint64_t divide(uint64_t a, uint32_t b) {      // nearly always in 32 bits, a fraction of the latency
@@ -219,9 +224,10 @@ __device__ __forceinline__ bool saw(float m, float l) { return m > kNoMax || !(l
 __device__ __forceinline__ float log_sum(float m, float l) { return saw(m, l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
 
 template <int TYPE, int D, int NT>
-__global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_attend_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_attend_kernel(const __grid_constant__ AttendParams p) {
   using S = Shape<TYPE, D, NT>;
   constexpr int J = S::kGroups, R = S::kRows;
+  constexpr uint32_t kWarps = S::kWarps, kThreads = S::kThreads;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t bars[kWarps][S::kStages];
   __shared__ uint64_t scan[kWarps];
@@ -245,60 +251,71 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
   chain_wait();
 
   // ---- the warps' stretches of the line of units, and the sequences that they begin in -----------------------------------
-  uint64_t total = 0;
-  for (uint32_t b = tid; b < p.c.sequences; b += kThreads) total += sequence_at<R>(p, b).units;
+  uint64_t u0, u1, per_cta = 0, seq_base = 0;
+  Sequence seq{};
+  if (p.direct) {                                           // segment blockIdx.x, of sequences with as many segments each
+    const uint32_t row_tiles = (p.group + R - 1) / R, each = p.c.heads * row_tiles;
+    seq = sequence_at<R>(p, blockIdx.x / each);
+    const uint32_t stretch = (seq.tiles + kWarps - 1) / kWarps;
+    const uint64_t begin = (uint64_t)(blockIdx.x % each) * (seq.tiles + kSegmentCost) + kSegmentCost;
+    u0 = begin + warp * stretch;
+    u1 = begin + (warp * stretch + stretch < seq.tiles ? warp * stretch + stretch : seq.tiles);
+  } else {
+    uint64_t total = 0;
+    for (uint32_t b = tid; b < p.c.sequences; b += kThreads) total += sequence_at<R>(p, b).units;
 #pragma unroll
-  for (int m = 16; m; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
-  if (lane == 0) scan[warp] = total;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (uint32_t w = 0; w < kWarps; ++w) total += scan[w];
-  uint64_t stretch = divide(total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
-  if (stretch < kLeastStretch) stretch = kLeastStretch;
-  const uint64_t cta0 = (uint64_t)blockIdx.x * kWarps * stretch;
-  if (cta0 >= total) {
-    if (tid == 0) p.join[blockIdx.x].parts = 0;
-    return;
-  }
-  uint64_t base = 0;
-  const uint64_t last_start = cta0 + (kWarps - 1) * stretch < total ? cta0 + (kWarps - 1) * stretch : total - 1;
-  for (uint32_t b0 = 0;; b0 += kThreads) {                 // ends: last_start < total
-    const uint64_t mine = b0 + tid < p.c.sequences ? sequence_at<R>(p, b0 + tid).units : 0;
-    uint64_t sum = mine;
-#pragma unroll
-    for (int m = 1; m < 32; m <<= 1) {
-      const uint64_t up = __shfl_up_sync(0xffffffffu, sum, m);
-      if (lane >= (uint32_t)m) sum += up;
-    }
+    for (int m = 16; m; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
+    if (lane == 0) scan[warp] = total;
     __syncthreads();
-    if (lane == 31) scan[warp] = sum;
-    __syncthreads();
-    uint64_t here = base, all = 0;
+    total = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) {
-      if (w < warp) here += scan[w];
-      all += scan[w];
+    for (uint32_t w = 0; w < kWarps; ++w) total += scan[w];
+    per_cta = divide(total + gridDim.x - 1, gridDim.x);
+    if (per_cta < kLeastCta) per_cta = kLeastCta;
+    uint64_t stretch = (per_cta + kWarps - 1) / kWarps;
+    if (stretch < kLeastStretch) stretch = kLeastStretch;
+    const uint64_t cta0 = blockIdx.x * per_cta, cta1 = cta0 + per_cta < total ? cta0 + per_cta : total;
+    if (cta0 >= total) {
+      if (tid == 0) p.join[blockIdx.x].parts = 0;
+      return;
     }
-    here += sum - mine;
-    if (mine && here < cta0 + kWarps * stretch && here + mine > cta0) {
+    uint64_t base = 0;
+    for (uint32_t b0 = 0;; b0 += kThreads) {                 // ends: cta1 <= total
+      const uint64_t mine = b0 + tid < p.c.sequences ? sequence_at<R>(p, b0 + tid).units : 0;
+      uint64_t sum = mine;
+#pragma unroll
+      for (int m = 1; m < 32; m <<= 1) {
+        const uint64_t up = __shfl_up_sync(0xffffffffu, sum, m);
+        if (lane >= (uint32_t)m) sum += up;
+      }
+      __syncthreads();
+      if (lane == 31) scan[warp] = sum;
+      __syncthreads();
+      uint64_t here = base, all = 0;
 #pragma unroll
       for (uint32_t w = 0; w < kWarps; ++w) {
-        const uint64_t at = cta0 + w * stretch;
-        if (here <= at && at < here + mine) { found_base[w] = here; found_b[w] = b0 + tid; }
+        if (w < warp) here += scan[w];
+        all += scan[w];
       }
+      here += sum - mine;
+      if (mine && here < cta1 && here + mine > cta0) {
+#pragma unroll
+        for (uint32_t w = 0; w < kWarps; ++w) {
+          const uint64_t at = cta0 + w * stretch;
+          if (here <= at && at < here + mine) { found_base[w] = here; found_b[w] = b0 + tid; }
+        }
+      }
+      base += all;
+      if (base >= cta1) break;
     }
-    base += all;
-    if (base > last_start) break;
-  }
-  __syncthreads();
+    __syncthreads();
 
-  const uint64_t u0 = cta0 + warp * stretch, u1 = u0 + stretch < total ? u0 + stretch : total;
-  Sequence seq{};
-  uint64_t seq_base = 0;
-  if (u0 < u1) {
-    seq = sequence_at<R>(p, found_b[warp]);
-    seq_base = found_base[warp];
+    u0 = cta0 + warp * stretch;
+    u1 = u0 + stretch < cta1 ? u0 + stretch : cta1;
+    if (u0 < u1) {
+      seq = sequence_at<R>(p, found_b[warp]);
+      seq_base = found_base[warp];
+    }
   }
   uint32_t stage = 0, parity = 0;                           // of the next wait; the ring goes on from segment to segment
   bool timed_out = false;
@@ -329,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     if (tile_end > tile1) tile_end = tile1;
     const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
     const uint32_t clear = see_all / kCacheTile > tile0 ? see_all / kCacheTile - tile0 : 0u;      // tiles that every row sees whole
-    const uint32_t plain = clear < count ? clear : count;
+    // (A few tiles all go the way of those that are not seen whole: the code of the other way, cold, would take longer than it saves.)
+    const uint32_t plain = count <= 4 ? 0u : clear < count ? clear : count;
     // ---- the warp's first copies: everything else of a segment's beginning goes on while they fly ---------------------------
     // Lane l knows where pairs l, l + 32, ... of the warp's tiles lie, and starts their copies.
     const uint32_t pairs = (count + 1) / 2;
@@ -690,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
     if (part_open[slot][w0] == 0) continue;
     uint32_t w1 = w0;                                       // last warp that has some of the segment
     bool goes_on = part_open[slot][w0] == 2;
-    while (goes_on && w1 + 1 < kWarps) goes_on = part_open[0][++w1] == 2;
+    while (goes_on && w1 + 1 < kWarps && part_open[0][w1 + 1]) goes_on = part_open[0][++w1] == 2;       // (the last warps may have no units)
     const Rows which = part_rows[slot][w0];
     const bool out_here = k != 0 && !goes_on;
     float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
@@ -717,7 +735,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       }
     }
     if (k == 0) {
-      const uint64_t per_cta = kWarps * stretch;
       const uint32_t first = (uint32_t)(head_begin / per_cta);
       if (first + 1 == blockIdx.x) {                        // this CTA's start is the first such boundary inside the segment
         info.rows = which;
@@ -726,15 +743,15 @@ __global__ void __launch_bounds__(kThreads, (Shape<TYPE, D, NT>::kCtas)) cache_a
       }
     }
   }
-  if (tid == 0) p.join[blockIdx.x] = info;
+  if (tid == 0 && !p.direct) p.join[blockIdx.x] = info;
 }
 
 // Parts of a segment that several CTAs hold, one row to a CTA: a warp to every eighth part, each D / 32 coordinates a lane.
 template <int TYPE, int D, int R>
-__global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_constant__ AttendParams p, uint32_t n) {
+__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const __grid_constant__ AttendParams p, uint32_t n) {
   constexpr int V = D / 32;
-  __shared__ float sum[kWarps][D];
-  __shared__ float part_m[kWarps], part_l[kWarps];
+  __shared__ float sum[kJoinWarps][D];
+  __shared__ float part_m[kJoinWarps], part_l[kJoinWarps];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, r = blockIdx.x / n, cta = blockIdx.x - r * n;
   chain_wait();
   const JoinInfo j = p.join[cta];
@@ -742,7 +759,7 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_const
   float m = kNoMax, l = 0.0f, o[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) o[i] = 0.0f;
-  for (uint32_t k = warp; k < j.parts; k += kWarps) {
+  for (uint32_t k = warp; k < j.parts; k += kJoinWarps) {
     const float* part = p.parts + ((uint64_t)(j.first + k) * 2 + (k == 0 ? 1u : 0u)) * part_floats(R, D);
     const float pm = part[R * D + r], pl = part[R * D + R + r], top = fmaxf(m, pm), f = exp2_approx(m - top), e = exp2_approx(pm - top);
     l = fmaf(e, pl, l * f);
@@ -758,10 +775,10 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const __grid_const
     m = kNoMax;
     l = 0.0f;
 #pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) m = fmaxf(m, part_m[w]);
+    for (uint32_t w = 0; w < kJoinWarps; ++w) m = fmaxf(m, part_m[w]);
     float v = 0.0f;
 #pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) {
+    for (uint32_t w = 0; w < kJoinWarps; ++w) {
       const float f = exp2_approx(part_m[w] - m);
       l = fmaf(f, part_l[w], l);
       v = fmaf(f, sum[w][threadIdx.x], v);
@@ -779,17 +796,20 @@ int launch_attend(AttendParams& p, cudaStream_t stream) {
   static KernelSite site;
   auto kern = cache_attend_kernel<TYPE, D, NT>;
   int sms = 0, occ = 0;
-  const int st = site.lookup(kern, kThreads, S::kSmem, &sms, &occ);
+  const int st = site.lookup(kern, S::kThreads, S::kSmem, &sms, &occ);
   if (st) return st;
-  uint32_t grid = (uint32_t)(sms * occ);
+  // One CTA to a segment where there is an SM for each and none is long: no line of units to find one's place on, and nothing to join behind.
+  const uint64_t segments = (uint64_t)p.c.sequences * p.c.heads * ((p.group + S::kRows - 1) / S::kRows);
+  p.direct = !p.c.starts && segments <= (uint64_t)sms && (uint64_t)p.c.table_pages * p.c.page_tiles * kCacheTile <= kDirectTokens;
+  uint32_t grid = p.direct ? (uint32_t)segments : (uint32_t)(sms * occ);
   if (grid > kMostCtas) grid = kMostCtas;
   {
     ScopedKernel sk(kKernCacheAttend, stream);
-    const cudaError_t e = launch_chained(kern, grid, kThreads, S::kSmem, stream, p);
-    if (e != cudaSuccess) return (int)e;
+    const cudaError_t e = launch_chained(kern, grid, S::kThreads, S::kSmem, stream, p);
+    if (e != cudaSuccess || p.direct) return (int)e;
   }
   ScopedKernel sk(kKernCacheJoin, stream);
-  return (int)launch_chained(cache_join_kernel<TYPE, D, S::kRows>, grid * S::kRows, kThreads, 0, stream, p, grid);
+  return (int)launch_chained(cache_join_kernel<TYPE, D, S::kRows>, grid * S::kRows, kJoinThreads, 0, stream, p, grid);
 }
 
 template <int TYPE>
