@@ -48,6 +48,10 @@ struct AttendArgs {
   uint8_t* workspace;
 };
 size_t cache_attend_workspace_bytes(uint32_t head_dim);
+// For many rows a key head (cache_attend_wide.cu): whether it takes a call, and the launch.
+bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads);
+int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const AttendArgs& args, cudaStream_t stream);
+
 int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, const AttendArgs& args, cudaStream_t stream);
 
 #ifdef __CUDACC__

@@ -193,9 +193,9 @@ __device__ __forceinline__ Sequence sequence_at(const AttendParams& p, uint32_t 
 template <int TYPE, int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT, kGroups = D / 64;
-  // A CTA fills its SM: with 128 registers a thread 16 warps, else 8. (As two CTAs of 8, the second one's warps were given 18 % less of the SM's
+  // A CTA fills its SM: with 128 registers a thread 16 warps, with 168 (D = 64, 16 rows) 12, else 8. (As two CTAs of 8, the second one's warps were given 18 % less of the SM's
   // time than the first one's, and worked on alone at the end.)
-  static constexpr uint32_t kWarps = D <= 128 && NT == 1 ? 16 : 8, kThreads = 32 * kWarps;
+  static constexpr uint32_t kWarps = D > 128 ? 8 : NT == 1 ? 16 : D == 64 ? 12 : 8, kThreads = 32 * kWarps;
   static constexpr uint32_t kTileBytes = 18 * D;
   // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (16 warps: 150 KB), and room for the warp's part of the join.
   static constexpr uint32_t kStages = D == 64 ? 4 : 2;
@@ -829,6 +829,7 @@ size_t cache_attend_workspace_bytes(uint32_t head_dim) {
 }
 
 int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, const AttendArgs& a, cudaStream_t stream) {
+  if (cache_attend_wide_takes(view, head_dim, type, a.q_heads)) return launch_cache_attend_wide(view, head_dim, a, stream);
   AttendParams p;
   p.c = view;
   p.q = static_cast<const uint16_t*>(a.q);

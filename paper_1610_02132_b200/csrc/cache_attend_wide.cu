@@ -1,0 +1,596 @@
+// Attention over the 4-bit cache for many query rows a key head (chunks of a prompt), head sizes 64 and 128, bf16.
+//
+// The mathematics is that of cache_attend.cu. Here 128 rows share what is unpacked, so the codes become numbers once, k = lo + step * c and v likewise in
+// fp16, and both products run on the fifth-generation tensor cores, sums in tensor memory:
+//   S = Q K^T   128 rows x 64 tokens,   O += P V   128 rows x head_dim
+// A CTA has 128 rows of one (sequence, key head) and goes over its tokens 64 at a time:
+//   warp 0       brings the packed tiles in by bulk copies, three steps ahead
+//   warp 1       issues the products (one thread)
+//   warps 4-7    softmax: a thread has a row of S; P goes to shared memory; O is scaled in tensor memory when a maximum rises by 2^8
+//   warps 8-15   unpack: keys as rows of a token, values turned round (rows of a coordinate), 128-byte swizzle, two buffers each
+// Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
+// likewise at 2^11; numbers 2^-28 below the largest of 64 tokens lose bits, which is less than fp32 sums lose. Roundings: k and v to 11 bits, p to 11
+// bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
+//
+// What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
+// of the special-function units, and about 1100 instructions of unpacking in 8 warps.
+#include "cache.cuh"
+
+namespace qsgd {
+
+namespace {
+
+constexpr uint32_t kRows = 128, kStep = 64, kThreads = 512, kUnpackWarps = 8, kSoftmaxWarps = 4, kRawStages = 3;
+constexpr uint32_t kPolls = 1u << 22;
+constexpr float kNoMax = -1.0e30f;
+constexpr float kLeastCap = 7.5231638452626401e-37f;       // 2^-120
+
+struct WideParams {
+  CacheView c;
+  const uint16_t* q;
+  uint16_t* out;
+  uint64_t q_token, q_head, out_token, out_head;
+  float* lse;
+  uint32_t q_heads, group;
+  float scale_log2;
+};
+
+template <int D>
+struct Shape {
+  static constexpr int kGroups = D / 64;
+  static constexpr uint32_t kTile = 18 * D;                // 16 packed tokens
+  static constexpr uint32_t kRaw = 4 * kTile;
+  static constexpr uint32_t kQ = kRows * D * 2, kK = kStep * D * 2, kV = D * kStep * 2, kP = kRows * kStep * 2;
+  static constexpr uint32_t kAtK = kQ, kAtV = kAtK + 2 * kK, kAtP = kAtV + 2 * kV, kAtRaw = kAtP + kP;
+  static constexpr uint32_t kSmem = kAtRaw + kRawStages * kRaw + 1024;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// False when the wait ran out or another role's has.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+  for (uint32_t i = 0; i < kPolls; ++i) {
+    if (mbar_try(bar, parity)) return true;
+    if ((i & 63u) == 63u && *given_up) return false;
+  }
+  *given_up = 1;
+  return false;
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Rows of 128 bytes, 128-byte swizzle: 8 rows are 1024 bytes apart.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
+  return ((uint64_t)0x40004040u << 32) | (1u << 16) | ((addr >> 4) & 0x3fffu);
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+               "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t at, float* v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+      "%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const float* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+      "%27,%28,%29,%30,%31,%32};" ::"r"(at),
+      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
+      "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])),
+      "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])), "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])),
+      "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15])), "r"(__float_as_uint(v[16])), "r"(__float_as_uint(v[17])),
+      "r"(__float_as_uint(v[18])), "r"(__float_as_uint(v[19])), "r"(__float_as_uint(v[20])), "r"(__float_as_uint(v[21])),
+      "r"(__float_as_uint(v[22])), "r"(__float_as_uint(v[23])), "r"(__float_as_uint(v[24])), "r"(__float_as_uint(v[25])),
+      "r"(__float_as_uint(v[26])), "r"(__float_as_uint(v[27])), "r"(__float_as_uint(v[28])), "r"(__float_as_uint(v[29])),
+      "r"(__float_as_uint(v[30])), "r"(__float_as_uint(v[31]))
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float exp2_approx(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// 2^(put - e) for a number of [2^e, 2^(e + 1)), as the exponent to build it from; 0 for zero, an infinity or what is no number.
+__device__ __forceinline__ int32_t lift(float largest, int32_t put) {
+  const int32_t e = (int32_t)(__float_as_uint(largest) >> 23) - 127;
+  if (!(largest > 0.0f) || e == 128) return 0;
+  const int32_t up = put - e;
+  return up > 120 ? 120 : up;
+}
+__device__ __forceinline__ float power2(int32_t e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+// Nibble s of either half of a word as lo + step * code.
+__device__ __forceinline__ void values_of(uint32_t w, uint32_t step, uint32_t lo, uint32_t (&v)[4]) {
+  const uint32_t u = w >> 8;
+  v[0] = fma_f16x2(sub_f16x2((w & 0x000f000fu) | 0x64006400u, 0x64006400u), step, lo);      // 1024 + c, less 1024
+  v[1] = fma_f16x2(sub_f16x2((w & 0x00f000f0u) | 0x54005400u, 0x54005400u), step, lo);      // 64 + c, less 64
+  v[2] = fma_f16x2(sub_f16x2((u & 0x000f000fu) | 0x64006400u, 0x64006400u), step, lo);
+  v[3] = fma_f16x2(sub_f16x2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u), step, lo);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __grid_constant__ WideParams p) {
+  using S = Shape<D>;
+  constexpr int J = S::kGroups;
+  constexpr int TYPE = QSGD_TYPE_BF16;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bars[2 * kRawStages + 15];
+  __shared__ uint64_t scan[kThreads / 32];
+  __shared__ uint64_t found_base;
+  __shared__ uint32_t found_b, tmem_base, given_up;
+  __shared__ float key_back[4], value_size[4];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
+  __shared__ uint8_t poison[2][kStep];                     // groups of a token's values that hold what is no number
+  __shared__ uint32_t poisoned[2];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* const mem = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bar0 = smem_u32(bars);
+  const uint32_t raw_full = bar0, raw_empty = raw_full + 8 * kRawStages, k_full = raw_empty + 8 * kRawStages, k_empty = k_full + 16,
+                 v_full = k_empty + 16, v_empty = v_full + 16, s_full = v_empty + 16, s_empty = s_full + 16, p_full = s_empty + 16, pv = p_full + 8,
+                 q_full = pv + 8;
+  if (tid == 0) {
+    for (uint32_t s = 0; s < kRawStages; ++s) { mbar_init(raw_full + 8 * s, 1); mbar_init(raw_empty + 8 * s, kUnpackWarps); }
+    for (uint32_t s = 0; s < 2; ++s) {
+      mbar_init(k_full + 8 * s, kUnpackWarps); mbar_init(k_empty + 8 * s, 1);
+      mbar_init(v_full + 8 * s, kUnpackWarps); mbar_init(v_empty + 8 * s, 1);
+      mbar_init(s_full + 8 * s, 1); mbar_init(s_empty + 8 * s, kSoftmaxWarps);
+    }
+    mbar_init(p_full, kSoftmaxWarps);
+    mbar_init(pv, 1);                                       // a product P V is done
+    mbar_init(q_full, kSoftmaxWarps);
+    given_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" ::"r"(smem_u32(&tmem_base)) : "memory");
+  chain_wait();
+
+  // ---- which rows of which sequence -----------------------------------------------------------------------------------
+  const uint32_t item = blockIdx.x;
+  uint64_t before = 0;
+  bool found = false;
+  auto items_of = [&](uint32_t b, SequenceRows* s) -> uint32_t {
+    bool bad;
+    *s = rows_of(p.c, b, &bad);
+    if (bad) atomicOr(p.c.status, QSGD_DEV_PAGE);
+    return p.c.heads * ((s->n * p.group + kRows - 1) / kRows);
+  };
+  for (uint32_t b0 = 0; b0 < p.c.sequences && !found; b0 += kThreads) {
+    SequenceRows s;
+    const uint32_t mine = b0 + tid < p.c.sequences ? items_of(b0 + tid, &s) : 0u;
+    uint64_t sum = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const uint64_t up = __shfl_up_sync(0xffffffffu, sum, m);
+      if (lane >= (uint32_t)m) sum += up;
+    }
+    if (lane == 31) scan[warp] = sum;
+    __syncthreads();
+    uint64_t here = before + sum - mine, all = before;
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) here += scan[w];
+      all += scan[w];
+    }
+    if (here <= item && item < here + mine) { found_base = here; found_b = b0 + tid; }
+    found = item < all;
+    before = all;
+    __syncthreads();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_base, tmem_o = tmem + 2 * kStep;
+  uint32_t steps = 0, see_any = 0, head = 0, row0 = 0, rows = 0;
+  SequenceRows seq{};
+  if (found) {
+    bool bad;
+    seq = rows_of(p.c, found_b, &bad);
+    const uint32_t row_tiles = (seq.n * p.group + kRows - 1) / kRows, at = (uint32_t)(item - found_base);
+    head = at / row_tiles;
+    row0 = (at - head * row_tiles) * kRows;
+    rows = seq.n * p.group - row0 < kRows ? seq.n * p.group - row0 : kRows;
+    const int64_t any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
+    see_any = any > 0 ? (uint32_t)any : 0u;
+    steps = (see_any + kStep - 1) / kStep;
+  }
+
+  if (warp == 0) {                                          // ---- packed tiles in -------------------------------------------------
+    const uint32_t tiles = (see_any + kCacheTile - 1) / kCacheTile;
+    auto look_up = [&](uint32_t tile) -> const uint8_t* {   // by lanes 0 to 3
+      if (lane >= 4 || tile >= tiles) return nullptr;
+      const uint32_t page = tile / p.c.page_tiles;
+      int32_t at = __ldg(p.c.table + (uint64_t)found_b * p.c.table_stride + page);
+      if (at < 0 || (uint32_t)at >= p.c.n_pages) { atomicOr(p.c.status, QSGD_DEV_PAGE); at = 0; }
+      return p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride + (uint64_t)(tile - page * p.c.page_tiles) * S::kTile;
+    };
+    const uint8_t* next = look_up(lane);
+    uint32_t i = 0;
+    for (; i < steps; ++i) {
+      const uint8_t* const src = next;
+      next = look_up(4 * (i + 1) + lane);
+      const uint32_t s = i % kRawStages, round = i / kRawStages;
+      const bool fine = i < kRawStages || mbar_wait(raw_empty + 8 * s, (round - 1) & 1u, &given_up);
+      if (!__all_sync(0xffffffffu, fine)) break;
+      const uint32_t have = tiles - 4 * i < 4 ? tiles - 4 * i : 4u;
+      if (lane == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(raw_full + 8 * s), "r"(have * S::kTile) : "memory");
+      __syncwarp();
+      if (src)
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                         base + S::kAtRaw + s * S::kRaw + lane * S::kTile), "l"(src), "r"(S::kTile), "r"(raw_full + 8 * s) : "memory");
+    }
+    // After a wait that ran out: what is in flight lands before the CTA's shared memory goes away.
+    for (uint32_t back = 1; i < steps && back <= kRawStages && back <= i; ++back) {
+      const uint32_t fill = i - back;
+      for (uint32_t t = 0; t < kPolls && !mbar_try(raw_full + 8 * (fill % kRawStages), (fill / kRawStages) & 1u); ++t) {}
+    }
+  } else if (warp == 1) {                                   // ---- the products ------------------------------------------------------
+    if (lane == 0 && steps) {
+      constexpr uint32_t idesc_s = (1u << 4) | ((kStep >> 3) << 17) | ((kRows >> 4) << 24);        // fp32 += fp16 * fp16
+      constexpr uint32_t idesc_o = (1u << 4) | ((D >> 3) << 17) | ((kRows >> 4) << 24);
+      bool fine = mbar_wait(q_full, 0, &given_up);
+      uint32_t done = 0;                                    // products P V issued
+      auto product_pv = [&](uint32_t i) {
+        const uint32_t b = i & 1u;
+        if (!mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) || !mbar_wait(p_full, i & 1u, &given_up)) { fine = false; return; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t pa = tile_desc(base + S::kAtP), vb = tile_desc(base + S::kAtV + b * S::kV);
+#pragma unroll
+        for (uint32_t x = 0; x < kStep / 16; ++x) mma_f16(tmem_o, pa + 2 * x, vb + 2 * x, idesc_o, i != 0 || x != 0);
+        tc_commit(v_empty + 8 * b);
+        tc_commit(pv);
+        ++done;
+      };
+      uint32_t i = 0;
+      for (; i < steps && fine; ++i) {
+        const uint32_t b = i & 1u;
+        if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, &given_up) ||
+            (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) { fine = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (uint32_t x = 0; x < D / 16; ++x)
+          mma_f16(tmem + b * kStep, tile_desc(base + (x / 4) * (kRows * 128)) + 2 * (x % 4),
+                  tile_desc(base + S::kAtK + b * S::kK + (x / 4) * (kStep * 128)) + 2 * (x % 4), idesc_s, x != 0);
+        tc_commit(k_empty + 8 * b);
+        tc_commit(s_full + 8 * b);
+        if (i) product_pv(i - 1);
+      }
+      if (fine) product_pv(steps - 1);
+      if (!fine && i) {                                     // products in flight are done before tensor memory is freed
+        for (uint32_t t = 0; t < kPolls && !mbar_try(k_empty + 8 * ((i - 1) & 1u), ((i - 1) >> 1) & 1u); ++t) {}
+        for (uint32_t t = 0; done && t < kPolls && !mbar_try(pv, (done - 1) & 1u); ++t) {}
+      }
+    }
+  } else if (warp >= 8) {                                   // ---- unpacking ---------------------------------------------------------
+    const uint32_t w = warp - 8, ut = tid - 256;
+    for (uint32_t i = 0; i < steps; ++i) {
+      const uint32_t b = i & 1u, s = i % kRawStages;
+      const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;     // tokens of the step that some row sees
+      bool fine = mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, &given_up);
+      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
+      if (!__all_sync(0xffffffffu, fine)) break;
+      const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw;
+      auto pair_at = [&](uint32_t token, int j, bool value) -> uint32_t {
+        return *reinterpret_cast<const uint32_t*>(raw + (token >> 4) * S::kTile + (value ? 17 : 8) * D + ((token & 15u) * J + j) * 4);
+      };
+      // The largest numbers of the keys and of the values, over the tokens that are there; every warp finds them by itself.
+      float largest_k = 0.0f, largest_v = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t token = lane + 32 * x;
+        if (token < have) {
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const uint32_t a = pair_at(token, j, false), v = pair_at(token, j, true);
+            const float lo = from_bits16<TYPE>(a & 0xffffu), lov = from_bits16<TYPE>(v & 0xffffu);
+            largest_k = fmaxf(largest_k, fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(a >> 16), lo))));
+            largest_v = fmaxf(largest_v, fmaxf(fabsf(lov), fabsf(fmaf(15.0f, from_bits16<TYPE>(v >> 16), lov))));
+          }
+        }
+      }
+      largest_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest_k)));
+      largest_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest_v)));
+      const int32_t up_k = lift(largest_k, 14), up_v = lift(largest_v, 14);
+      const float times_k = power2(up_k), times_v = power2(up_v);
+
+      // Keys: a thread has 4 J / 2 words (of 8 coordinates) of one token; a word becomes 16 bytes of the token's row, in the order that the queries
+      // have too (0 4 1 5 2 6 3 7).
+      {
+        const uint32_t token = ut & 63u, part = ut >> 6;
+        constexpr int kWords = 2 * J;                       // D / 8 words over 4 threads
+        const int j = (int)(part * kWords) / 8;
+        const uint32_t word0 = part * kWords - 8 * j;
+        const uint32_t pair = token < have ? pair_at(token, j, false) : 0u;
+        const uint32_t step = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair >> 16) * times_k, from_bits16<TYPE>(pair >> 16) * times_k);
+        const uint32_t lo = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair & 0xffffu) * times_k, from_bits16<TYPE>(pair & 0xffffu) * times_k);
+        uint32_t words[kWords];
+        const uint8_t* const src = raw + (token >> 4) * S::kTile + (j * 16 + (token & 15u)) * 32 + word0 * 4;
+#pragma unroll
+        for (int x = 0; x < kWords; x += 2) {
+          const uint2 c = token < have ? *reinterpret_cast<const uint2*>(src + 4 * x) : make_uint2(0u, 0u);
+          words[x] = c.x;
+          words[x + 1] = c.y;
+        }
+        uint8_t* const row = mem + S::kAtK + b * S::kK + j * (kStep * 128) + token * 128;
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) {
+          uint32_t v[4];
+          values_of(words[x], step, lo, v);
+          *reinterpret_cast<uint4*>(row + (((word0 + x) ^ (token & 7u)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      }
+      if (ut == 0) { key_back[i & 3u] = power2(-up_k); value_size[i & 3u] = largest_v > 0.0f ? power2(14 - up_v) : 0.0f; }
+      async_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(k_full + 8 * b);
+
+      // Values: a lane has two neighbouring tokens, a warp J words of them; a word becomes pairs in 8 coordinates' rows.
+      if (!__all_sync(0xffffffffu, i < 2 || mbar_wait(v_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) break;
+      {
+        const uint32_t token = 2 * lane;
+        const int j = (int)(w * J) / 8;
+        const uint32_t word0 = w * J - 8 * j;
+        uint32_t pair[2];
+        bool bad = false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          pair[x] = token + x < have ? pair_at(token + x, j, true) : 0u;
+          const bool nan = (pair[x] & 0x7fffu) > 0x7f80u;   // zeros here; the rows that see it are told
+          if (w == 0) {
+            uint32_t groups = nan ? 1u : 0u;
+            if (J == 2 && token + x < have && (pair_at(token + x, J - 1, true) & 0x7fffu) > 0x7f80u) groups |= 2u;
+            poison[b][token + x] = (uint8_t)groups;
+            bad |= groups != 0;
+          }
+          if (nan) pair[x] = 0;
+        }
+        if (w == 0) {
+          const bool any = __any_sync(0xffffffffu, bad);
+          if (lane == 0) poisoned[b] = any;
+        }
+        const uint32_t step = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair[0] >> 16) * times_v, from_bits16<TYPE>(pair[1] >> 16) * times_v);
+        const uint32_t lo = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair[0] & 0xffffu) * times_v, from_bits16<TYPE>(pair[1] & 0xffffu) * times_v);
+        const uint8_t* const src = raw + (token >> 4) * S::kTile + 9 * D + (j * 16 + (token & 15u)) * 32 + word0 * 4;
+        uint8_t* const to = mem + S::kAtV + b * S::kV + (lane & 3u) * 4;
+#pragma unroll
+        for (int x = 0; x < J; ++x) {
+          const uint32_t c0 = token < have ? *reinterpret_cast<const uint32_t*>(src + 4 * x) : 0u;
+          const uint32_t c1 = token + 1 < have ? *reinterpret_cast<const uint32_t*>(src + 32 + 4 * x) : 0u;
+          uint32_t v[8];
+          {
+            uint32_t a[4], c[4];
+            values_of(__byte_perm(c0, c1, 0x5410), step, lo, a);
+            values_of(__byte_perm(c0, c1, 0x7632), step, lo, c);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) { v[y] = a[y]; v[y + 4] = c[y]; }
+          }
+          const uint32_t coordinate = 64 * j + 8 * (word0 + x);
+#pragma unroll
+          for (uint32_t y = 0; y < 8; ++y)
+            *reinterpret_cast<uint32_t*>(to + (coordinate + y) * 128 + (((lane >> 2) ^ y) << 4)) = v[y];
+        }
+      }
+      async_fence();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(v_full + 8 * b); mbar_arrive(raw_empty + 8 * s); }
+    }
+  } else if (warp >= 4) {                                   // ---- softmax -----------------------------------------------------------
+    const uint32_t r = tid - 128, lanes = (32 * (warp & 3u)) << 16;
+    const bool live = r < rows;
+    const uint32_t query = (row0 + r) / p.group, hh = head * p.group + (row0 + r) - query * p.group;
+    const int64_t far = live ? seq.length - (int64_t)(seq.n - 1 - query) : 0;
+    const uint32_t see = far > 0 ? (uint32_t)far : 0u;
+    float factor = 0.0f, top = kNoMax, l = 0.0f, cap = kLeastCap;
+    uint32_t nan_groups = 0;
+    bool fine = true;
+    if (steps) {
+      // The row of q, scaled, in the keys' order of coordinates.
+      const uint16_t* const src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)hh * p.q_head;
+      float largest = 0.0f;
+      for (uint32_t c = 0; c < D / 8; ++c) {
+        const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) largest = fmaxf(largest, fmaxf(fabsf(from_bits16<TYPE>(w[y] & 0xffffu)), fabsf(from_bits16<TYPE>(w[y] >> 16))));
+      }
+      const int32_t up = lift(largest, 11);
+      const float times = power2(up);
+      factor = p.scale_log2 * power2(-up);
+      for (uint32_t c = 0; c < D / 8; ++c) {
+        const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        float v[8];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) { v[2 * y] = from_bits16<TYPE>(w[y] & 0xffffu) * times; v[2 * y + 1] = from_bits16<TYPE>(w[y] >> 16) * times; }
+        *reinterpret_cast<uint4*>(mem + (c >> 3) * (kRows * 128) + r * 128 + (((c & 7u) ^ (r & 7u)) << 4)) =
+            make_uint4(pack16<QSGD_TYPE_F16>(v[0], v[4]), pack16<QSGD_TYPE_F16>(v[1], v[5]), pack16<QSGD_TYPE_F16>(v[2], v[6]),
+                       pack16<QSGD_TYPE_F16>(v[3], v[7]));
+      }
+      async_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+    }
+    for (uint32_t i = 0; i < steps; ++i) {
+      const uint32_t b = i & 1u, first = i * kStep;
+      fine = mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, &given_up);
+      fine = __all_sync(0xffffffffu, fine);
+      if (!fine) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      float sc[kStep];
+      tmem_load32(tmem + b * kStep + lanes, sc);
+      tmem_load32(tmem + b * kStep + 32 + lanes, sc + 32);
+      const float scale = factor * key_back[i & 3u];
+      float size = value_size[i & 3u];
+      if (size == 0.0f) size = cap;                         // values that are all zero are of any size
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_empty + 8 * b);
+      float high = kNoMax;
+      if (first + kStep <= see) {
+#pragma unroll
+        for (int x = 0; x < (int)kStep; ++x) { sc[x] *= scale; high = fmaxf(high, sc[x]); }
+      } else {
+#pragma unroll
+        for (int x = 0; x < (int)kStep; ++x) {
+          sc[x] = first + x < see ? sc[x] * scale : -INFINITY;
+          high = fmaxf(high, sc[x]);
+        }
+      }
+      if (poisoned[b]) {
+        for (uint32_t x = 0; x < kStep; ++x)
+          if (first + x < see) nan_groups |= poison[b][x];
+      }
+      const bool raise = high > top + 8.0f || size > cap;
+      float f = 1.0f;
+      if (raise) {
+        const float new_top = fmaxf(top, high), new_cap = fmaxf(cap, size);
+        f = exp2_approx(top - new_top);
+        l *= f;
+        f *= cap / new_cap;
+        top = new_top;
+        cap = new_cap;
+      }
+      // P holds p * 2^7 * size / cap: at most 2^15, and 2^-14, where fp16 begins to lose bits, for p = 2^-21. (Values 2^-40 below the largest are
+      // taken for larger ones than they are rather than their p for zero.)
+      int32_t shift = (int32_t)(__float_as_uint(size) >> 23) - (int32_t)(__float_as_uint(cap) >> 23) + 7;
+      if (shift < -40) shift = -40;
+      float sum = 0.0f;
+      uint32_t packed[kStep / 2];
+      const float off = (float)shift - top;
+#pragma unroll
+      for (int x = 0; x < (int)kStep; x += 2) {
+        const float p0 = exp2_approx(sc[x] + off), p1 = exp2_approx(sc[x + 1] + off);
+        sum += p0 + p1;
+        packed[x / 2] = pack16<QSGD_TYPE_F16>(p0, p1);
+      }
+      l = fmaf(sum, power2(-shift), l);
+      // The product before this one reads P, and adds to O.
+      if (i) {
+        fine = __all_sync(0xffffffffu, mbar_wait(pv, (i - 1) & 1u, &given_up));
+        if (!fine) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll 1
+          for (uint32_t c = 0; c < D; c += 32) {
+            float o[32];
+            tmem_load32(tmem_o + c + lanes, o);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] *= f;
+            tmem_store32(tmem_o + c + lanes, o);
+          }
+        }
+      }
+#pragma unroll
+      for (uint32_t c = 0; c < kStep / 8; ++c)
+        *reinterpret_cast<uint4*>(mem + S::kAtP + r * 128 + ((c ^ (r & 7u)) << 4)) =
+            make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+      async_fence();
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full);
+    }
+    if (steps && fine) {
+      fine = __all_sync(0xffffffffu, mbar_wait(pv, (steps - 1) & 1u, &given_up));
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    if (fine && found) {
+      const uint64_t row = (uint64_t)seq.start + query;
+      uint16_t* const out = p.out + row * p.out_token + (uint64_t)hh * p.out_head;
+      const bool saw = see != 0;
+      const float back = saw ? cap * power2(-21) / l : 0.0f;                // o is sum (p 2^7 size / cap) (v 2^14 / size)
+#pragma unroll 1
+      for (uint32_t c = 0; c < D; c += 32) {
+        float o[32];
+        if (steps) tmem_load32(tmem_o + c + lanes, o);
+        if (live) {
+          const float nan = nan_groups >> (c / 64) & 1u ? NAN : 0.0f;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) o[x] = saw ? o[x] * back + nan : 0.0f;
+#pragma unroll
+          for (int x = 0; x < 32; x += 8)
+            *reinterpret_cast<uint4*>(out + c + x) =
+                make_uint4(pack16<TYPE>(o[x], o[x + 1]), pack16<TYPE>(o[x + 2], o[x + 3]), pack16<TYPE>(o[x + 4], o[x + 5]), pack16<TYPE>(o[x + 6], o[x + 7]));
+        }
+        __syncwarp();
+      }
+      if (live && p.lse) p.lse[row * p.q_heads + hh] = saw ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 0) {
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem));
+  }
+  if (tid == 0 && given_up) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+}
+
+template <int D>
+int launch_wide(const WideParams& p, cudaStream_t stream) {
+  static KernelSite site;
+  int sms = 0, occ = 0;
+  const int st = site.lookup(cache_attend_wide_kernel<D>, kThreads, Shape<D>::kSmem, &sms, &occ);
+  if (st) return st;
+  // At most this many row tiles: where the sequences' rows end inside one is known on the device only.
+  const uint64_t ctas = (uint64_t)p.c.heads * ((uint64_t)p.c.rows * p.group / kRows + p.c.sequences);
+  ScopedKernel sk(kKernCacheAttend, stream);
+  return (int)launch_chained(cache_attend_wide_kernel<D>, (uint32_t)ctas, kThreads, Shape<D>::kSmem, stream, p);
+}
+
+}  // namespace
+
+bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads) {
+  const uint64_t rows = (uint64_t)view.rows * (q_heads / view.heads);        // of a key head
+  return type == QSGD_TYPE_BF16 && (head_dim == 64 || head_dim == 128) && view.starts && rows >= 64ull * view.sequences &&
+         (rows / kRows + view.sequences) * view.heads < (1ull << 31);
+}
+
+int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const AttendArgs& a, cudaStream_t stream) {
+  WideParams p;
+  p.c = view;
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.out = static_cast<uint16_t*>(a.out);
+  p.q_token = a.q_token; p.q_head = a.q_head; p.out_token = a.out_token; p.out_head = a.out_head;
+  p.lse = a.lse;
+  p.q_heads = a.q_heads;
+  p.group = a.q_heads / view.heads;
+  p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+  return head_dim == 64 ? launch_wide<64>(p, stream) : launch_wide<128>(p, stream);
+}
+
+}  // namespace qsgd

@@ -148,11 +148,11 @@ def test_more_rows_than_tokens():
         assert torch.equal(got.cpu(), want)
 
 
-def check(out, lse, q, ks, vs, scale, lengths, runs, dtype, rows=None):
+def check(out, lse, q, ks, vs, scale, lengths, runs, dtype, wide=False):
     """Bounds. A score: 64 products summed per group in fp32, each at most |q| * (128 + 15) * step (less with centred codes): 68 roundings
     or truncations of 2^-23 of sum |q| * 143 * step, which also covers 2^-17 * 2^-11 of the largest |q| for numbers of q that fp16 does not hold
     exactly, and a few of 2^-22 of the score; p then differs by twice that and by 2^-19 for its exponential and the sums. p * step is rounded to
-    fp16, half a step of 2^-11 (for an fp16 output the rest follows: 2^-22), and multiplied by |c - 8| <= 8. The output adds half a step of its type."""
+    fp16, half a step of 2^-11 (for an fp16 output the rest follows: 2^-22), and multiplied by |c - 8| <= 8. The output adds half a step of its type. wide: keys, values and p are rounded to fp16 instead, half a step of 2^-11 of each."""
     at, worst, num, den = 0, 0.0, 0.0, 0.0
     for b, (n, r) in enumerate(zip(lengths, runs)):
         if r == 0:
@@ -166,13 +166,15 @@ def check(out, lse, q, ks, vs, scale, lengths, runs, dtype, rows=None):
             group = qq.shape[1] // step.shape[0]
             asum = qq.double().abs().unflatten(-1, (-1, 64)).sum(-1)                                  # [row, head, group]
             reach = (k.abs().amax(0).repeat_interleave(group, 0)[None] * qq.double().abs()).sum(-1)   # [row, head]: of a score
-            err = abs(scale) * ((asum * step.repeat_interleave(group, 0)[None]).sum(-1) * 143 * 68 * 2.0 ** -23 + reach * 2.0 ** -20)
+            err = abs(scale) * ((asum * step.repeat_interleave(group, 0)[None]).sum(-1) * 143 * 68 * 2.0 ** -23 + reach * (2.0 ** -11 if wide else 2.0 ** -20))
         else:
             err = torch.zeros(r, qq.shape[1], dtype=torch.float64)
         y = vs[b].double().unflatten(-1, (-1, 64)) if n else torch.zeros(1, qq.shape[1], qq.shape[2] // 64, 64, dtype=torch.float64)
-        wide = ((y.amax(-1) - y.amin(-1)) / 15).amax(0) * 1.01                                        # [kv head, group]
-        wide = wide.repeat_interleave(qq.shape[1] // wide.shape[0], 0).repeat_interleave(64, 1)[None]
-        rounded = (2.0 ** -11 if dtype == BF16 else 2.0 ** -22) * 8 * wide
+        width = ((y.amax(-1) - y.amin(-1)) / 15).amax(0) * 1.01                                       # [kv head, group]
+        width = width.repeat_interleave(qq.shape[1] // width.shape[0], 0).repeat_interleave(64, 1)[None]
+        rounded = (2.0 ** -11 if dtype == BF16 else 2.0 ** -22) * 8 * width
+        if wide and n:
+            rounded = 2.0 ** -11 * (v.abs().amax(0).repeat_interleave(qq.shape[1] // v.shape[1], 0)[None] + mean)
         tol = F.HALF_STEP[dtype] * ref.abs() + (2 * err[..., None] + 2.0 ** -19) * mean + rounded + 1e-7
         got, got_lse = out[at: at + r].cpu().double(), lse[at: at + r].cpu().double()
         assert bool(((got - ref).abs() <= tol).all()), ((got - ref).abs() / tol).max()
@@ -218,6 +220,35 @@ def test_attend_runs(dtype, dim, heads, group, lengths, runs):
     assert bool((out[sum(runs):] == 42).all()) and bool((lse[sum(runs):] == 42).all())
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads, group, page, lengths, runs", [(1, 1, 16, [64], [64]), (1, 1, 16, [300], [129]), (2, 4, 64, [200, 65, 130], [70, 65, 33]),
+                                                               (1, 8, 16, [5, 700, 0], [40, 33, 7]), (2, 3, 32, [1000, 63], [90, 1]), (1, 2, 48, [64, 128, 192], [32, 64, 96]),
+                                                               (1, 12, 16, [17, 16, 2000], [17, 1, 20]), (4, 4, 128, [513], [257])])
+def test_attend_chunks(dim, heads, group, page, lengths, runs):
+    """Runs that are long enough for tiles of 128 rows; more queries than tokens among them."""
+    f = Filled(lengths, page, heads, dim, BF16).write_all()
+    assert sum(runs) * group >= 64 * len(runs)
+    q, out, lse = run_attend(f, heads * group, runs, BF16, rows=sum(runs) + 2)
+    check(out, lse, q, f.k, f.v, 1 / math.sqrt(dim), lengths, runs, BF16, wide=True)
+    assert bool((out[sum(runs):] == 42).all()) and bool((lse[sum(runs):] == 42).all())
+
+
+@pytest.mark.parametrize("size_k, size_v", [(1e30, 1e30), (1e-30, 1e-36), (1.0, 3e37), (1e4, 1e-4)])
+def test_attend_chunks_of_all_sizes(size_k, size_v):
+    """bf16 numbers far outside fp16's range, and tokens of very different sizes side by side."""
+    f = Filled([400], 16, 1, 128, BF16)
+    sizes = torch.ones(400)
+    sizes[100:200] = 1e-4
+    f.k[0] = (f.k[0].float() * size_k * sizes[:, None, None]).to(BF16)
+    f.v[0] = (f.v[0].float() * size_v * sizes.flip(0)[:, None, None]).to(BF16)
+    f.write_all()
+    q, out, lse = run_attend(f, 2, [100], BF16, scale=0.1 / size_k if size_k < 1e20 else 0.0)
+    ref, ref_lse, mean = F.attend(q.cpu(), F.held_value(f.k[0]), F.held_value(f.v[0]), 0.1 / size_k if size_k < 1e20 else 0.0, 400, 100)
+    err = 0.1 * q.cpu().double().abs().sum(-1, keepdim=True) * 8 * 2.0 ** -11 if size_k < 1e20 else 0.0     # |k| below 8 sizes
+    tol = F.HALF_STEP[BF16] * ref.abs() + (2 * err + 2.0 ** -10) * mean + 2.0 ** -11 * f.v[0].double().abs().max()
+    assert bool(((out.cpu().double() - ref).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 @pytest.mark.parametrize("heads, group, dim, lengths", [(2, 4, 128, [20011, 3]), (1, 1, 64, [9000]), (1, 8, 256, [5000, 4999, 1])])
 def test_attend_long(dtype, heads, group, dim, lengths):
@@ -257,18 +288,18 @@ def test_attend_strided_and_without_lse():
     check(whole, lse, wide[:, :4], f.k, f.v, 1 / math.sqrt(128), [90, 40], [1, 1], BF16)
 
 
-def test_poisoned_tokens():
+@pytest.mark.parametrize("n, dim", [(40, 128), (100, 128), (100, 64)])
+def test_poisoned_tokens(n, dim):
     """A key that is not finite makes the rows that see it NaN and no others; a value that is not finite, its group of coordinates."""
-    f = Filled([40], 16, 1, 128, BF16)
+    f = Filled([n], 16, 1, dim, BF16)
     f.k[0][30, 0, 5] = math.inf
-    f.v[0][20, 0, 70] = math.nan
+    f.v[0][20, 0, dim - 58] = math.nan
     f.write_all()
-    q, out, lse = run_attend(f, 1, [40], BF16)
+    q, out, lse = run_attend(f, 1, [n], BF16)
     nan = out.isnan()[:, 0]
-    assert bool(nan[30:].all()) and not bool(nan[:20].any()) and not bool(nan[20:30, :64].any()) and bool(nan[20:30, 64:].all())
-    assert torch.equal(lse.isnan()[:, 0], torch.arange(40).cuda() >= 30)
-    clean = [f.k[0].clone()], [f.v[0].clone()]
-    check(out[:20], lse[:20], q[:20], [clean[0][0][:20]], [clean[1][0][:20]], 1 / math.sqrt(128), [20], [20], BF16)
+    assert bool(nan[30:].all()) and not bool(nan[:20].any()) and not bool(nan[20:30, : dim - 64].any()) and bool(nan[20:30, dim - 64:].all())
+    assert torch.equal(lse.isnan()[:, 0], torch.arange(n).cuda() >= 30)
+    check(out[:20], lse[:20], q[:20], [f.k[0][:20]], [f.v[0][:20]], 1 / math.sqrt(dim), [20], [20], BF16, wide=n >= 64)
 
 
 @pytest.mark.parametrize("what", ["page below", "page above", "length", "negative length", "starts"])
