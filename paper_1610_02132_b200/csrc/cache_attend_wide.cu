@@ -6,8 +6,9 @@
 // A CTA has 128 rows of one (sequence, key head) and goes over its tokens 64 at a time:
 //   warp 0       brings the packed tiles in by bulk copies, three steps ahead
 //   warp 1       issues the products (one thread)
-//   warps 4-7    softmax: a thread has a row of S; P goes to shared memory; O is scaled in tensor memory when a maximum rises by 2^8
-//   warps 8-15   unpack: keys as rows of a token, values turned round (rows of a coordinate), 128-byte swizzle, two buffers each
+//   warps 2, 3   the (lo, step) pairs of the keys, of the values: their largest number, and the pairs in fp16
+//   warps 4-11   softmax: two threads to a row of S, 32 tokens each; P goes to shared memory; O is scaled in tensor memory when a maximum rises by 2^8
+//   warps 12-19  unpack: keys as rows of a token, values turned round (rows of a coordinate), 128-byte swizzle, two buffers each
 // Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
 // likewise at 2^11; numbers 2^-28 below the largest of 64 tokens lose bits, which is less than fp32 sums lose. Roundings: k and v to 11 bits, p to 11
 // bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
@@ -20,7 +21,7 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kRows = 128, kStep = 64, kThreads = 512, kUnpackWarps = 8, kSoftmaxWarps = 4, kRawStages = 3;
+constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 3;
 constexpr uint32_t kPolls = 1u << 22;
 constexpr float kNoMax = -1.0e30f;
 constexpr float kLeastCap = 7.5231638452626401e-37f;       // 2^-120
@@ -52,14 +53,19 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// False when the wait ran out or another role's has.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+// False when the wait ran out or another role's has. (Out of line: the roles' loops share the instruction cache, and each step goes through all of
+// them; with every wait's loop in its place a step took 3000 cycles, most of them waiting for instructions.)
+__device__ __noinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+#pragma unroll 1
   for (uint32_t i = 0; i < kPolls; ++i) {
     if (mbar_try(bar, parity)) return true;
     if ((i & 63u) == 63u && *given_up) return false;
   }
   *given_up = 1;
   return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+  return mbar_try(bar, parity) || mbar_poll(bar, parity, given_up);
 }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -132,6 +138,13 @@ __device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
+// A named barrier of 64 threads; whether all of them said yes.
+__device__ __forceinline__ bool meet(uint32_t id, bool yes) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %2, 0;\n\tbar.red.and.pred p, %1, 64, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(all) : "r"(id), "r"((uint32_t)yes) : "memory");
+  return all != 0;
+}
 // Nibble s of either half of a word as lo + step * code.
 __device__ __forceinline__ void values_of(uint32_t w, uint32_t step, uint32_t lo, uint32_t (&v)[4]) {
   const uint32_t u = w >> 8;
@@ -147,20 +160,24 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   constexpr int J = S::kGroups;
   constexpr int TYPE = QSGD_TYPE_BF16;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[2 * kRawStages + 15];
+  __shared__ uint64_t bars[2 * kRawStages + 19];
   __shared__ uint64_t scan[kThreads / 32];
   __shared__ uint64_t found_base;
   __shared__ uint32_t found_b, tmem_base, given_up;
   __shared__ float key_back[4], value_size[4];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
-  __shared__ uint8_t poison[2][kStep];                     // groups of a token's values that hold what is no number
-  __shared__ uint32_t poisoned[2];
+  __shared__ uint2 key_pair[2][kStep * J];                 // (step, step), (lo, lo) in fp16
+  __shared__ uint32_t value_pair[2][kStep * J];            // step, lo
+  __shared__ float row_max[2][2][kRows], row_sum[2][kRows];
+  __shared__ uint32_t row_nan[2][kRows];
+  __shared__ uint8_t poison[4][kStep];                     // groups of a token's values that hold what is no number
+  __shared__ uint32_t poisoned[4];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const mem = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t raw_full = bar0, raw_empty = raw_full + 8 * kRawStages, k_full = raw_empty + 8 * kRawStages, k_empty = k_full + 16,
                  v_full = k_empty + 16, v_empty = v_full + 16, s_full = v_empty + 16, s_empty = s_full + 16, p_full = s_empty + 16, pv = p_full + 8,
-                 q_full = pv + 8;
+                 q_full = pv + 8, pairs_full = q_full + 8, pairs_empty = pairs_full + 16;
   if (tid == 0) {
     for (uint32_t s = 0; s < kRawStages; ++s) { mbar_init(raw_full + 8 * s, 1); mbar_init(raw_empty + 8 * s, kUnpackWarps); }
     for (uint32_t s = 0; s < 2; ++s) {
@@ -171,6 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     mbar_init(p_full, kSoftmaxWarps);
     mbar_init(pv, 1);                                       // a product P V is done
     mbar_init(q_full, kSoftmaxWarps);
+    for (uint32_t s = 0; s < 2; ++s) { mbar_init(pairs_full + 8 * s, 2); mbar_init(pairs_empty + 8 * s, kUnpackWarps); }
     given_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -199,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     if (lane == 31) scan[warp] = sum;
     __syncthreads();
     uint64_t here = before + sum - mine, all = before;
-#pragma unroll
+#pragma unroll 1
     for (uint32_t w = 0; w < kThreads / 32; ++w) {
       if (w < warp) here += scan[w];
       all += scan[w];
@@ -238,6 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     };
     const uint8_t* next = look_up(lane);
     uint32_t i = 0;
+#pragma unroll 1
     for (; i < steps; ++i) {
       const uint8_t* const src = next;
       next = look_up(4 * (i + 1) + lane);
@@ -255,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     // After a wait that ran out: what is in flight lands before the CTA's shared memory goes away.
     for (uint32_t back = 1; i < steps && back <= kRawStages && back <= i; ++back) {
       const uint32_t fill = i - back;
+#pragma unroll 1
       for (uint32_t t = 0; t < kPolls && !mbar_try(raw_full + 8 * (fill % kRawStages), (fill / kRawStages) & 1u); ++t) {}
     }
   } else if (warp == 1) {                                   // ---- the products ------------------------------------------------------
@@ -262,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       constexpr uint32_t idesc_s = (1u << 4) | ((kStep >> 3) << 17) | ((kRows >> 4) << 24);        // fp32 += fp16 * fp16
       constexpr uint32_t idesc_o = (1u << 4) | ((D >> 3) << 17) | ((kRows >> 4) << 24);
       bool fine = mbar_wait(q_full, 0, &given_up);
-      uint32_t done = 0;                                    // products P V issued
+      uint32_t issued = 0, done = 0;                        // products Q K^T, P V issued
       auto product_pv = [&](uint32_t i) {
         const uint32_t b = i & 1u;
         if (!mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) || !mbar_wait(p_full, i & 1u, &given_up)) { fine = false; return; }
@@ -275,140 +295,160 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         ++done;
       };
       uint32_t i = 0;
-      for (; i < steps && fine; ++i) {
+#pragma unroll 1
+      for (; i <= steps && fine; ++i) {                     // S of step i, then O of the step before
         const uint32_t b = i & 1u;
-        if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, &given_up) ||
-            (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) { fine = false; break; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (i < steps) {
+          if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, &given_up) ||
+              (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) { fine = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-        for (uint32_t x = 0; x < D / 16; ++x)
-          mma_f16(tmem + b * kStep, tile_desc(base + (x / 4) * (kRows * 128)) + 2 * (x % 4),
-                  tile_desc(base + S::kAtK + b * S::kK + (x / 4) * (kStep * 128)) + 2 * (x % 4), idesc_s, x != 0);
-        tc_commit(k_empty + 8 * b);
-        tc_commit(s_full + 8 * b);
+          for (uint32_t x = 0; x < D / 16; ++x)
+            mma_f16(tmem + b * kStep, tile_desc(base + (x / 4) * (kRows * 128)) + 2 * (x % 4),
+                    tile_desc(base + S::kAtK + b * S::kK + (x / 4) * (kStep * 128)) + 2 * (x % 4), idesc_s, x != 0);
+          tc_commit(k_empty + 8 * b);
+          tc_commit(s_full + 8 * b);
+          ++issued;
+        }
         if (i) product_pv(i - 1);
       }
-      if (fine) product_pv(steps - 1);
-      if (!fine && i) {                                     // products in flight are done before tensor memory is freed
-        for (uint32_t t = 0; t < kPolls && !mbar_try(k_empty + 8 * ((i - 1) & 1u), ((i - 1) >> 1) & 1u); ++t) {}
+      if (!fine && issued) {                                     // products in flight are done before tensor memory is freed
+#pragma unroll 1
+        for (uint32_t t = 0; t < kPolls && !mbar_try(k_empty + 8 * ((issued - 1) & 1u), ((issued - 1) >> 1) & 1u); ++t) {}
+#pragma unroll 1
         for (uint32_t t = 0; done && t < kPolls && !mbar_try(pv, (done - 1) & 1u); ++t) {}
       }
     }
-  } else if (warp >= 8) {                                   // ---- unpacking ---------------------------------------------------------
-    const uint32_t w = warp - 8, ut = tid - 256;
+  } else if (warp < 4) {                                    // ---- pairs: warp 2 the keys', warp 3 the values' ---------------------
+    const bool value = warp == 3;
+#pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
       const uint32_t b = i & 1u, s = i % kRawStages;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;     // tokens of the step that some row sees
       bool fine = mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, &given_up);
-      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
+      fine = fine && (i < 2 || mbar_wait(pairs_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
       if (!__all_sync(0xffffffffu, fine)) break;
-      const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw;
-      auto pair_at = [&](uint32_t token, int j, bool value) -> uint32_t {
-        return *reinterpret_cast<const uint32_t*>(raw + (token >> 4) * S::kTile + (value ? 17 : 8) * D + ((token & 15u) * J + j) * 4);
-      };
-      // The largest numbers of the keys and of the values, over the tokens that are there; every warp finds them by itself.
-      float largest_k = 0.0f, largest_v = 0.0f;
+      const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw + (value ? 17 : 8) * D;
+      float largest = 0.0f;
+      uint32_t pair[2][J];
+      bool bad = false;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const uint32_t token = lane + 32 * x;
-        if (token < have) {
+        uint32_t groups = 0;
 #pragma unroll
-          for (int j = 0; j < J; ++j) {
-            const uint32_t a = pair_at(token, j, false), v = pair_at(token, j, true);
-            const float lo = from_bits16<TYPE>(a & 0xffffu), lov = from_bits16<TYPE>(v & 0xffffu);
-            largest_k = fmaxf(largest_k, fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(a >> 16), lo))));
-            largest_v = fmaxf(largest_v, fmaxf(fabsf(lov), fabsf(fmaf(15.0f, from_bits16<TYPE>(v >> 16), lov))));
+        for (int j = 0; j < J; ++j) {
+          pair[x][j] = token < have ? *reinterpret_cast<const uint32_t*>(raw + (token >> 4) * S::kTile + ((token & 15u) * J + j) * 4) : 0u;
+          const float lo = from_bits16<TYPE>(pair[x][j] & 0xffffu);
+          largest = fmaxf(largest, fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(pair[x][j] >> 16), lo))));
+          if (value && lo != lo) {                          // no number: zeros here, and the rows that see it are told
+            groups |= 1u << j;
+            pair[x][j] = 0;
           }
         }
+        if (value) poison[i & 3u][token] = (uint8_t)groups;
+        bad |= groups != 0;
       }
-      largest_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest_k)));
-      largest_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest_v)));
-      const int32_t up_k = lift(largest_k, 14), up_v = lift(largest_v, 14);
-      const float times_k = power2(up_k), times_v = power2(up_v);
+      largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));
+      const int32_t up = lift(largest, 14);
+      const float times = power2(up);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const float lo = from_bits16<TYPE>(pair[x][j] & 0xffffu) * times, step = from_bits16<TYPE>(pair[x][j] >> 16) * times;
+          const uint32_t at = (lane + 32 * x) * J + j;
+          if (value) value_pair[b][at] = pack16<QSGD_TYPE_F16>(step, lo);
+          else key_pair[b][at] = make_uint2(pack16<QSGD_TYPE_F16>(step, step), pack16<QSGD_TYPE_F16>(lo, lo));
+        }
+      const bool any = __any_sync(0xffffffffu, bad);
+      if (lane == 0) {
+        if (value) { value_size[i & 3u] = largest > 0.0f ? power2(14 - up) : 0.0f; poisoned[i & 3u] = any; }
+        else key_back[i & 3u] = power2(-up);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(pairs_full + 8 * b);
+    }
+  } else if (warp >= 12) {                                  // ---- unpacking ---------------------------------------------------------
+    const uint32_t w = warp - 12, ut = tid - 384;
+#pragma unroll 1
+    for (uint32_t i = 0; i < steps; ++i) {
+      const uint32_t b = i & 1u, s = i % kRawStages;
+      const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;
+      bool fine = mbar_wait(pairs_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, &given_up);
+      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
+      if (!__all_sync(0xffffffffu, fine)) break;
+      const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw;
 
-      // Keys: a thread has 4 J / 2 words (of 8 coordinates) of one token; a word becomes 16 bytes of the token's row, in the order that the queries
+      // Keys: a thread has 2 J words (of 8 coordinates) of one token; a word becomes 16 bytes of the token's row, in the order that the queries
       // have too (0 4 1 5 2 6 3 7).
       {
         const uint32_t token = ut & 63u, part = ut >> 6;
         constexpr int kWords = 2 * J;                       // D / 8 words over 4 threads
         const int j = (int)(part * kWords) / 8;
         const uint32_t word0 = part * kWords - 8 * j;
-        const uint32_t pair = token < have ? pair_at(token, j, false) : 0u;
-        const uint32_t step = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair >> 16) * times_k, from_bits16<TYPE>(pair >> 16) * times_k);
-        const uint32_t lo = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair & 0xffffu) * times_k, from_bits16<TYPE>(pair & 0xffffu) * times_k);
+        const uint2 pair = key_pair[b][token * J + j];
         uint32_t words[kWords];
         const uint8_t* const src = raw + (token >> 4) * S::kTile + (j * 16 + (token & 15u)) * 32 + word0 * 4;
-#pragma unroll
-        for (int x = 0; x < kWords; x += 2) {
-          const uint2 c = token < have ? *reinterpret_cast<const uint2*>(src + 4 * x) : make_uint2(0u, 0u);
-          words[x] = c.x;
-          words[x + 1] = c.y;
+        if constexpr (J == 2) {
+          const uint4 c = token < have ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+          words[0] = c.x; words[1] = c.y; words[2] = c.z; words[3] = c.w;
+        } else {
+          const uint2 c = token < have ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
+          words[0] = c.x; words[1] = c.y;
         }
         uint8_t* const row = mem + S::kAtK + b * S::kK + j * (kStep * 128) + token * 128;
 #pragma unroll
         for (int x = 0; x < kWords; ++x) {
           uint32_t v[4];
-          values_of(words[x], step, lo, v);
+          values_of(words[x], pair.x, pair.y, v);
           *reinterpret_cast<uint4*>(row + (((word0 + x) ^ (token & 7u)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
-      if (ut == 0) { key_back[i & 3u] = power2(-up_k); value_size[i & 3u] = largest_v > 0.0f ? power2(14 - up_v) : 0.0f; }
       async_fence();
       __syncwarp();
       if (lane == 0) mbar_arrive(k_full + 8 * b);
 
-      // Values: a lane has two neighbouring tokens, a warp J words of them; a word becomes pairs in 8 coordinates' rows.
+      // Values: a lane has two tokens, 16 apart (so that a warp's reads of the codes meet fewer banks twice; P's columns are in the same order), a warp J
+      // words of them; a word becomes pairs in 8 coordinates' rows.
       if (!__all_sync(0xffffffffu, i < 2 || mbar_wait(v_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) break;
       {
-        const uint32_t token = 2 * lane;
+        const uint32_t token = (lane & 15u) + 2 * (lane & 16u);
         const int j = (int)(w * J) / 8;
         const uint32_t word0 = w * J - 8 * j;
-        uint32_t pair[2];
-        bool bad = false;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          pair[x] = token + x < have ? pair_at(token + x, j, true) : 0u;
-          const bool nan = (pair[x] & 0x7fffu) > 0x7f80u;   // zeros here; the rows that see it are told
-          if (w == 0) {
-            uint32_t groups = nan ? 1u : 0u;
-            if (J == 2 && token + x < have && (pair_at(token + x, J - 1, true) & 0x7fffu) > 0x7f80u) groups |= 2u;
-            poison[b][token + x] = (uint8_t)groups;
-            bad |= groups != 0;
-          }
-          if (nan) pair[x] = 0;
-        }
-        if (w == 0) {
-          const bool any = __any_sync(0xffffffffu, bad);
-          if (lane == 0) poisoned[b] = any;
-        }
-        const uint32_t step = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair[0] >> 16) * times_v, from_bits16<TYPE>(pair[1] >> 16) * times_v);
-        const uint32_t lo = pack16<QSGD_TYPE_F16>(from_bits16<TYPE>(pair[0] & 0xffffu) * times_v, from_bits16<TYPE>(pair[1] & 0xffffu) * times_v);
+        const uint32_t pair0 = value_pair[b][token * J + j], pair1 = value_pair[b][(token + 16) * J + j];
+        const uint32_t step = __byte_perm(pair0, pair1, 0x5410), lo = __byte_perm(pair0, pair1, 0x7632);
         const uint8_t* const src = raw + (token >> 4) * S::kTile + 9 * D + (j * 16 + (token & 15u)) * 32 + word0 * 4;
         uint8_t* const to = mem + S::kAtV + b * S::kV + (lane & 3u) * 4;
+        uint32_t c0[J], c1[J];
+        if constexpr (J == 2) {
+          const uint2 x = token < have ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
+          const uint2 y = token + 16 < have ? *reinterpret_cast<const uint2*>(src + S::kTile) : make_uint2(0u, 0u);
+          c0[0] = x.x; c0[1] = x.y; c1[0] = y.x; c1[1] = y.y;
+        } else {
+          c0[0] = token < have ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+          c1[0] = token + 16 < have ? *reinterpret_cast<const uint32_t*>(src + S::kTile) : 0u;
+        }
 #pragma unroll
         for (int x = 0; x < J; ++x) {
-          const uint32_t c0 = token < have ? *reinterpret_cast<const uint32_t*>(src + 4 * x) : 0u;
-          const uint32_t c1 = token + 1 < have ? *reinterpret_cast<const uint32_t*>(src + 32 + 4 * x) : 0u;
-          uint32_t v[8];
-          {
-            uint32_t a[4], c[4];
-            values_of(__byte_perm(c0, c1, 0x5410), step, lo, a);
-            values_of(__byte_perm(c0, c1, 0x7632), step, lo, c);
+          uint32_t front[4], behind[4];
+          values_of(__byte_perm(c0[x], c1[x], 0x5410), step, lo, front);
+          values_of(__byte_perm(c0[x], c1[x], 0x7632), step, lo, behind);
+          uint8_t* const row = to + (64 * j + 8 * (word0 + x)) * 128;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) { v[y] = a[y]; v[y + 4] = c[y]; }
+          for (uint32_t y = 0; y < 4; ++y) {
+            *reinterpret_cast<uint32_t*>(row + y * 128 + (((lane >> 2) ^ y) << 4)) = front[y];
+            *reinterpret_cast<uint32_t*>(row + (y + 4) * 128 + (((lane >> 2) ^ (y + 4)) << 4)) = behind[y];
           }
-          const uint32_t coordinate = 64 * j + 8 * (word0 + x);
-#pragma unroll
-          for (uint32_t y = 0; y < 8; ++y)
-            *reinterpret_cast<uint32_t*>(to + (coordinate + y) * 128 + (((lane >> 2) ^ y) << 4)) = v[y];
         }
       }
       async_fence();
       __syncwarp();
-      if (lane == 0) { mbar_arrive(v_full + 8 * b); mbar_arrive(raw_empty + 8 * s); }
+      if (lane == 0) { mbar_arrive(v_full + 8 * b); mbar_arrive(pairs_empty + 8 * b); mbar_arrive(raw_empty + 8 * s); }
     }
-  } else if (warp >= 4) {                                   // ---- softmax -----------------------------------------------------------
-    const uint32_t r = tid - 128, lanes = (32 * (warp & 3u)) << 16;
+  } else {                                                  // ---- softmax -----------------------------------------------------------
+    const uint32_t quarter = warp & 3u, r = 32 * quarter + lane, side = (warp - 4) >> 2, lanes = (32 * quarter) << 16;
+    const uint32_t twins = 1 + quarter;                     // named barrier of the two warps that share their rows
     const bool live = r < rows;
     const uint32_t query = (row0 + r) / p.group, hh = head * p.group + (row0 + r) - query * p.group;
     const int64_t far = live ? seq.length - (int64_t)(seq.n - 1 - query) : 0;
@@ -417,9 +457,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     uint32_t nan_groups = 0;
     bool fine = true;
     if (steps) {
-      // The row of q, scaled, in the keys' order of coordinates.
+      // Half of the row of q, scaled, in the keys' order of coordinates.
       const uint16_t* const src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)hh * p.q_head;
       float largest = 0.0f;
+#pragma unroll 2
       for (uint32_t c = 0; c < D / 8; ++c) {
         const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -429,7 +470,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       const int32_t up = lift(largest, 11);
       const float times = power2(up);
       factor = p.scale_log2 * power2(-up);
-      for (uint32_t c = 0; c < D / 8; ++c) {
+#pragma unroll 1
+      for (uint32_t c = side * (D / 16); c < (side + 1) * (D / 16); ++c) {
         const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
         float v[8];
@@ -443,36 +485,49 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
     }
+#pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
-      const uint32_t b = i & 1u, first = i * kStep;
-      fine = mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, &given_up);
+      const uint32_t b = i & 1u, first = i * kStep + 32 * side;
+      fine = fine && mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, &given_up);
       fine = __all_sync(0xffffffffu, fine);
-      if (!fine) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      float sc[kStep];
-      tmem_load32(tmem + b * kStep + lanes, sc);
-      tmem_load32(tmem + b * kStep + 32 + lanes, sc + 32);
+      float sc[32] = {};
+      if (fine) tmem_load32(tmem + b * kStep + 32 * side + lanes, sc);
       const float scale = factor * key_back[i & 3u];
       float size = value_size[i & 3u];
       if (size == 0.0f) size = cap;                         // values that are all zero are of any size
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(s_empty + 8 * b);
-      float high = kNoMax;
-      if (first + kStep <= see) {
+      if (fine && lane == 0) mbar_arrive(s_empty + 8 * b);
+      // The largest of scale * s: with a negative scale it comes from the smallest.
+      const float turn = scale < 0.0f ? -1.0f : 1.0f;
+      float high = -INFINITY;
+      if (first + 32 <= see) {
+        if (scale < 0.0f) {
 #pragma unroll
-        for (int x = 0; x < (int)kStep; ++x) { sc[x] *= scale; high = fmaxf(high, sc[x]); }
+          for (int x = 0; x < 32; ++x) sc[x] = -sc[x];
+        }
+#pragma unroll
+        for (int x = 0; x < 32; ++x) high = fmaxf(high, sc[x]);
+        high *= fabsf(scale);
       } else {
 #pragma unroll
-        for (int x = 0; x < (int)kStep; ++x) {
-          sc[x] = first + x < see ? sc[x] * scale : -INFINITY;
-          high = fmaxf(high, sc[x]);
+        for (int x = 0; x < 32; ++x) {
+          const bool seen = first + x < see;
+          sc[x] = seen ? sc[x] * turn : 0.0f;
+          high = seen ? fmaxf(high, sc[x] * fabsf(scale)) : high;
         }
       }
-      if (poisoned[b]) {
-        for (uint32_t x = 0; x < kStep; ++x)
-          if (first + x < see) nan_groups |= poison[b][x];
+      if (poisoned[i & 3u]) {
+#pragma unroll 1
+        for (uint32_t x = 0; x < 32; ++x)
+          if (first + x < see) nan_groups |= poison[i & 3u][32 * side + x];
       }
+      row_max[b][side][r] = high;                           // (two, so that a step's is read before the next but one writes it)
+      fine = meet(twins, fine);
+      if (!fine) break;                                     // both of them, after the same number of meetings
+      high = fmaxf(high, row_max[b][side ^ 1u][r]);
+      if (high == -INFINITY) high = kNoMax;                 // nothing seen
       const bool raise = high > top + 8.0f || size > cap;
       float f = 1.0f;
       if (raise) {
@@ -487,24 +542,33 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       // taken for larger ones than they are rather than their p for zero.)
       int32_t shift = (int32_t)(__float_as_uint(size) >> 23) - (int32_t)(__float_as_uint(cap) >> 23) + 7;
       if (shift < -40) shift = -40;
+      const float times = fabsf(scale), off = (float)shift - top;
       float sum = 0.0f;
-      uint32_t packed[kStep / 2];
-      const float off = (float)shift - top;
+      uint32_t packed[16];                                  // tokens x and x + 16, as the values' columns
+      if (first + 32 <= see) {
 #pragma unroll
-      for (int x = 0; x < (int)kStep; x += 2) {
-        const float p0 = exp2_approx(sc[x] + off), p1 = exp2_approx(sc[x + 1] + off);
-        sum += p0 + p1;
-        packed[x / 2] = pack16<QSGD_TYPE_F16>(p0, p1);
+        for (int x = 0; x < 16; ++x) {
+          const float p0 = exp2_approx(fmaf(sc[x], times, off)), p1 = exp2_approx(fmaf(sc[x + 16], times, off));
+          sum += p0 + p1;
+          packed[x] = pack16<QSGD_TYPE_F16>(p0, p1);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float p0 = first + x < see ? exp2_approx(fmaf(sc[x], times, off)) : 0.0f;
+          const float p1 = first + x + 16 < see ? exp2_approx(fmaf(sc[x + 16], times, off)) : 0.0f;
+          sum += p0 + p1;
+          packed[x] = pack16<QSGD_TYPE_F16>(p0, p1);
+        }
       }
       l = fmaf(sum, power2(-shift), l);
       // The product before this one reads P, and adds to O.
       if (i) {
-        fine = __all_sync(0xffffffffu, mbar_wait(pv, (i - 1) & 1u, &given_up));
-        if (!fine) break;
+        fine = __all_sync(0xffffffffu, fine && mbar_wait(pv, (i - 1) & 1u, &given_up));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (__any_sync(0xffffffffu, raise)) {
+        if (fine && __any_sync(0xffffffffu, raise)) {
 #pragma unroll 1
-          for (uint32_t c = 0; c < D; c += 32) {
+          for (uint32_t c = side * (D / 2); c < (side + 1) * (D / 2); c += 32) {
             float o[32];
             tmem_load32(tmem_o + c + lanes, o);
 #pragma unroll
@@ -513,9 +577,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
           }
         }
       }
+      if (!fine) continue;                                  // to the next meeting
 #pragma unroll
-      for (uint32_t c = 0; c < kStep / 8; ++c)
-        *reinterpret_cast<uint4*>(mem + S::kAtP + r * 128 + ((c ^ (r & 7u)) << 4)) =
+      for (uint32_t c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4*>(mem + S::kAtP + r * 128 + (((4 * side + c) ^ (r & 7u)) << 4)) =
             make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
       async_fence();
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -526,13 +591,19 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       fine = __all_sync(0xffffffffu, mbar_wait(pv, (steps - 1) & 1u, &given_up));
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
+    // The row's sum: both halves', in the same order for both.
+    row_sum[side][r] = l;
+    row_nan[side][r] = nan_groups;
+    fine = meet(twins, fine);
+    l = row_sum[0][r] + row_sum[1][r];
+    nan_groups = row_nan[0][r] | row_nan[1][r];
     if (fine && found) {
       const uint64_t row = (uint64_t)seq.start + query;
       uint16_t* const out = p.out + row * p.out_token + (uint64_t)hh * p.out_head;
       const bool saw = see != 0;
       const float back = saw ? cap * power2(-21) / l : 0.0f;                // o is sum (p 2^7 size / cap) (v 2^14 / size)
 #pragma unroll 1
-      for (uint32_t c = 0; c < D; c += 32) {
+      for (uint32_t c = side * (D / 2); c < (side + 1) * (D / 2); c += 32) {
         float o[32];
         if (steps) tmem_load32(tmem_o + c + lanes, o);
         if (live) {
@@ -546,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         }
         __syncwarp();
       }
-      if (live && p.lse) p.lse[row * p.q_heads + hh] = saw ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      if (live && side == 0 && p.lse) p.lse[row * p.q_heads + hh] = saw ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
     }
   }
   __syncwarp();
