@@ -702,8 +702,16 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
   // ---- what spans warps: joined, and written out where it ends in this CTA -------------------------------------------------
   __syncthreads();
   JoinInfo info{};
+  // Segment k: the one that begins in front of the CTA (0), or in warp k - 1. All threads take a few long ones together; of many short ones each
+  // warp takes the one that begins in it (one after another, each waiting for the latency of its reads, 15 took 3 us).
+  uint32_t segments = part_open[0][0] ? 1u : 0u;
+#pragma unroll
+  for (uint32_t w = 0; w < kWarps; ++w) segments += part_open[1][w] ? 1u : 0u;
+  const bool together = segments <= 2;
+  const uint32_t member = together ? tid : lane, members = together ? kThreads : 32u;
 #pragma unroll 1
-  for (uint32_t k = 0; k <= kWarps; ++k) {                  // parts that begin in front of the CTA, then those that begin in warp k - 1
+  for (uint32_t k = 0; k <= kWarps; ++k) {
+    if (!together && (k ? k - 1 : 0u) != warp) continue;
     const uint32_t slot = k ? 1u : 0u, w0 = k ? k - 1 : 0u;
     if (part_open[slot][w0] == 0) continue;
     uint32_t w1 = w0;                                       // last warp that has some of the segment
@@ -712,7 +720,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     const Rows which = part_rows[slot][w0];
     const bool out_here = k != 0 && !goes_on;
     float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
-    for (uint32_t i = tid; i < which.rows * (D / 4); i += kThreads) {
+    for (uint32_t i = member; i < which.rows * (D / 4); i += members) {
       const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
       float m = part_m[slot][w0][r], l = part_l[slot][w0][r];
       float4 sum = *reinterpret_cast<const float4*>(smem + w0 * S::kPerWarp + (slot ? 0 : S::kRingSpace) + (r * S::kRowFloats + 4 * d4) * 4);
