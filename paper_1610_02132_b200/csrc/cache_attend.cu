@@ -35,7 +35,9 @@ constexpr uint32_t kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
 constexpr uint32_t kLeastStretch = 2;     // units of a warp's stretch at least, and of a CTA's
 constexpr uint32_t kLeastCta = 8;
-constexpr uint32_t kDirectTokens = 2048;  // longest sequence that may be given to one CTA
+constexpr uint32_t kDirectTokens = 1024;  // of a sequence at most to a CTA of a cluster, and so many at least that it is worth having one more
+constexpr uint32_t kClusterTokens = 96;
+constexpr uint32_t kMostCluster = 8, kMostDirect = 128;     // CTAs that share a segment, and all of those
 constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kPolls = 1u << 22;
@@ -64,7 +66,7 @@ struct AttendParams {
   float* lse;
   uint32_t q_heads, group;
   float scale_log2;
-  bool direct;                            // a CTA to a segment: nothing spans CTAs
+  uint32_t direct;                        // CTAs, a cluster, to a segment (0: a line of units)
   JoinInfo* join;
   float* parts;                           // [CTA][2][rows * (dim + 2)]
 };
@@ -95,6 +97,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok) : "r"(bar), "r"(parity), "n"(kPolls) : "memory");
   return ok != 0;
+}
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// From the same place in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ float cluster_load(uint32_t at, uint32_t rank) {
+  float v;
+  asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(at), "r"(rank) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 cluster_load4(uint32_t at, uint32_t rank) {
+  float4 v;
+  asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at), "r"(rank) : "memory");
+  return v;
 }
 
 // One lane's copies of one or two tiles into a stage, two places one behind the other.
@@ -234,6 +252,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
   __shared__ uint64_t found_base[kWarps];
   __shared__ uint32_t found_b[kWarps];
   __shared__ float part_m[2][kWarps][R], part_l[2][kWarps][R];
+  __shared__ float cta_m[R], cta_l[R];                      // of the CTA's part of a segment that a cluster has
   __shared__ Rows part_rows[2][kWarps];
   __shared__ uint32_t part_open[2][kWarps];                 // 0: no part; 1: the segment ends inside the warp's stretch; 2: it goes on
   __shared__ uint64_t head_begin, head_end;                 // of the segment that the CTA's stretch begins inside of, on the line of units
@@ -247,19 +266,22 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     part_open[0][warp] = part_open[1][warp] = 0;
   }
+  if (tid < R) { cta_m[tid] = kNoMax; cta_l[tid] = 0.0f; }
   __syncwarp();
   chain_wait();
 
   // ---- the warps' stretches of the line of units, and the sequences that they begin in -----------------------------------
   uint64_t u0, u1, per_cta = 0, seq_base = 0;
   Sequence seq{};
-  if (p.direct) {                                           // segment blockIdx.x, of sequences with as many segments each
-    const uint32_t row_tiles = (p.group + R - 1) / R, each = p.c.heads * row_tiles;
-    seq = sequence_at<R>(p, blockIdx.x / each);
-    const uint32_t stretch = (seq.tiles + kWarps - 1) / kWarps;
-    const uint64_t begin = (uint64_t)(blockIdx.x % each) * (seq.tiles + kSegmentCost) + kSegmentCost;
-    u0 = begin + warp * stretch;
-    u1 = begin + (warp * stretch + stretch < seq.tiles ? warp * stretch + stretch : seq.tiles);
+  if (p.direct) {                                           // segment blockIdx.x / p.direct, of sequences with as many segments each
+    const uint32_t row_tiles = (p.group + R - 1) / R, each = p.c.heads * row_tiles, segment = blockIdx.x / p.direct, rank = blockIdx.x % p.direct;
+    seq = sequence_at<R>(p, segment / each);
+    const uint32_t mine = (seq.tiles + p.direct - 1) / p.direct, front = rank * mine, back = front + mine < seq.tiles ? front + mine : seq.tiles;
+    uint32_t stretch = (mine + kWarps - 1) / kWarps;
+    if (stretch < kLeastStretch) stretch = kLeastStretch;
+    const uint64_t begin = (uint64_t)(segment % each) * (seq.tiles + kSegmentCost) + kSegmentCost;
+    u0 = begin + front + warp * stretch;
+    u1 = u0 + stretch < begin + back ? u0 + stretch : begin + back;
   } else {
     uint64_t total = 0;
     for (uint32_t b = tid; b < p.c.sequences; b += kThreads) total += sequence_at<R>(p, b).units;
@@ -644,6 +666,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 
     // ---- the segment's rows, or a part of them -----------------------------------------------------------------------------
     const bool from_front = tile0 == 0, to_end = tile1 == seq.tiles;
+    const bool whole = from_front && to_end && p.direct <= 1;               // (a cluster's CTAs meet over every segment)
     const uint32_t slot = from_front ? 1u : 0u;             // a part without the segment's front is the stretch's first, one with it the last
     const Rows which{head, row0, rows, seq.start};
     float* const mine = reinterpret_cast<float*>(slot ? ring : ring + S::kRingSpace);
@@ -659,7 +682,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         uint64_t lse_at = 0;
         uint16_t* out = nullptr;
         float over = 0.0f;
-        if (from_front && to_end) {
+        if (whole) {
           if (r < rows) {
             out = out_row(p, which, r, &lse_at);
             if (p.lse && g == 0) p.lse[lse_at] = log_sum(top[nt][e], l);
@@ -684,14 +707,14 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
             *reinterpret_cast<uint4*>(out + 64 * j + 8 * g) =
                 make_uint4(pack16<TYPE>(v[0] * over, v[1] * over), pack16<TYPE>(v[2] * over, v[3] * over), pack16<TYPE>(v[4] * over, v[5] * over),
                            pack16<TYPE>(v[6] * over, v[7] * over));
-          } else if (!(from_front && to_end)) {
+          } else if (!whole) {
             float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
             *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
           }
         }
       }
-    if (!(from_front && to_end) && lane == 0) {
+    if (!whole && lane == 0) {
       part_rows[slot][warp] = which;
       part_open[slot][warp] = to_end ? 1u : 2u;
       if (warp == 0 && slot == 0) { head_begin = begin; head_end = begin + seq.tiles; }
@@ -718,7 +741,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     bool goes_on = part_open[slot][w0] == 2;
     while (goes_on && w1 + 1 < kWarps && part_open[0][w1 + 1]) goes_on = part_open[0][++w1] == 2;       // (the last warps may have no units)
     const Rows which = part_rows[slot][w0];
-    const bool out_here = k != 0 && !goes_on;
+    const bool out_here = p.direct <= 1 && k != 0 && !goes_on;
     float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
     for (uint32_t i = member; i < which.rows * (D / 4); i += members) {
       const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
@@ -737,12 +760,15 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         const float over = saw(m, l) ? 1.0f / l : 0.0f;
         *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
         if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
+      } else if (p.direct) {                                // where the cluster's other CTAs look for it: nobody else's part, or this very place's
+        *reinterpret_cast<float4*>(smem + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4) = sum;
+        if (d4 == 0) { cta_m[r] = m; cta_l[r] = l; }
       } else {
         *reinterpret_cast<float4*>(part + r * D + 4 * d4) = sum;
         if (d4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
       }
     }
-    if (k == 0) {
+    if (k == 0 && !p.direct) {
       const uint32_t first = (uint32_t)(head_begin / per_cta);
       if (first + 1 == blockIdx.x) {                        // this CTA's start is the first such boundary inside the segment
         info.rows = which;
@@ -752,6 +778,34 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     }
   }
   if (tid == 0 && !p.direct) p.join[blockIdx.x] = info;
+  if (p.direct <= 1) return;
+
+  // ---- a segment that a cluster has: each CTA joins the parts of some of the rows' coordinates --------------------------------
+  cluster_barrier();
+  const uint32_t segment = blockIdx.x / p.direct, rank = blockIdx.x % p.direct, row_tiles = (p.group + R - 1) / R;
+  const uint32_t b = segment / (p.c.heads * row_tiles), rest = segment % (p.c.heads * row_tiles), row0 = rest % row_tiles * R;
+  const Rows which{rest / row_tiles, row0, p.group - row0 < (uint32_t)R ? p.group - row0 : (uint32_t)R, b};
+  for (uint32_t i = tid * p.direct + rank; i < which.rows * (D / 4); i += kThreads * p.direct) {
+    const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
+    float m = kNoMax, l = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (uint32_t c = 0; c < p.direct; ++c) {
+      const float cm = cluster_load(smem_u32(&cta_m[r]), c), cl = cluster_load(smem_u32(&cta_l[r]), c);
+      if (!saw(cm, cl)) continue;                           // a CTA without tiles has no part
+      const float high = fmaxf(m, cm), f = exp2_approx(m - high), e = exp2_approx(cm - high);
+      const float4 v = cluster_load4(smem_u32(smem + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4), c);
+      m = high;
+      l = fmaf(e, cl, f * l);
+      sum.x = fmaf(e, v.x, f * sum.x); sum.y = fmaf(e, v.y, f * sum.y); sum.z = fmaf(e, v.z, f * sum.z); sum.w = fmaf(e, v.w, f * sum.w);
+    }
+    uint64_t lse_at;
+    uint16_t* const out = out_row(p, which, r, &lse_at);
+    const float over = saw(m, l) ? 1.0f / l : 0.0f;
+    *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
+    if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
+  }
+  cluster_barrier();                                        // no CTA leaves while another reads its shared memory
 }
 
 // Parts of a segment that several CTAs hold, one row to a CTA: a warp to every eighth part, each D / 32 coordinates a lane.
@@ -806,14 +860,34 @@ int launch_attend(AttendParams& p, cudaStream_t stream) {
   int sms = 0, occ = 0;
   const int st = site.lookup(kern, S::kThreads, S::kSmem, &sms, &occ);
   if (st) return st;
-  // One CTA to a segment where there is an SM for each and none is long: no line of units to find one's place on, and nothing to join behind.
+  // Few segments, none long: a cluster of CTAs to each, as many as there are SMs for. Then there is no line of units to find one's place on, and
+  // nothing to join behind.
   const uint64_t segments = (uint64_t)p.c.sequences * p.c.heads * ((p.group + S::kRows - 1) / S::kRows);
-  p.direct = !p.c.starts && segments <= (uint64_t)sms && (uint64_t)p.c.table_pages * p.c.page_tiles * kCacheTile <= kDirectTokens;
-  uint32_t grid = p.direct ? (uint32_t)segments : (uint32_t)(sms * occ);
+  const uint64_t longest = (uint64_t)p.c.table_pages * p.c.page_tiles * kCacheTile;
+  p.direct = 0;
+  if (!p.c.starts && segments <= kMostDirect) {
+    uint32_t ctas = 1;
+    while (ctas < kMostCluster && 2 * ctas * segments <= kMostDirect && 2 * ctas * kClusterTokens <= longest && (uint64_t)sms >= kMostDirect) ctas *= 2;
+    if (longest <= (uint64_t)kDirectTokens * ctas) p.direct = ctas;
+  }
+  uint32_t grid = p.direct ? (uint32_t)segments * p.direct : (uint32_t)(sms * occ);
   if (grid > kMostCtas) grid = kMostCtas;
   {
     ScopedKernel sk(kKernCacheAttend, stream);
-    const cudaError_t e = launch_chained(kern, grid, S::kThreads, S::kSmem, stream, p);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.direct ? p.direct : 1;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = launch_chaining_enabled() ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
     if (e != cudaSuccess || p.direct) return (int)e;
   }
   ScopedKernel sk(kKernCacheJoin, stream);
