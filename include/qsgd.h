@@ -215,7 +215,8 @@ int qsgd_set_launch_chaining(int on);
  * main-loop waits for later launches of this process (0 = every such wait gives up at once), so a
  * test can drive that path without any fault; qsgd_test_default_wait_polls returns the built-in
  * bound to restore. Output written by a launch that timed out is unspecified inside the message
- * buffer and never outside it.
+ * buffer and never outside it. The waits of qsgd_cache_attend, qsgd_matmul_i8 and qsgd_linear_i8 follow the same bound in the
+ * same way; what they had to write is then unspecified.
  */
 void qsgd_test_set_wait_polls(uint32_t polls);
 uint32_t qsgd_test_default_wait_polls(void);
@@ -403,7 +404,7 @@ int qsgd_cache_read(const qsgd_cache* cache, const qsgd_cache_rows* rows, void* 
  * Attention over the cache: each row is a query of q_heads heads (a multiple of the cache's heads; query
  * head h uses key head h / (q_heads / heads)) at the position of its token, and sees the tokens up to its own:
  *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q . k_t),  lse = ln sum_t p_t
- * over what the cache stands for. A row that sees no token (an empty sequence, or a row in front of the first
+ * over what the cache stands for (the sums are kept unscaled: values beyond 2^100 may give infinities). A row that sees no token (an empty sequence, or a row in front of the first
  * token) gives 0 and -infinity.
  *   q, out       [rows][q_heads][head_dim] as k and v above; scores, sums and the output are kept in fp32, p_t * step
  *                in 11 bits of fraction (22 for F16), the output is rounded to the type once. Where a sequence is split over the GPU

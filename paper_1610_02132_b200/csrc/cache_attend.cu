@@ -10,21 +10,26 @@
 //   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two that puts the largest step so far at 64
 //            (p may reach 2^8). For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
 //            For fp16 p * step goes as the sum of two fp16 numbers, since one would put as much error into the output as rounding it does.
-//            Every tile's -8 sum(p step) is added by a product with a constant operand: these sums run over the whole sequence, and without it
-//            8 sum(p step) would grow until what is left of the rounded sums, after taking it off at the end, is its error.
+//            The codes are centred here because these sums run over the whole sequence: 8 sum(p step) would grow until what is left
+//            after taking it off at the end is the error of its rounded sums.
 // A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
-// and one shift; the powers of two are undone in q, and in the output's scale at the end. (Nibbles under the exponent of 1024 or of 64 and a
-// subtraction each: 101 us against %s for 64 sequences of 100 to 8000 tokens, 8 heads of 128; bf16 operands: 143.)
+// and one shift (and an exact addition each where they are centred); the powers of two are undone in q, and in the output's scale at the end.
+// For 64 sequences of 100 to 8000 tokens, 8 heads of 128: nibbles moved into place under a bf16 exponent, p in two bf16 numbers 143 us; nibbles under the
+// exponents of 1024 and 64 and a subtraction each 101; as now, with the -8 by a product with a constant operand 87; as now 84.
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
-// What bounds it: with up to 8 rows a key head, HBM: 9/8 * head_dim bytes a token and head, each read once, against about 100
-// integer and 16 tensor instructions per 16 tokens. So everything is arranged around the stream of tiles. The tiles of all (sequence, key
+// What bounds it: HBM holds 9/8 * head_dim bytes a token and head, each read once; issue slots and the integer pipe are nearly as busy (350 warp
+// instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 62 %, integer pipe 55 %, tensor pipe 22 %). 64 sequences of
+// 16000 tokens: 241 us, 4.9 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
+// So everything is arranged around the stream of tiles. The tiles of all (sequence, key
 // head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
 // takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
 // written out by its warp; what spans warps of a CTA is joined in shared memory; what spans CTAs leaves (m, sum, o) in the workspace,
 // at most two parts a CTA, and a second kernel joins those. (With tiles dealt out to the eight warps of a CTA, which met at the end of each
-// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us: a CTA had up to 40 segments one after another.)
+// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 21: a CTA had up to 40 segments one after another.)
+// Few and short segments need no such line: a cluster of CTAs has one each and joins it over its shared memory (one user's step, 1000 tokens, with
+// the write in front of it: 13.5 us against 16).
 #include "cache.cuh"
 
 namespace qsgd {
@@ -35,12 +40,13 @@ constexpr uint32_t kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
 constexpr uint32_t kLeastStretch = 2;     // units of a warp's stretch at least, and of a CTA's
 constexpr uint32_t kLeastCta = 8;
-constexpr uint32_t kDirectTokens = 1024;  // of a sequence at most to a CTA of a cluster, and so many at least that it is worth having one more
-constexpr uint32_t kClusterTokens = 96;
+// Of a sequence at most to a CTA of a cluster: 8000 tokens take 16 us by a cluster of 8 and as long by the line. And at least, before one more is worth it:
+// 16 tokens take 7.4 us by one CTA and 9.7 by eight, 1000 take 13.5 and 10.9.
+constexpr uint32_t kDirectTokens = 1024, kClusterTokens = 96;
 constexpr uint32_t kMostCluster = 8, kMostDirect = 128;     // CTAs that share a segment, and all of those
 constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
 constexpr uint32_t kMostRowTile = 16;
-constexpr uint32_t kPolls = 1u << 22;
+constexpr uint32_t kDrainPolls = 1u << 22;   // bound of the waits for copies in flight
 constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;     // 2^-120, 2^126
 constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that differences of maxima are numbers
 
@@ -66,6 +72,7 @@ struct AttendParams {
   float* lse;
   uint32_t q_heads, group;
   float scale_log2;
+  uint32_t polls;                         // bound of the waits for tiles
   uint32_t direct;                        // CTAs, a cluster, to a segment (0: a line of units)
   JoinInfo* join;
   float* parts;                           // [CTA][2][rows * (dim + 2)]
@@ -74,18 +81,20 @@ struct AttendParams {
 __host__ __device__ constexpr size_t part_floats(uint32_t rows, uint32_t dim) { return (size_t)rows * (dim + 2); }
 
 // Token of a tile that row r (of 8) of a score tile stands for; rows 8 .. 15 are the same behind 8. Lane (g, t) of a warp reads key
-// codes of token kToken[g] and value codes of tokens kToken[2 t] and kToken[2 t + 1]: both sets of four rows of 32 bytes that go
+// codes of token token_of(g) and value codes of tokens token_of(2 t) and token_of(2 t + 1): both sets of four rows of 32 bytes that go
 // together differ modulo 4.
 __device__ __forceinline__ uint32_t token_of(uint32_t r) { return (0x57463120u >> (4 * r)) & 7u; }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// Waits for a phase, at most kPolls times as long as the hardware suspends a thread that tries; false if that was not enough.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+// Waits for a phase, `polls` times at most (0: not at all) as long as the hardware suspends a thread that tries; false if that was not enough.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t polls) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
       "mov.u32 n, 0;\n\t"
+      "setp.ne.u32 p, %3, 0;\n\t"
+      "@!p bra done;\n\t"
       "again:\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "@p bra done;\n\t"
@@ -95,10 +104,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
       "setp.ne.u32 p, n, n;\n\t"
       "done:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity), "n"(kPolls) : "memory");
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(polls) : "memory");
   return ok != 0;
 }
-
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -254,6 +262,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
   __shared__ float part_m[2][kWarps][R], part_l[2][kWarps][R];
   __shared__ float cta_m[R], cta_l[R];                      // of the CTA's part of a segment that a cluster has
   __shared__ Rows part_rows[2][kWarps];
+  __shared__ uint32_t late[kWarps];                         // a wait ran out
   __shared__ uint32_t part_open[2][kWarps];                 // 0: no part; 1: the segment ends inside the warp's stretch; 2: it goes on
   __shared__ uint64_t head_begin, head_end;                 // of the segment that the CTA's stretch begins inside of, on the line of units
 
@@ -264,7 +273,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
     for (uint32_t s = 0; s < S::kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_u32 + 8 * s) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    part_open[0][warp] = part_open[1][warp] = 0;
+    part_open[0][warp] = part_open[1][warp] = late[warp] = 0;
   }
   if (tid < R) { cta_m[tid] = kNoMax; cta_l[tid] = 0.0f; }
   __syncwarp();
@@ -340,7 +349,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     }
   }
   uint32_t stage = 0, parity = 0;                           // of the next wait; the ring goes on from segment to segment
-  bool timed_out = false;
 
 #pragma unroll 1
   for (uint64_t u = u0; u < u1;) {
@@ -372,7 +380,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     const uint32_t plain = count <= 4 ? 0u : clear < count ? clear : count;
     // ---- the warp's first copies: everything else of a segment's beginning goes on while they fly ---------------------------
     // Lane l knows where pairs l, l + 32, ... of the warp's tiles lie, and starts their copies.
-    const uint32_t pairs = (count + 1) / 2;
+    uint32_t pairs = (count + 1) / 2;
     auto look_up = [&](uint32_t i) -> const uint8_t* {
       if (i >= count) return nullptr;
       const uint32_t tile = tile0 + i, page = tile / p.c.page_tiles;
@@ -649,7 +657,12 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 
 #pragma unroll 1
     for (uint32_t i = 0; i < pairs; ++i) {
-      if (!mbar_wait(bar_u32 + 8 * stage, parity)) timed_out = true;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * stage, parity, p.polls))) {
+        // Said in the status word; the copy is waited for all the same, since it writes into the CTA's shared memory. One that does not land
+        // within the built-in bound either ends the warp's work. (A way out of the loop here would cost 100 bytes of spilled registers.)
+        late[warp] = 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * stage, parity, kDrainPolls))) pairs = 0;
+      }
       const uint32_t first = (tile0 + 2 * i) * kCacheTile;
       const uint8_t* const tiles = ring + stage * 2 * S::kTileBytes;
       // Some row does not see both tiles whole, or the second one lies behind the warp's stretch (and holds what was there before).
@@ -720,7 +733,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
       if (warp == 0 && slot == 0) { head_begin = begin; head_end = begin + seq.tiles; }
     }
   }
-  if (timed_out) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+  __syncwarp();
+  if (late[warp] && lane == 0) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
 
   // ---- what spans warps: joined, and written out where it ends in this CTA -------------------------------------------------
   __syncthreads();
@@ -921,6 +935,7 @@ int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, cons
   p.q_heads = a.q_heads;
   p.group = a.q_heads / view.heads;
   p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+  p.polls = quantize_poll_limit();
   p.join = reinterpret_cast<JoinInfo*>(a.workspace);
   p.parts = reinterpret_cast<float*>(a.workspace + kMostCtas * sizeof(JoinInfo));
   // 16 rows to a tile where a sequence has more than 8 on average: the codes are unpacked half as often.

@@ -14,7 +14,9 @@
 // bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
 //
 // What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
-// of the special-function units, and about 1100 instructions of unpacking in 8 warps.
+// of the special-function units, and about 5000 warp instructions, half of them unpacking: 2500 cycles, issue slots at half (tensor pipe 18 %). The step's roles
+// hand over eleven barriers, and their code is as large as the instruction cache: out-of-line waits alone took a step from 3000 to 2500 cycles.
+// Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 97 us, 0.32 PFLOP/s; by cache_attend.cu 204.
 #include "cache.cuh"
 
 namespace qsgd {
@@ -23,7 +25,7 @@ namespace {
 
 constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 3;
 constexpr uint32_t kMostSorted = 256;
-constexpr uint32_t kPolls = 1u << 22;
+constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 constexpr float kNoMax = -1.0e30f;
 constexpr float kLeastCap = 7.5231638452626401e-37f;       // 2^-120
 
@@ -35,6 +37,7 @@ struct WideParams {
   float* lse;
   uint32_t q_heads, group;
   float scale_log2;
+  uint32_t polls;              // bound of the roles' waits
 };
 
 template <int D>
@@ -56,17 +59,21 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 // False when the wait ran out or another role's has. (Out of line: the roles' loops share the instruction cache, and each step goes through all of
 // them; with every wait's loop in its place a step took 3000 cycles, most of them waiting for instructions.)
-__device__ __noinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
+__device__ __noinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* given_up, uint32_t polls) {
 #pragma unroll 1
-  for (uint32_t i = 0; i < kPolls; ++i) {
+  for (uint32_t i = 0; i < polls; ++i) {
     if (mbar_try(bar, parity)) return true;
     if ((i & 63u) == 63u && *given_up) return false;
   }
   *given_up = 1;
   return false;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
-  return mbar_try(bar, parity) || mbar_poll(bar, parity, given_up);
+struct Waits {
+  volatile uint32_t* given_up;
+  uint32_t polls;
+};
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {
+  return (w.polls && mbar_try(bar, parity)) || mbar_poll(bar, parity, w.given_up, w.polls);
 }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -175,6 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   __shared__ uint8_t poison[4][kStep];                     // groups of a token's values that hold what is no number
   __shared__ uint32_t poisoned[4];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+  const Waits waits{&given_up, p.polls};
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const mem = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t bar0 = smem_u32(bars);
@@ -200,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
 
   // ---- which rows of which sequence -----------------------------------------------------------------------------------
   // Items in the order of the sequences' lengths, the longest first, as long as those are few: CTAs are placed in their order, and the last ones to
-  // start should be short. (Sequences of 700 to 4096 tokens as they came: 122 us against %s.)
+  // start should be short. (Four sequences of 700 to 4096 tokens as they came: 122 us against 97.)
   const uint32_t item = blockIdx.x;
   const bool sorted = p.c.sequences <= kMostSorted;
   if (sorted) {
@@ -280,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       const uint8_t* const src = next;
       next = look_up(4 * (i + 1) + lane);
       const uint32_t s = i % kRawStages, round = i / kRawStages;
-      const bool fine = i < kRawStages || mbar_wait(raw_empty + 8 * s, (round - 1) & 1u, &given_up);
+      const bool fine = i < kRawStages || mbar_wait(raw_empty + 8 * s, (round - 1) & 1u, waits);
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint32_t have = tiles - 4 * i < 4 ? tiles - 4 * i : 4u;
       if (lane == 0)
@@ -290,21 +298,21 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                          base + S::kAtRaw + s * S::kRaw + lane * S::kTile), "l"(src), "r"(S::kTile), "r"(raw_full + 8 * s) : "memory");
     }
-    // After a wait that ran out: what is in flight lands before the CTA's shared memory goes away.
-    for (uint32_t back = 1; i < steps && back <= kRawStages && back <= i; ++back) {
+    // What is in flight lands before the CTA's shared memory goes away, whether anybody still waits for it or not.
+    for (uint32_t back = 1; back <= kRawStages && back <= i; ++back) {
       const uint32_t fill = i - back;
 #pragma unroll 1
-      for (uint32_t t = 0; t < kPolls && !mbar_try(raw_full + 8 * (fill % kRawStages), (fill / kRawStages) & 1u); ++t) {}
+      for (uint32_t t = 0; t < kDrainPolls && !mbar_try(raw_full + 8 * (fill % kRawStages), (fill / kRawStages) & 1u); ++t) {}
     }
   } else if (warp == 1) {                                   // ---- the products ------------------------------------------------------
     if (lane == 0 && steps) {
       constexpr uint32_t idesc_s = (1u << 4) | ((kStep >> 3) << 17) | ((kRows >> 4) << 24);        // fp32 += fp16 * fp16
       constexpr uint32_t idesc_o = (1u << 4) | ((D >> 3) << 17) | ((kRows >> 4) << 24);
-      bool fine = mbar_wait(q_full, 0, &given_up);
+      bool fine = mbar_wait(q_full, 0, waits);
       uint32_t issued = 0, done = 0;                        // products Q K^T, P V issued
       auto product_pv = [&](uint32_t i) {
         const uint32_t b = i & 1u;
-        if (!mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) || !mbar_wait(p_full, i & 1u, &given_up)) { fine = false; return; }
+        if (!mbar_wait(v_full + 8 * b, (i >> 1) & 1u, waits) || !mbar_wait(p_full, i & 1u, waits)) { fine = false; return; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t pa = tile_desc(base + S::kAtP), vb = tile_desc(base + S::kAtV + b * S::kV);
 #pragma unroll
@@ -318,8 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       for (; i <= steps && fine; ++i) {                     // S of step i, then O of the step before
         const uint32_t b = i & 1u;
         if (i < steps) {
-          if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, &given_up) ||
-              (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) { fine = false; break; }
+          if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, waits) ||
+              (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, waits))) { fine = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
           for (uint32_t x = 0; x < D / 16; ++x)
@@ -333,9 +341,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       }
       if (!fine && issued) {                                     // products in flight are done before tensor memory is freed
 #pragma unroll 1
-        for (uint32_t t = 0; t < kPolls && !mbar_try(k_empty + 8 * ((issued - 1) & 1u), ((issued - 1) >> 1) & 1u); ++t) {}
+        for (uint32_t t = 0; t < kDrainPolls && !mbar_try(k_empty + 8 * ((issued - 1) & 1u), ((issued - 1) >> 1) & 1u); ++t) {}
 #pragma unroll 1
-        for (uint32_t t = 0; done && t < kPolls && !mbar_try(pv, (done - 1) & 1u); ++t) {}
+        for (uint32_t t = 0; done && t < kDrainPolls && !mbar_try(pv, (done - 1) & 1u); ++t) {}
       }
     }
   } else if (warp < 4) {                                    // ---- pairs: warp 2 the keys', warp 3 the values' ---------------------
@@ -344,8 +352,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     for (uint32_t i = 0; i < steps; ++i) {
       const uint32_t b = i & 1u, s = i % kRawStages;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;     // tokens of the step that some row sees
-      bool fine = mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, &given_up);
-      fine = fine && (i < 2 || mbar_wait(pairs_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
+      bool fine = mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
+      fine = fine && (i < 2 || mbar_wait(pairs_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw + (value ? 17 : 8) * D;
       float largest = 0.0f;
@@ -394,8 +402,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     for (uint32_t i = 0; i < steps; ++i) {
       const uint32_t b = i & 1u, s = i % kRawStages;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;
-      bool fine = mbar_wait(pairs_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, &given_up);
-      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up));
+      bool fine = mbar_wait(pairs_full + 8 * b, (i >> 1) & 1u, waits) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
+      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw;
 
@@ -430,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
 
       // Values: a lane has two tokens, 16 apart (so that a warp's reads of the codes meet fewer banks twice; P's columns are in the same order), a warp J
       // words of them; a word becomes pairs in 8 coordinates' rows.
-      if (!__all_sync(0xffffffffu, i < 2 || mbar_wait(v_empty + 8 * b, ((i >> 1) - 1) & 1u, &given_up))) break;
+      if (!__all_sync(0xffffffffu, i < 2 || mbar_wait(v_empty + 8 * b, ((i >> 1) - 1) & 1u, waits))) break;
       {
         const uint32_t token = (lane & 15u) + 2 * (lane & 16u);
         const int j = (int)(w * J) / 8;
@@ -507,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
 #pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
       const uint32_t b = i & 1u, first = i * kStep + 32 * side;
-      fine = fine && mbar_wait(v_full + 8 * b, (i >> 1) & 1u, &given_up) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, &given_up);
+      fine = fine && mbar_wait(v_full + 8 * b, (i >> 1) & 1u, waits) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, waits);
       fine = __all_sync(0xffffffffu, fine);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       float sc[32] = {};
@@ -583,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       l = fmaf(sum, power2(-shift), l);
       // The product before this one reads P, and adds to O.
       if (i) {
-        fine = __all_sync(0xffffffffu, fine && mbar_wait(pv, (i - 1) & 1u, &given_up));
+        fine = __all_sync(0xffffffffu, fine && mbar_wait(pv, (i - 1) & 1u, waits));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (fine && __any_sync(0xffffffffu, raise)) {
 #pragma unroll 1
@@ -607,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       if (lane == 0) mbar_arrive(p_full);
     }
     if (steps && fine) {
-      fine = __all_sync(0xffffffffu, mbar_wait(pv, (steps - 1) & 1u, &given_up));
+      fine = __all_sync(0xffffffffu, mbar_wait(pv, (steps - 1) & 1u, waits));
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
     // The row's sum: both halves', in the same order for both.
@@ -680,6 +688,7 @@ int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const Att
   p.q_heads = a.q_heads;
   p.group = a.q_heads / view.heads;
   p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+  p.polls = quantize_poll_limit();
   return head_dim == 64 ? launch_wide<64>(p, stream) : launch_wide<128>(p, stream);
 }
 

@@ -8,9 +8,11 @@
 // Both directions move 2 * head_dim * 2 dense bytes and 9/8 * head_dim held bytes a token and head and compute little: HBM
 // bounds them, once the conversions stay off the slow conversion pipe (codes become floats, and floats codes, by adding 2^23) and nobody waits for
 // places: where a row lies in the cache takes a search in `starts` and two dependent reads, and a ninth warp looks that up for the next rows
-// of its CTA while the others move the present ones (without it 55 against %s us for 15.6 K tokens of 8 heads of 128, written and read back).
+// of its CTA while the others move the present ones.
 // Four lanes share a group (two times 16 dense bytes and two words of codes each: with eight lanes what a group takes once, its span and step,
 // was done twice as often), a warp's eight teams neighbouring rows or heads; a team goes along its row's keys, or values, head by head.
+// 65536 tokens of 8 heads of 128 read back: 60 us, 5.7 TB/s (102 with a conversion instruction a code). 15.6 K tokens written and read back: 47 us (78 at
+// first, 53 with eight lanes to a group); writing is bound by issue slots: nine operations a value.
 #include <float.h>
 
 #include "cache.cuh"

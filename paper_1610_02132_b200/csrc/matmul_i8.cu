@@ -29,7 +29,7 @@ constexpr uint32_t kRingBytes = 4 * (kBM + kMostWidth) * kBK;
 // Stages on 1024-byte boundaries. A stage holds no more rows of a than there are; the products read 128 all the same, whatever lies behind (sums of
 // rows that are not there go nowhere), so there is that much room behind the last stage.
 constexpr uint32_t kSmem = kRingBytes + kBM * kBK + 1024;
-constexpr uint32_t kPolls = 1u << 22;
+constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 // Up to here matmul_i8_few.cu: 16 rows of 16384 x 4096 take 19.0 us there and 21.6 here, 32 rows 36.5 and 16.8 (4096 x 4096: 7.9 and 16, 16 rows).
 constexpr uint32_t kFewRows = 16;
 
@@ -38,6 +38,7 @@ struct GemmParams {
   uint32_t m_tiles, n_tiles, k_steps;
   uint32_t width, stages;      // columns of a tile (a multiple of 16), stages of the ring
   uint32_t a_bytes;            // of a stage's rows of a
+  uint32_t polls;              // bound of the roles' waits
   bool vector_out;             // rows of out begin on 16-byte boundaries
 };
 
@@ -59,12 +60,17 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // False when the wait ran out or another role's has.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* given_up) {
-  for (uint32_t i = 0; i < kPolls; ++i) {
+struct Waits {
+  volatile uint32_t* given_up;
+  uint32_t polls;
+};
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < w.polls; ++i) {
     if (mbar_try(bar, parity)) return true;
-    if ((i & 63u) == 63u && *given_up) return false;
+    if ((i & 63u) == 63u && *w.given_up) return false;
   }
-  *given_up = 1;
+  *w.given_up = 1;
   return false;
 }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
@@ -148,6 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   __shared__ uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_empty[2];
   __shared__ uint32_t tmem_base, given_up;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const Waits waits{&given_up, g.polls};
   const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u, stage_bytes = g.a_bytes + g.width * kBK;
   const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), sums_full0 = smem_u32(sums_full), sums_empty0 = smem_u32(sums_empty);
   if (threadIdx.x == 0) {
@@ -173,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
         uint32_t m, n;
         tile_at(g, i, &m, &n);
         for (uint32_t k = 0; k < g.k_steps; ++k) {
-          if (r.fills >= g.stages && !mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, &given_up)) { fine = false; break; }
+          if (r.fills >= g.stages && !mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, waits)) { fine = false; break; }
           const uint32_t at = ring0 + r.stage * stage_bytes, bar = full0 + 8 * r.stage;
           mbar_expect(bar, stage_bytes);
           tma_load(at, &map_a, k * kBK, m * kBM, bar);
@@ -181,10 +188,10 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
           r.next(g.stages);
         }
       }
-      // After a wait that ran out: what is in flight lands before the CTA's shared memory goes away.
-      for (uint32_t back = 1; !fine && back <= g.stages && back <= r.fills; ++back) {
+      // What is in flight lands before the CTA's shared memory goes away, whether anybody still waits for it or not.
+      for (uint32_t back = 1; back <= g.stages && back <= r.fills; ++back) {
         const uint32_t fill = r.fills - back;
-        for (uint32_t t = 0; t < kPolls && !mbar_try(full0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
+        for (uint32_t t = 0; t < kDrainPolls && !mbar_try(full0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
       }
     }
   } else if (warp == 1) {                                   // ---- issues the products -------------------------------------------
@@ -195,10 +202,10 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
       bool fine = true;
       for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x, ++done) {
         const uint32_t half = done & 1u, use = done >> 1;
-        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, &given_up)) { fine = false; break; }
+        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, waits)) { fine = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (uint32_t k = 0; k < g.k_steps; ++k) {
-          if (!mbar_wait(full0 + 8 * r.stage, r.parity, &given_up)) { fine = false; break; }
+          if (!mbar_wait(full0 + 8 * r.stage, r.parity, waits)) { fine = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = ring0 + r.stage * stage_bytes;
           const uint64_t a = tile_desc(at), b = tile_desc(at + g.a_bytes);
@@ -212,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
       // After a wait that ran out: products in flight are done before tensor memory is freed.
       if (!fine && r.fills) {
         const uint32_t fill = r.fills - 1;
-        for (uint32_t t = 0; t < kPolls && !mbar_try(empty0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
+        for (uint32_t t = 0; t < kDrainPolls && !mbar_try(empty0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
       }
     }
   } else {                                                  // ---- takes the sums out --------------------------------------------
@@ -222,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
       uint32_t m, n;
       tile_at(g, i, &m, &n);
       const uint32_t half = done & 1u;
-      const bool fine = __all_sync(0xffffffffu, mbar_wait(sums_full0 + 8 * half, (done >> 1) & 1u, &given_up));
+      const bool fine = __all_sync(0xffffffffu, mbar_wait(sums_full0 + 8 * half, (done >> 1) & 1u, waits));
       if (!fine) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t row = m * kBM + 32 * quarter + lane;
@@ -329,6 +336,7 @@ int launch(const MatmulArgs& p, cudaStream_t stream) {
   g.k_steps = (p.k + kBK - 1) / kBK;
   g.stages = kRingBytes / (g.a_bytes + g.width * kBK);
   if (g.stages > kMostStages) g.stages = kMostStages;
+  g.polls = quantize_poll_limit();
   g.vector_out = ((reinterpret_cast<uintptr_t>(p.out) | p.out_stride * (TYPE == QSGD_TYPE_F32 ? 4 : 2)) & 15u) == 0;
   CUtensorMap a, b;
   st = make_map(&a, p.a, p.k, p.m, p.a_stride, a_rows);

@@ -231,6 +231,7 @@ struct KernelSite {
 // Test hook: bound (in polls) of the waits inside the streaming encoder's main loop.
 void set_quantize_poll_limit(uint32_t polls);
 uint32_t default_quantize_poll_limit();
+uint32_t quantize_poll_limit();          // (also of the main-loop waits of the cache's attention and the 8-bit products)
 
 // Programmatic dependent launch. Every kernel of the library is launched with programmatic stream
 // serialization, so the launch of the next kernel is prepared while the one ahead still runs and its

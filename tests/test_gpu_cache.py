@@ -201,7 +201,7 @@ def run_attend(f, q_heads, runs, dtype, seed=3, scale=None, rows=None, one_each=
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 @pytest.mark.parametrize("dim", [64, 128, 192, 256])
 @pytest.mark.parametrize("heads, group, page, lengths", [(1, 1, 16, [1]), (2, 4, 16, [16, 17, 0, 5]), (1, 8, 32, [300, 31]), (4, 3, 48, [129, 1, 64]),
-                                                         (1, 12, 16, [500])])
+                                                         (1, 12, 16, [500]), (1, 64, 16, [700, 90]), (3, 1, 256, [1000] * 3)])
 def test_attend_single_tokens(dtype, dim, heads, group, page, lengths):
     f = Filled(lengths, page, heads, dim, dtype).write_all()
     q, out, lse = run_attend(f, heads * group, [1] * len(lengths), dtype, one_each=True)
@@ -400,6 +400,30 @@ def test_a_generation_in_a_graph():
         f.fine()
         check(out, lse, q, keys, vals, 1 / math.sqrt(128), lengths, [1, 1], BF16)
         assert torch.equal(out, out2)
+
+
+@pytest.mark.parametrize("lengths, runs", [([900, 300], None), ([9000], None), ([300, 200], [100, 60])])
+def test_every_route_in_a_graph(lengths, runs):
+    """Clusters to a segment, the line of units with its second kernel, tiles of 128 rows: replayed with other queries and lengths."""
+    f = Filled(lengths, 16, 2, 128, BF16).write_all()
+    rows, starts = sum(runs or [1] * len(lengths)), starts_of(runs) if runs else None
+    q, out = torch.zeros(rows, 8, 128, dtype=BF16, device="cuda"), torch.zeros(rows, 8, 128, dtype=BF16, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 8), dtype=torch.uint8, device="cuda")
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts)
+    for seed in (1, 2, 3):
+        q.copy_(values((rows, 8, 128), BF16, seed))
+        f.len.copy_(torch.tensor([n - 7 * seed for n in lengths], dtype=torch.int32))
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        again = torch.empty_like(out)
+        Q.qsgd_cache_attend(f.cache, f.table, f.len, q, again, torch.empty_like(ws), f.status, starts=starts)
+        assert torch.equal(out, again) and bool(out.isfinite().all())
+    f.fine()
 
 
 def test_given_stream_and_repeated_calls():
