@@ -64,7 +64,8 @@ int qsgd_linear_i8(const void* x, uint64_t x_stride, int x_type, const int8_t* w
   float* scale = reinterpret_cast<float*>(codes + m * padded_cols(cols));
   const MatmulArgs args{codes, w, scale, w_scale, bias, out, padded_cols(cols), n > 1 ? w_stride : padded_cols(cols), out_stride, (uint32_t)m,
                         (uint32_t)n, cols, out_type, status_dev};
-  const bool few = !matmul_i8_many_takes(args) && m <= 64;
+  // Few rows: the product starts while the quantizing kernel still runs, and brings in w before it waits for it.
+  const bool few = m <= 128;
   const int st = launch_quantize_rows(x, m, cols, x_stride, x_type, codes, padded_cols(cols), scale, few, static_cast<cudaStream_t>(stream));
   return st ? st : launch_matmul_i8(args, few, static_cast<cudaStream_t>(stream));
 }

@@ -26,7 +26,7 @@ int launch_matmul_i8(const MatmulArgs& args, bool early, cudaStream_t stream);
 
 // For many rows (matmul_i8.cu): whether it takes a product, and the launch.
 bool matmul_i8_many_takes(const MatmulArgs& args);
-int launch_matmul_i8_many(const MatmulArgs& args, cudaStream_t stream);
+int launch_matmul_i8_many(const MatmulArgs& args, bool early, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // The sum, scaled: in fp32, in this order, rounded to the output's type once.

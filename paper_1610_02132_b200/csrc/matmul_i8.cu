@@ -39,6 +39,7 @@ struct GemmParams {
   uint32_t width, stages;      // columns of a tile (a multiple of 16), stages of the ring
   uint32_t a_bytes;            // of a stage's rows of a
   uint32_t polls;              // bound of the roles' waits
+  bool early;                  // the kernel ahead writes a and its scales only
   bool vector_out;             // rows of out begin on 16-byte boundaries
 };
 
@@ -153,6 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_empty[2];
   __shared__ uint32_t tmem_base, given_up;
+  __shared__ float b_scale[kMostWidth], bias[kMostWidth];   // of the tile that is taken out
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const Waits waits{&given_up, g.polls};
   const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u, stage_bytes = g.a_bytes + g.width * kBK;
@@ -169,22 +171,36 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-  chain_wait();
+  if (!g.early) chain_wait();
 
   const uint32_t tiles = g.m_tiles * g.n_tiles;
   if (warp == 0) {                                          // ---- fills the ring ------------------------------------------------
     if (lane == 0) {
       Ring r;
       bool fine = true;
+      // Behind the library's own quantizing kernel: the first stages' rows of b are on their way before that has written a.
+      uint32_t ahead = 0;
+      if (g.early) {
+        uint32_t m, n;
+        tile_at(g, blockIdx.x, &m, &n);
+        for (; ahead < g.stages && ahead < g.k_steps; ++ahead) {
+          const uint32_t bar = full0 + 8 * ahead;
+          mbar_expect(bar, stage_bytes);
+          tma_load(ring0 + ahead * stage_bytes + g.a_bytes, &map_b, ahead * kBK, n * g.width, bar);
+        }
+        chain_wait();
+      }
       for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x) {
         uint32_t m, n;
         tile_at(g, i, &m, &n);
         for (uint32_t k = 0; k < g.k_steps; ++k) {
           if (r.fills >= g.stages && !mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, waits)) { fine = false; break; }
           const uint32_t at = ring0 + r.stage * stage_bytes, bar = full0 + 8 * r.stage;
-          mbar_expect(bar, stage_bytes);
+          if (r.fills >= ahead) {
+            mbar_expect(bar, stage_bytes);
+            tma_load(at + g.a_bytes, &map_b, k * kBK, n * g.width, bar);
+          }
           tma_load(at, &map_a, k * kBK, m * kBM, bar);
-          tma_load(at + g.a_bytes, &map_b, k * kBK, n * g.width, bar);
           r.next(g.stages);
         }
       }
@@ -225,12 +241,22 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
   } else {                                                  // ---- takes the sums out --------------------------------------------
     const uint32_t quarter = warp & 3u;                     // of tensor memory's lanes: a warp reaches those of its number modulo 4
     uint32_t done = 0;
+    bool waited = !g.early, fine = true;
     for (uint32_t i = blockIdx.x; i < tiles; i += gridDim.x, ++done) {
       uint32_t m, n;
       tile_at(g, i, &m, &n);
       const uint32_t half = done & 1u;
-      const bool fine = __all_sync(0xffffffffu, mbar_wait(sums_full0 + 8 * half, (done >> 1) & 1u, waits));
-      if (!fine) break;
+      // The columns' scales come while the sums do. (All four warps meet twice a tile, whether they have given up or not.)
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      for (uint32_t c = threadIdx.x - 64; c < g.width; c += 128) {
+        const uint32_t col = n * g.width + c < g.p.n ? n * g.width + c : g.p.n - 1;
+        b_scale[c] = __ldg(g.p.b_scale + col);
+        bias[c] = g.p.bias ? __ldg(g.p.bias + col) : 0.0f;
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (!waited) { chain_wait(); waited = true; }
+      fine = fine && __all_sync(0xffffffffu, mbar_wait(sums_full0 + 8 * half, (done >> 1) & 1u, waits));
+      if (!fine) continue;                                  // (to the next tile's meetings, and no further)
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t row = m * kBM + 32 * quarter + lane;
       const bool live = row < g.p.m;
@@ -247,8 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
             float y[16];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const uint32_t at = col + x < g.p.n ? col + x : g.p.n - 1;
-              y[x] = scaled_sum(v[x], a_scale, __ldg(g.p.b_scale + at), g.p.bias ? __ldg(g.p.bias + at) : 0.0f);
+              y[x] = scaled_sum(v[x], a_scale, b_scale[c + x], bias[c + x]);
             }
             if (g.vector_out && col + 16 <= g.p.n) {
               constexpr int kPer = 16 / sizeof(T);
@@ -321,7 +346,7 @@ uint32_t pick_width(uint32_t m_tiles, uint32_t a_rows, uint32_t n, uint32_t sms)
 }
 
 template <int TYPE>
-int launch(const MatmulArgs& p, cudaStream_t stream) {
+int launch(const MatmulArgs& p, bool early, cudaStream_t stream) {
   static KernelSite site;
   int sms = 0, occ = 0;
   int st = site.lookup(matmul_i8_kernel<TYPE>, kThreads, kSmem, &sms, &occ);
@@ -337,6 +362,7 @@ int launch(const MatmulArgs& p, cudaStream_t stream) {
   g.stages = kRingBytes / (g.a_bytes + g.width * kBK);
   if (g.stages > kMostStages) g.stages = kMostStages;
   g.polls = quantize_poll_limit();
+  g.early = early;
   g.vector_out = ((reinterpret_cast<uintptr_t>(p.out) | p.out_stride * (TYPE == QSGD_TYPE_F32 ? 4 : 2)) & 15u) == 0;
   CUtensorMap a, b;
   st = make_map(&a, p.a, p.k, p.m, p.a_stride, a_rows);
@@ -356,11 +382,11 @@ bool matmul_i8_many_takes(const MatmulArgs& p) {
   return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > kFewRows;
 }
 
-int launch_matmul_i8_many(const MatmulArgs& p, cudaStream_t stream) {
+int launch_matmul_i8_many(const MatmulArgs& p, bool early, cudaStream_t stream) {
   switch (p.type) {
-    case QSGD_TYPE_F32: return launch<QSGD_TYPE_F32>(p, stream);
-    case QSGD_TYPE_F16: return launch<QSGD_TYPE_F16>(p, stream);
-    default: return launch<QSGD_TYPE_BF16>(p, stream);
+    case QSGD_TYPE_F32: return launch<QSGD_TYPE_F32>(p, early, stream);
+    case QSGD_TYPE_F16: return launch<QSGD_TYPE_F16>(p, early, stream);
+    default: return launch<QSGD_TYPE_BF16>(p, early, stream);
   }
 }
 

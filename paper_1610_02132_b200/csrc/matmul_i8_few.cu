@@ -148,7 +148,7 @@ int launch(const MatmulArgs& p, bool early, cudaStream_t stream) {
 }  // namespace
 
 int launch_matmul_i8(const MatmulArgs& p, bool early, cudaStream_t stream) {
-  if (matmul_i8_many_takes(p)) return launch_matmul_i8_many(p, stream);
+  if (matmul_i8_many_takes(p)) return launch_matmul_i8_many(p, early, stream);
   const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | p.a_stride | p.b_stride) & 15u) == 0;
   // The second grid axis takes 65535 tiles: more rows go in several launches.
   constexpr uint32_t kMostRows = 65535u * 8;

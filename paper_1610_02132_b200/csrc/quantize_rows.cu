@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_co
   __shared__ float warp_top[kThreads / 32];
   const uint32_t c0 = 8 * threadIdx.x;
   chain_wait();
-  // (The library's kernels else release no dependents: waiting CTAs slow running ones down. Here the running ones are a CTA to a row, 64 at most.)
+  // (The library's kernels else release no dependents: waiting CTAs slow running ones down. Here the running ones are a CTA to a row, 128 at most.)
   if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = static_cast<const T*>(a.x) + r * a.row_stride;
