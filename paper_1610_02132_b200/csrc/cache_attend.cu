@@ -58,6 +58,10 @@ struct Rows {                             // of a segment: which rows of which s
   uint32_t start;                         // first query row of the sequence
 };
 
+struct Span {                             // of a segment in a CTA: where its first part lies, its first and last warp, whether it ends here (and began here)
+  uint8_t slot, first, last, ends;
+};
+
 struct JoinInfo {                         // of the segment that a CTA's stretch begins inside of, written by every CTA of every call
   Rows rows;
   uint32_t parts, first;                  // CTAs from `first` on hold a part each; 0: another CTA says so, or there is none
@@ -165,8 +169,17 @@ __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
 }
 
 // The largest pair (as a number) whose step is not above a power of two.
+// Of either half by itself.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 template <int TYPE>
-__device__ __forceinline__ uint32_t cap_bits(float cap) { return to_bits16<TYPE>(cap) << 16 | 0xffffu; }
+__device__ __forceinline__ uint32_t cap_bits(float cap) {
+  const float lo = cap * 1024.0f, most = TYPE == QSGD_TYPE_F16 ? 65504.0f : 3.3895314e38f;
+  return to_bits16<TYPE>(cap) << 16 | to_bits16<TYPE>(lo < most ? lo : most);
+}
 
 // The same less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
 __device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
@@ -263,6 +276,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
   __shared__ float cta_m[R], cta_l[R];                      // of the CTA's part of a segment that a cluster has
   __shared__ Rows part_rows[2][kWarps];
   __shared__ uint32_t late[kWarps];                         // a wait ran out
+  __shared__ Span spans[kWarps + 1];
+  __shared__ uint32_t n_spans;
   __shared__ uint32_t part_open[2][kWarps];                 // 0: no part; 1: the segment ends inside the warp's stretch; 2: it goes on
   __shared__ uint64_t head_begin, head_end;                 // of the segment that the CTA's stretch begins inside of, on the line of units
 
@@ -487,8 +502,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     }
 
     // ---- the warp's tiles, two at a time -------------------------------------------------------------------------------
-    float cap = kLeastCap;                                  // power of two that no step so far exceeds
-    uint32_t cap_pair = cap_bits<TYPE>(kLeastCap);          // the largest pair whose step does not
+    float cap = kLeastCap;                                  // power of two that no step so far exceeds, nor 2^-10 of any lo
+    uint32_t cap_pair = cap_bits<TYPE>(kLeastCap);          // the largest step and lo that do not
     auto take_tiles = [&](auto masked_, const uint8_t* const tiles, const uint32_t first) {
       constexpr bool kMasked = decltype(masked_)::value;
       const uint32_t ka = token_of(g), kb = ka + 8;
@@ -531,7 +546,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 
       // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
       uint32_t seen = 0xffffffffu;                                          // bit 4 * (NT * h + nt) + e
-      uint32_t widest = 0;                                                  // steps are not negative: pairs order like their upper halves
+      uint32_t widest = 0;                                                  // the largest step and the largest lo (sign aside)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -549,10 +564,10 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (kMasked && first + 16 * h + (x ? kb : ka) >= see_any) pair[h][x][j] = 0;      // was never written, perhaps
-            widest = pair[h][x][j] > widest ? pair[h][x][j] : widest;
+            widest = max_u16x2(widest, pair[h][x][j] & 0xffff7fffu);
           }
       }
-      bool raise = widest > cap_pair;
+      bool raise = widest >> 16 > cap_pair >> 16 || (widest & 0xffffu) > (cap_pair & 0xffffu);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -563,7 +578,10 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) step = fmaxf(step, from_bits16<TYPE>(pair[x >> 1][x & 1][j] >> 16));
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t w = pair[x >> 1][x & 1][j];
+            step = fmaxf(step, fmaxf(from_bits16<TYPE>(w >> 16), fabsf(from_bits16<TYPE>(w & 0xffffu)) * (1.0f / 1024.0f)));
+          }
 #pragma unroll
         for (int m = 4; m < 32; m <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, m));
         const uint32_t bits = (__float_as_uint(fminf(step, kMostCap)) + 0x007fffffu) & 0xff800000u;      // the next power of two
@@ -584,7 +602,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
             lsum[nt][e] *= f;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-              osum[nt][j][e] *= f;
+              osum[nt][j][e] *= fo;
 #pragma unroll
               for (int r = 0; r < 4; ++r) { o[nt][j][r][e] *= fo; o[nt][j][r][e + 2] *= fo; }
             }
@@ -609,9 +627,9 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const float step_a = from_bits16<TYPE>(pair[h][0][j] >> 16), step_b = from_bits16<TYPE>(pair[h][1][j] >> 16);
-          const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pair[h][0][j] & 0xffffu));
-          const float mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pair[h][1][j] & 0xffffu));
           const float times_a = step_a * times, times_b = step_b * times;
+          const float mid_a = fmaf(8.0f, times_a, from_bits16<TYPE>(pair[h][0][j] & 0xffffu) * times);
+          const float mid_b = fmaf(8.0f, times_b, from_bits16<TYPE>(pair[h][1][j] & 0xffffu) * times);
           uint32_t bh[NT][2], bl[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -683,7 +701,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     const uint32_t slot = from_front ? 1u : 0u;             // a part without the segment's front is the stretch's first, one with it the last
     const Rows which{head, row0, rows, seq.start};
     float* const mine = reinterpret_cast<float*>(slot ? ring : ring + S::kRingSpace);
-    const float held = cap * (1.0f / 64.0f);                // undoes the power of two in o
+    const float held = cap * (1.0f / 64.0f);                // undoes the power of two in o and osum
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -694,16 +712,22 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         for (int m = 4; m < 32; m <<= 1) l += __shfl_xor_sync(0xffffffffu, l, m);
         uint64_t lse_at = 0;
         uint16_t* out = nullptr;
-        float over = 0.0f;
+        float over = 0.0f;                                  // (sums that are not divided yet may lie outside fp32: times this, then times `held`)
         if (whole) {
           if (r < rows) {
             out = out_row(p, which, r, &lse_at);
             if (p.lse && g == 0) p.lse[lse_at] = log_sum(top[nt][e], l);
             over = saw(top[nt][e], l) ? 1.0f / l : 0.0f;
           }
-        } else if (g == 0) {
-          part_m[slot][warp][r] = top[nt][e];
-          part_l[slot][warp][r] = l;
+        } else {
+          // A part goes with its sum between 2^-12 and 2^-11, the power of two in its maximum, so that 2^11 of them add up to no more than the
+          // largest value.
+          const int32_t up = l > 0.0f && l < INFINITY ? (int32_t)(__float_as_uint(l) >> 23) - 127 + 12 : 0;
+          over = __uint_as_float((uint32_t)(127 - up) << 23);
+          if (g == 0) {
+            part_m[slot][warp][r] = top[nt][e] + (float)up;
+            part_l[slot][warp][r] = l * over;
+          }
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
@@ -713,13 +737,12 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
           float v[8];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            v[i] = fmaf(o[nt][j][i][e] * (i & 1 ? 1048576.0f : 16777216.0f), held, z);
-            v[i + 4] = fmaf(o[nt][j][i][e + 2] * (i & 1 ? 1048576.0f : 16777216.0f), held, z);
+            v[i] = fmaf(o[nt][j][i][e], i & 1 ? 1048576.0f : 16777216.0f, z) * over * held;
+            v[i + 4] = fmaf(o[nt][j][i][e + 2], i & 1 ? 1048576.0f : 16777216.0f, z) * over * held;
           }
           if (out) {
             *reinterpret_cast<uint4*>(out + 64 * j + 8 * g) =
-                make_uint4(pack16<TYPE>(v[0] * over, v[1] * over), pack16<TYPE>(v[2] * over, v[3] * over), pack16<TYPE>(v[4] * over, v[5] * over),
-                           pack16<TYPE>(v[6] * over, v[7] * over));
+                make_uint4(pack16<TYPE>(v[0], v[1]), pack16<TYPE>(v[2], v[3]), pack16<TYPE>(v[4], v[5]), pack16<TYPE>(v[6], v[7]));
           } else if (!whole) {
             float* const at = mine + r * S::kRowFloats + 64 * j + 8 * g;
             *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
@@ -738,57 +761,58 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 
   // ---- what spans warps: joined, and written out where it ends in this CTA -------------------------------------------------
   __syncthreads();
-  JoinInfo info{};
-  // Segment k: the one that begins in front of the CTA (0), or in warp k - 1. All threads take a few long ones together; of many short ones each
-  // warp takes the one that begins in it (one after another, each waiting for the latency of its reads, 15 took 3 us).
-  uint32_t segments = part_open[0][0] ? 1u : 0u;
-#pragma unroll
-  for (uint32_t w = 0; w < kWarps; ++w) segments += part_open[1][w] ? 1u : 0u;
-  const bool together = segments <= 2;
-  const uint32_t member = together ? tid : lane, members = together ? kThreads : 32u;
-#pragma unroll 1
-  for (uint32_t k = 0; k <= kWarps; ++k) {
-    if (!together && (k ? k - 1 : 0u) != warp) continue;
-    const uint32_t slot = k ? 1u : 0u, w0 = k ? k - 1 : 0u;
-    if (part_open[slot][w0] == 0) continue;
+  // Segment 0 begins in front of the CTA, segment k in warp k - 1. All threads go over all segments' rows. (Segments one after another, each waiting for
+  // the latency of its reads, or a warp to each: 256 segments of 16 rows and 512 tokens took 37.5 us that way, 33.4 this.)
+  if (warp == 0) {
+    const uint32_t slot = lane ? 1u : 0u, w0 = lane ? lane - 1 : 0u;
+    const bool open = lane <= kWarps && part_open[slot][w0] != 0;
     uint32_t w1 = w0;                                       // last warp that has some of the segment
-    bool goes_on = part_open[slot][w0] == 2;
+    bool goes_on = open && part_open[slot][w0] == 2;
     while (goes_on && w1 + 1 < kWarps && part_open[0][w1 + 1]) goes_on = part_open[0][++w1] == 2;       // (the last warps may have no units)
+    const uint32_t all = __ballot_sync(0xffffffffu, open);
+    if (open) spans[__popc(all & ((1u << lane) - 1u))] = Span{(uint8_t)slot, (uint8_t)w0, (uint8_t)w1, (uint8_t)(slot && !goes_on)};
+    if (lane == 0) n_spans = __popc(all);
+  }
+  __syncthreads();
+  constexpr uint32_t kPieces = R * (D / 4);
+  const uint32_t pieces = n_spans * kPieces;
+#pragma unroll 1
+  for (uint32_t i = tid; i < pieces; i += kThreads) {
+    const Span span = spans[i / kPieces];
+    const uint32_t r = i % kPieces / (D / 4), d4 = i % (D / 4), slot = span.slot, w0 = span.first;
     const Rows which = part_rows[slot][w0];
-    const bool out_here = p.direct <= 1 && k != 0 && !goes_on;
-    float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
-    for (uint32_t i = member; i < which.rows * (D / 4); i += members) {
-      const uint32_t r = i / (D / 4), d4 = i - r * (D / 4);
-      float m = part_m[slot][w0][r], l = part_l[slot][w0][r];
-      float4 sum = *reinterpret_cast<const float4*>(smem + w0 * S::kPerWarp + (slot ? 0 : S::kRingSpace) + (r * S::kRowFloats + 4 * d4) * 4);
-      for (uint32_t w = w0 + 1; w <= w1; ++w) {
-        const float wm = part_m[0][w][r], high = fmaxf(m, wm), f = exp2_approx(m - high), e = exp2_approx(wm - high);
-        const float4 v = *reinterpret_cast<const float4*>(smem + w * S::kPerWarp + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4);
-        m = high;
-        l = fmaf(e, part_l[0][w][r], f * l);
-        sum.x = fmaf(e, v.x, f * sum.x); sum.y = fmaf(e, v.y, f * sum.y); sum.z = fmaf(e, v.z, f * sum.z); sum.w = fmaf(e, v.w, f * sum.w);
-      }
-      if (out_here) {
-        uint64_t lse_at;
-        uint16_t* const out = out_row(p, which, r, &lse_at);
-        const float over = saw(m, l) ? 1.0f / l : 0.0f;
-        *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
-        if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
-      } else if (p.direct) {                                // where the cluster's other CTAs look for it: nobody else's part, or this very place's
-        *reinterpret_cast<float4*>(smem + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4) = sum;
-        if (d4 == 0) { cta_m[r] = m; cta_l[r] = l; }
-      } else {
-        *reinterpret_cast<float4*>(part + r * D + 4 * d4) = sum;
-        if (d4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
-      }
+    if (r >= which.rows) continue;
+    float m = part_m[slot][w0][r], l = part_l[slot][w0][r];
+    float4 sum = *reinterpret_cast<const float4*>(smem + w0 * S::kPerWarp + (slot ? 0 : S::kRingSpace) + (r * S::kRowFloats + 4 * d4) * 4);
+    for (uint32_t w = w0 + 1; w <= span.last; ++w) {
+      const float wm = part_m[0][w][r], high = fmaxf(m, wm), f = exp2_approx(m - high), e = exp2_approx(wm - high);
+      const float4 v = *reinterpret_cast<const float4*>(smem + w * S::kPerWarp + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4);
+      m = high;
+      l = fmaf(e, part_l[0][w][r], f * l);
+      sum.x = fmaf(e, v.x, f * sum.x); sum.y = fmaf(e, v.y, f * sum.y); sum.z = fmaf(e, v.z, f * sum.z); sum.w = fmaf(e, v.w, f * sum.w);
     }
-    if (k == 0 && !p.direct) {
-      const uint32_t first = (uint32_t)(head_begin / per_cta);
-      if (first + 1 == blockIdx.x) {                        // this CTA's start is the first such boundary inside the segment
-        info.rows = which;
-        info.first = first;
-        info.parts = (uint32_t)((head_end - 1) / per_cta) - first + 1;
-      }
+    if (span.ends && p.direct <= 1) {
+      uint64_t lse_at;
+      uint16_t* const out = out_row(p, which, r, &lse_at);
+      const float over = saw(m, l) ? 1.0f / l : 0.0f;
+      *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
+      if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
+    } else if (p.direct) {                                  // where the cluster's other CTAs look for it: nobody else's part, or this very place's
+      *reinterpret_cast<float4*>(smem + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4) = sum;
+      if (d4 == 0) { cta_m[r] = m; cta_l[r] = l; }
+    } else {
+      float* const part = p.parts + ((uint64_t)blockIdx.x * 2 + slot) * part_floats(R, D);
+      *reinterpret_cast<float4*>(part + r * D + 4 * d4) = sum;
+      if (d4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
+    }
+  }
+  JoinInfo info{};
+  if (part_open[0][0] && !p.direct) {
+    const uint32_t first = (uint32_t)(head_begin / per_cta);
+    if (first + 1 == blockIdx.x) {                          // this CTA's start is the first such boundary inside the segment
+      info.rows = part_rows[0][0];
+      info.first = first;
+      info.parts = (uint32_t)((head_end - 1) / per_cta) - first + 1;
     }
   }
   if (tid == 0 && !p.direct) p.join[blockIdx.x] = info;

@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     const uint32_t twins = 1 + quarter;                     // named barrier of the two warps that share their rows
     const bool live = r < rows;
     const uint32_t query = (row0 + r) / p.group, hh = head * p.group + (row0 + r) - query * p.group;
-    const int64_t far = live ? seq.length - (int64_t)(seq.n - 1 - query) : 0;
+    // (A row that is not there sees what any other does: a warp without masks is a fifth faster, 366 us against 467 for 64 rows of 16384 tokens.)
+    const int64_t far = live ? seq.length - (int64_t)(seq.n - 1 - query) : (int64_t)see_any;
     const uint32_t see = far > 0 ? (uint32_t)far : 0u;
     float factor = 0.0f, top = kNoMax, l = 0.0f, cap = kLeastCap;
     uint32_t nan_groups = 0;
@@ -659,10 +660,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
 }
 
 template <int D>
-int launch_wide(const WideParams& p, cudaStream_t stream) {
+int look_up(int* sms) {
   static KernelSite site;
-  int sms = 0, occ = 0;
-  const int st = site.lookup(cache_attend_wide_kernel<D>, kThreads, Shape<D>::kSmem, &sms, &occ);
+  int occ = 0;
+  return site.lookup(cache_attend_wide_kernel<D>, kThreads, Shape<D>::kSmem, sms, &occ);
+}
+
+template <int D>
+int launch_wide(const WideParams& p, cudaStream_t stream) {
+  int sms = 0;
+  const int st = look_up<D>(&sms);
   if (st) return st;
   // At most this many row tiles: where the sequences' rows end inside one is known on the device only.
   const uint64_t ctas = (uint64_t)p.c.heads * ((uint64_t)p.c.rows * p.group / kRows + p.c.sequences);
@@ -672,10 +679,19 @@ int launch_wide(const WideParams& p, cudaStream_t stream) {
 
 }  // namespace
 
+// A CTA has a row tile for itself, and all of its tokens, so that few tiles leave SMs idle, while cache_attend.cu spreads any rows over all SMs. A round of
+// tiles over the SMs takes 57, 190 and 366 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
+// 46, 108 and 200 for 4096 rows in all heads, 70, 199 and 375 for 8192, and 115, 374 and 727 for 16384. At head size 64: 51, 175 and 338 against 42, 117
+// and 213 for 8192 rows, 68, 215 and 408 for 16384. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays.
 bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads) {
+  if (type != QSGD_TYPE_BF16 || (head_dim != 64 && head_dim != 128) || !view.starts || !view.sequences) return false;
   const uint64_t rows = (uint64_t)view.rows * (q_heads / view.heads);        // of a key head
-  return type == QSGD_TYPE_BF16 && (head_dim == 64 || head_dim == 128) && view.starts && rows >= 64ull * view.sequences &&
-         (rows / kRows + view.sequences) * view.heads < (1ull << 31);
+  if ((rows / kRows + view.sequences) * view.heads >= (1ull << 31)) return false;
+  int sms = 0;
+  if ((head_dim == 64 ? look_up<64>(&sms) : look_up<128>(&sms)) || sms < 1) return false;
+  const uint64_t each = (rows + view.sequences - 1) / view.sequences, tiles = (each + kRows - 1) / kRows * view.sequences * view.heads;
+  const uint64_t room = (tiles + sms - 1) / sms * sms * kRows;
+  return rows * view.heads * 12 >= room * (head_dim == 64 ? 9 : 5);
 }
 
 int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const AttendArgs& a, cudaStream_t stream) {

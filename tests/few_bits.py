@@ -74,12 +74,11 @@ def attend(q, k, v, scale, length, runs):
         n = length - rows + i + 1
         if n <= 0:
             continue
-        for h in range(heads):
-            s = k[:n, h // group] @ q[i, h].double() * scale
-            lse[i, h] = torch.logsumexp(s, 0)
-            p = torch.softmax(s, 0)
-            out[i, h] = p @ v[:n, h // group]
-            mean[i, h] = p @ v[:n, h // group].abs()
+        s = torch.einsum("nkd,kgd->kgn", k[:n], q[i].double().unflatten(0, (-1, group))) * scale
+        lse[i] = torch.logsumexp(s, -1).flatten()
+        p = torch.softmax(s, -1)
+        out[i] = torch.einsum("kgn,nkd->kgd", p, v[:n]).flatten(0, 1)
+        mean[i] = torch.einsum("kgn,nkd->kgd", p, v[:n].abs()).flatten(0, 1)
     return out, lse, mean
 
 

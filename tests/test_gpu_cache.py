@@ -233,16 +233,32 @@ def test_attend_chunks(dim, heads, group, page, lengths, runs):
     assert bool((out[sum(runs):] == 42).all()) and bool((lse[sum(runs):] == 42).all())
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads, group, page, lengths, runs", [(28, 4, 16, [300], [129]), (24, 4, 64, [200, 65, 130], [70, 65, 33]), (48, 8, 16, [5, 700, 0], [40, 33, 7]),
+                                                               (24, 12, 16, [17, 16, 2000], [17, 9, 30]), (49, 2, 48, [64, 128, 192], [30, 64, 96]),
+                                                               (49, 1, 128, [513], [380])])
+def test_attend_chunks_that_fill_the_device(dim, heads, group, page, lengths, runs):
+    """Rows enough for a tile of 128 to nearly every SM: one kernel, without a second one that joins parts."""
+    f = Filled(lengths, page, heads, dim, BF16).write_all()
+    torch.cuda.synchronize()
+    before = Q.qsgd_launch_count()
+    q, out, lse = run_attend(f, heads * group, runs, BF16, rows=sum(runs) + 2)
+    assert Q.qsgd_launch_count() - before == 1
+    check(out, lse, q, f.k, f.v, 1 / math.sqrt(dim), lengths, runs, BF16, wide=True)
+    assert bool((out[sum(runs):] == 42).all()) and bool((lse[sum(runs):] == 42).all())
+
+
+@pytest.mark.parametrize("heads", [1, 74])
 @pytest.mark.parametrize("size_k, size_v", [(1e30, 1e30), (1e-30, 1e-36), (1.0, 3e37), (1e4, 1e-4)])
-def test_attend_chunks_of_all_sizes(size_k, size_v):
+def test_attend_chunks_of_all_sizes(size_k, size_v, heads):
     """bf16 numbers far outside fp16's range, and tokens of very different sizes side by side."""
-    f = Filled([400], 16, 1, 128, BF16)
+    f = Filled([400], 16, heads, 128, BF16)
     sizes = torch.ones(400)
     sizes[100:200] = 1e-4
     f.k[0] = (f.k[0].float() * size_k * sizes[:, None, None]).to(BF16)
     f.v[0] = (f.v[0].float() * size_v * sizes.flip(0)[:, None, None]).to(BF16)
     f.write_all()
-    q, out, lse = run_attend(f, 2, [100], BF16, scale=0.1 / size_k if size_k < 1e20 else 0.0)
+    q, out, lse = run_attend(f, 2 * heads, [100], BF16, scale=0.1 / size_k if size_k < 1e20 else 0.0)
     ref, ref_lse, mean = F.attend(q.cpu(), F.held_value(f.k[0]), F.held_value(f.v[0]), 0.1 / size_k if size_k < 1e20 else 0.0, 400, 100)
     err = 0.1 * q.cpu().double().abs().sum(-1, keepdim=True) * 8 * 2.0 ** -11 if size_k < 1e20 else 0.0     # |k| below 8 sizes
     tol = F.HALF_STEP[BF16] * ref.abs() + (2 * err + 2.0 ** -10) * mean + 2.0 ** -11 * f.v[0].double().abs().max()
@@ -256,6 +272,20 @@ def test_attend_long(dtype, heads, group, dim, lengths):
     f = Filled(lengths, 64, heads, dim, dtype).write_all()
     q, out, lse = run_attend(f, heads * group, [1] * len(lengths), dtype, one_each=True)
     check(out, lse, q, f.k, f.v, 1 / math.sqrt(dim), lengths, [1] * len(lengths), dtype)
+
+
+@pytest.mark.parametrize("what", ["huge", "huge and nearly equal", "tiny", "far from zero"])
+@pytest.mark.parametrize("lengths, runs", [([9000, 40], [1, 1]), ([600], [1]), ([300, 90], [5, 9])])
+def test_attend_values_of_all_sizes(what, lengths, runs):
+    """Sums of p v that would not fit 32 bits before they are divided; steps far smaller than the values."""
+    f = Filled(lengths, 16, 2, 128, BF16)
+    for v in f.v:
+        x = v.float()
+        v.copy_({"huge": x * 3e37, "huge and nearly equal": 3e38 * (1 - x.abs() * 2.0 ** -8), "tiny": x * 1e-33, "far from zero": 1000 + x}[what])
+    f.write_all()
+    q, out, lse = run_attend(f, 8, runs, BF16, one_each=max(runs) == 1)
+    size = 2.0 ** -100 if "huge" in what else 2.0 ** 100 if what == "tiny" else 1.0
+    check(out.double() * size, lse, q, f.k, [(v.double() * size).to(BF16) for v in f.v], 1 / math.sqrt(128), lengths, runs, BF16)     # (exactly)
 
 
 def test_attend_many_sequences():
@@ -288,17 +318,18 @@ def test_attend_strided_and_without_lse():
     check(whole, lse, wide[:, :4], f.k, f.v, 1 / math.sqrt(128), [90, 40], [1, 1], BF16)
 
 
-@pytest.mark.parametrize("n, dim", [(40, 128), (100, 128), (100, 64)])
-def test_poisoned_tokens(n, dim):
+@pytest.mark.parametrize("n, dim, heads", [(40, 128, 1), (100, 128, 1), (100, 64, 1), (100, 128, 148), (100, 64, 148)])
+def test_poisoned_tokens(n, dim, heads):
     """A key that is not finite makes the rows that see it NaN and no others; a value that is not finite, its group of coordinates."""
-    f = Filled([n], 16, 1, dim, BF16)
-    f.k[0][30, 0, 5] = math.inf
-    f.v[0][20, 0, dim - 58] = math.nan
+    f = Filled([n], 16, heads, dim, BF16)
+    f.k[0][30, :, 5] = math.inf
+    f.v[0][20, :, dim - 58] = math.nan
     f.write_all()
-    q, out, lse = run_attend(f, 1, [n], BF16)
-    nan = out.isnan()[:, 0]
+    q, out, lse = run_attend(f, heads, [n], BF16)
+    nan = out.isnan()[:, heads // 2]
+    assert torch.equal(out.isnan(), nan[:, None].expand(-1, heads, -1))
     assert bool(nan[30:].all()) and not bool(nan[:20].any()) and not bool(nan[20:30, : dim - 64].any()) and bool(nan[20:30, dim - 64:].all())
-    assert torch.equal(lse.isnan()[:, 0], torch.arange(n).cuda() >= 30)
+    assert torch.equal(lse.isnan(), (torch.arange(n).cuda() >= 30)[:, None].expand(-1, heads))
     check(out[:20], lse[:20], q[:20], [f.k[0][:20]], [f.v[0][:20]], 1 / math.sqrt(dim), [20], [20], BF16, wide=n >= 64)
 
 
@@ -335,6 +366,28 @@ def test_places_that_the_cache_has_not(what):
     assert torch.equal(k[rows], good_k[rows])
     touched = (f.cache.data != before).flatten(1).any(1).nonzero().flatten().tolist()
     assert set(touched) <= {int(p) for p in f.table_host.flatten() if p >= 0}
+
+
+@pytest.mark.parametrize("what", ["page below", "page above", "length", "negative length", "starts"])
+def test_places_that_the_cache_has_not_in_chunks(what):
+    """The same where a tile of 128 rows has all tokens: the other sequences' rows are the same to the bit."""
+    f = Filled([50, 40, 35], 16, 48, 128, BF16).write_all()
+    starts = starts_of([32, 32, 32])
+    q, good, lse = run_attend(f, 192, [32, 32, 32], BF16)
+    if what == "page below": f.table[1, 2] = -1
+    if what == "page above": f.table[1, 2] = f.cache.n_pages
+    if what == "length": f.len[1] = 16 * f.table.shape[1] + 1
+    if what == "negative length": f.len[1] = -3
+    if what == "starts": starts[2] = 20
+    big = torch.full((96 + 8, 192, 128), 42.0, dtype=BF16, device="cuda")
+    ws, status = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 192), dtype=torch.uint8, device="cuda"), Q.new_status()
+    before = Q.qsgd_launch_count()
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, big[:96], ws, status, starts=starts)
+    assert Q.qsgd_launch_count() - before == 1
+    assert int(status.item()) == Q.DEV_PAGE
+    assert bool((big[96:] == 42).all())
+    if what != "starts":
+        assert torch.equal(big[:32], good[:32]) and torch.equal(big[64:96], good[64:])
 
 
 def test_far_pages():
@@ -402,20 +455,20 @@ def test_a_generation_in_a_graph():
         assert torch.equal(out, out2)
 
 
-@pytest.mark.parametrize("lengths, runs", [([900, 300], None), ([9000], None), ([300, 200], [100, 60])])
-def test_every_route_in_a_graph(lengths, runs):
+@pytest.mark.parametrize("lengths, runs, heads", [([900, 300], None, 2), ([9000], None, 2), ([300, 200], [100, 60], 2), ([300, 200], [100, 60], 24)])
+def test_every_route_in_a_graph(lengths, runs, heads):
     """Clusters to a segment, the line of units with its second kernel, tiles of 128 rows: replayed with other queries and lengths."""
-    f = Filled(lengths, 16, 2, 128, BF16).write_all()
+    f = Filled(lengths, 16, heads, 128, BF16).write_all()
     rows, starts = sum(runs or [1] * len(lengths)), starts_of(runs) if runs else None
-    q, out = torch.zeros(rows, 8, 128, dtype=BF16, device="cuda"), torch.zeros(rows, 8, 128, dtype=BF16, device="cuda")
-    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 8), dtype=torch.uint8, device="cuda")
+    q, out = torch.zeros(rows, 4 * heads, 128, dtype=BF16, device="cuda"), torch.zeros(rows, 4 * heads, 128, dtype=BF16, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 4 * heads), dtype=torch.uint8, device="cuda")
     Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts)
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts)
     for seed in (1, 2, 3):
-        q.copy_(values((rows, 8, 128), BF16, seed))
+        q.copy_(values((rows, 4 * heads, 128), BF16, seed))
         f.len.copy_(torch.tensor([n - 7 * seed for n in lengths], dtype=torch.int32))
         ws.fill_(255)
         g.replay()

@@ -22,8 +22,9 @@ def zero_polls():
         Q.qsgd_test_set_wait_polls(Q.qsgd_test_default_wait_polls())
 
 
-# clusters to a segment, a CTA to a segment, the line of units, rows in tiles of 128
-@pytest.mark.parametrize("lengths, runs, heads", [([600], None, 2), ([40], None, 1), ([3000] * 9, None, 8), ([700, 300], [100, 64], 1)])
+# clusters to a segment, a CTA to a segment, the line of units with one row a sequence and with several, rows in tiles of 128
+@pytest.mark.parametrize("lengths, runs, heads", [([600], None, 2), ([40], None, 1), ([3000] * 9, None, 8), ([700, 300], [100, 64], 1),
+                                                  ([700, 300], [100, 64], 24)])
 def test_attend_gives_up_and_returns(zero_polls, lengths, runs, heads):
     f = Filled(lengths, 16, heads, 128, BF16).write_all()
     rows = sum(runs or [1] * len(lengths))
