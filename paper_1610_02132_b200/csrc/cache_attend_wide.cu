@@ -23,7 +23,7 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 3;
+constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 3, kValues = 3;
 constexpr uint32_t kMostSorted = 256;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 constexpr float kNoMax = -1.0e30f;
@@ -46,7 +46,8 @@ struct Shape {
   static constexpr uint32_t kTile = 18 * D;                // 16 packed tokens
   static constexpr uint32_t kRaw = 4 * kTile;
   static constexpr uint32_t kQ = kRows * D * 2, kK = kStep * D * 2, kV = D * kStep * 2, kP = kRows * kStep * 2;
-  static constexpr uint32_t kAtK = kQ, kAtV = kAtK + 2 * kK, kAtP = kAtV + 2 * kV, kAtRaw = kAtP + kP;
+  static constexpr uint32_t kAtK = kQ, kAtV = kAtK + 2 * kK, kAtP = kAtV + kValues * kV, kAtRaw = kAtP + 2 * kP;
+  static constexpr uint32_t kTmem = 4 * D;                 // two tiles of S, 64 columns each, and two of O (at least a power of two)
   static constexpr uint32_t kSmem = kAtRaw + kRawStages * kRaw + 1024;
 };
 
@@ -54,6 +55,13 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)_
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Without the suspension that a try may bring.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
@@ -72,8 +80,19 @@ struct Waits {
   volatile uint32_t* given_up;
   uint32_t polls;
 };
+__device__ __forceinline__ bool given_up_now(const Waits& w) { return *w.given_up != 0; }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {
   return (w.polls && mbar_try(bar, parity)) || mbar_poll(bar, parity, w.given_up, w.polls);
+}
+// In line, where a call would have to save a row of scores.
+__device__ __forceinline__ bool mbar_wait_here(uint32_t bar, uint32_t parity, const Waits& w) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < w.polls; ++i) {
+    if (mbar_try(bar, parity)) return true;
+    if ((i & 63u) == 63u && *w.given_up) return false;
+  }
+  *w.given_up = 1;
+  return false;
 }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -92,34 +111,37 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
                "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at, float* v) {
-  uint32_t r[32];
+__device__ __forceinline__ void tmem_load16(uint32_t at, float* v) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
-      "%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
-        "=r"(r[31])
-      : "r"(at));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tmem_store32(uint32_t at, const float* v) {
+__device__ __forceinline__ void tmem_load64(uint32_t at, float* v) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
-      "%27,%28,%29,%30,%31,%32};" ::"r"(at),
-      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
-      "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])),
-      "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])), "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])),
-      "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15])), "r"(__float_as_uint(v[16])), "r"(__float_as_uint(v[17])),
-      "r"(__float_as_uint(v[18])), "r"(__float_as_uint(v[19])), "r"(__float_as_uint(v[20])), "r"(__float_as_uint(v[21])),
-      "r"(__float_as_uint(v[22])), "r"(__float_as_uint(v[23])), "r"(__float_as_uint(v[24])), "r"(__float_as_uint(v[25])),
-      "r"(__float_as_uint(v[26])), "r"(__float_as_uint(v[27])), "r"(__float_as_uint(v[28])), "r"(__float_as_uint(v[29])),
-      "r"(__float_as_uint(v[30])), "r"(__float_as_uint(v[31]))
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+      "%25,%26,%27,%28,%29,%30,%31}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,"
+      "%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
+        "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]),
+        "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]),
+        "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]),
+        "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]), "=f"(v[50]),
+        "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]),
+        "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+      : "r"(at), "r"(at + 32) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const float* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n\t"
+      "tcgen05.wait::st.sync.aligned;" ::"r"(at),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]),
+      "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
       : "memory");
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float exp2_approx(float v) {
@@ -168,42 +190,44 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   constexpr int J = S::kGroups;
   constexpr int TYPE = QSGD_TYPE_BF16;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[2 * kRawStages + 19];
+  __shared__ uint64_t bars[2 * kRawStages + 2 * kValues + 17];
   __shared__ uint64_t scan[kThreads / 32];
   __shared__ uint64_t found_base;
   __shared__ uint32_t found_b, tmem_base, given_up;
   __shared__ int32_t length_of[kMostSorted];
   __shared__ uint32_t order[kMostSorted];
-  __shared__ float key_back[4], value_size[4];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
+  __shared__ float key_back[8], value_size[8];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
   __shared__ uint2 key_pair[2][kStep * J];                 // (step, step), (lo, lo) in fp16
   __shared__ uint32_t value_pair[2][kStep * J];            // step, lo
-  __shared__ float row_max[2][2][kRows], row_sum[2][kRows];
+  __shared__ float row_max[2][kRows], row_sum[2][kRows], row_cap[2][kRows];
   __shared__ uint32_t row_nan[2][kRows];
-  __shared__ uint8_t poison[4][kStep];                     // groups of a token's values that hold what is no number
-  __shared__ uint32_t poisoned[4];
+  __shared__ uint8_t poison[8][kStep];                     // groups of a token's values that hold what is no number
+  __shared__ uint32_t poisoned[8];                         // (of eight steps: the pairs may be five ahead of the softmax)
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
   const Waits waits{&given_up, p.polls};
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const mem = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t raw_full = bar0, raw_empty = raw_full + 8 * kRawStages, k_full = raw_empty + 8 * kRawStages, k_empty = k_full + 16,
-                 v_full = k_empty + 16, v_empty = v_full + 16, s_full = v_empty + 16, s_empty = s_full + 16, p_full = s_empty + 16, pv = p_full + 8,
-                 q_full = pv + 8, pairs_full = q_full + 8, pairs_empty = pairs_full + 16;
+                 v_full = k_empty + 16, v_empty = v_full + 8 * kValues, s_full = v_empty + 8 * kValues, s_empty = s_full + 16, p_full = s_empty + 16, pv = p_full + 16,
+                 q_full = pv + 16, pairs_full = q_full + 8, pairs_empty = pairs_full + 16;
   if (tid == 0) {
     for (uint32_t s = 0; s < kRawStages; ++s) { mbar_init(raw_full + 8 * s, 1); mbar_init(raw_empty + 8 * s, kUnpackWarps); }
     for (uint32_t s = 0; s < 2; ++s) {
       mbar_init(k_full + 8 * s, kUnpackWarps); mbar_init(k_empty + 8 * s, 1);
-      mbar_init(v_full + 8 * s, kUnpackWarps); mbar_init(v_empty + 8 * s, 1);
-      mbar_init(s_full + 8 * s, 1); mbar_init(s_empty + 8 * s, kSoftmaxWarps);
+      mbar_init(s_full + 8 * s, 1); mbar_init(s_empty + 8 * s, kSoftmaxWarps / 2);
     }
-    mbar_init(p_full, kSoftmaxWarps);
-    mbar_init(pv, 1);                                       // a product P V is done
+    for (uint32_t s = 0; s < 2; ++s) {
+      mbar_init(p_full + 8 * s, kSoftmaxWarps / 2);
+      mbar_init(pv + 8 * s, 1);                             // a product P V is done
+    }
     mbar_init(q_full, kSoftmaxWarps);
     for (uint32_t s = 0; s < 2; ++s) { mbar_init(pairs_full + 8 * s, 2); mbar_init(pairs_empty + 8 * s, kUnpackWarps); }
+    for (uint32_t s = 0; s < kValues; ++s) { mbar_init(v_full + 8 * s, kUnpackWarps); mbar_init(v_empty + 8 * s, 1); }
     given_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 0) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" ::"r"(smem_u32(&tmem_base)) : "memory");
+  if (warp == 0) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(S::kTmem) : "memory");
   chain_wait();
 
   // ---- which rows of which sequence -----------------------------------------------------------------------------------
@@ -310,40 +334,43 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       constexpr uint32_t idesc_o = (1u << 4) | ((D >> 3) << 17) | ((kRows >> 4) << 24);
       bool fine = mbar_wait(q_full, 0, waits);
       uint32_t issued = 0, done = 0;                        // products Q K^T, P V issued
-      auto product_pv = [&](uint32_t i) {
-        const uint32_t b = i & 1u;
-        if (!mbar_wait(v_full + 8 * b, (i >> 1) & 1u, waits) || !mbar_wait(p_full, i & 1u, waits)) { fine = false; return; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t pa = tile_desc(base + S::kAtP), vb = tile_desc(base + S::kAtV + b * S::kV);
-#pragma unroll
-        for (uint32_t x = 0; x < kStep / 16; ++x) mma_f16(tmem_o, pa + 2 * x, vb + 2 * x, idesc_o, i != 0 || x != 0);
-        tc_commit(v_empty + 8 * b);
-        tc_commit(pv);
-        ++done;
-      };
-      uint32_t i = 0;
+      // S of a step as soon as its keys are there and S of the step before the last one has been read, O of a step as soon as P is there: whichever
+      // can go first, since the two halves of the softmax warps run by themselves.
+      uint32_t idle = 0;
 #pragma unroll 1
-      for (; i <= steps && fine; ++i) {                     // S of step i, then O of the step before
-        const uint32_t b = i & 1u;
-        if (i < steps) {
-          if (!mbar_wait(k_full + 8 * b, (i >> 1) & 1u, waits) ||
-              (i >= 2 && !mbar_wait(s_empty + 8 * b, ((i >> 1) - 1) & 1u, waits))) { fine = false; break; }
+      while (fine && done < steps) {
+        const uint32_t bs = issued & 1u, bo = done & 1u;
+        bool moved = false;
+        if (issued < steps && mbar_test(k_full + 8 * bs, (issued >> 1) & 1u) && (issued < 2 || mbar_test(s_empty + 8 * bs, ((issued >> 1) - 1) & 1u))) {
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
           for (uint32_t x = 0; x < D / 16; ++x)
-            mma_f16(tmem + b * kStep, tile_desc(base + (x / 4) * (kRows * 128)) + 2 * (x % 4),
-                    tile_desc(base + S::kAtK + b * S::kK + (x / 4) * (kStep * 128)) + 2 * (x % 4), idesc_s, x != 0);
-          tc_commit(k_empty + 8 * b);
-          tc_commit(s_full + 8 * b);
+            mma_f16(tmem + bs * kStep, tile_desc(base + (x / 4) * (kRows * 128)) + 2 * (x % 4),
+                    tile_desc(base + S::kAtK + bs * S::kK + (x / 4) * (kStep * 128)) + 2 * (x % 4), idesc_s, x != 0);
+          tc_commit(k_empty + 8 * bs);
+          tc_commit(s_full + 8 * bs);
           ++issued;
+          moved = true;
         }
-        if (i) product_pv(i - 1);
+        if (done < issued && mbar_test(v_full + 8 * (done % kValues), (done / kValues) & 1u) && mbar_test(p_full + 8 * bo, (done >> 1) & 1u)) {
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t pa = tile_desc(base + S::kAtP + bo * S::kP), vb = tile_desc(base + S::kAtV + (done % kValues) * S::kV);
+#pragma unroll
+          for (uint32_t x = 0; x < kStep / 16; ++x) mma_f16(tmem_o + bo * D, pa + 2 * x, vb + 2 * x, idesc_o, done >= 2 || x != 0);
+          tc_commit(v_empty + 8 * (done % kValues));
+          tc_commit(pv + 8 * bo);
+          ++done;
+          moved = true;
+        }
+        idle = moved ? 0u : idle + 1;
+        if (idle >= waits.polls || ((idle & 63u) == 63u && given_up_now(waits))) fine = false;
       }
+      if (!fine) *waits.given_up = 1;
       if (!fine && issued) {                                     // products in flight are done before tensor memory is freed
 #pragma unroll 1
         for (uint32_t t = 0; t < kDrainPolls && !mbar_try(k_empty + 8 * ((issued - 1) & 1u), ((issued - 1) >> 1) & 1u); ++t) {}
 #pragma unroll 1
-        for (uint32_t t = 0; done && t < kDrainPolls && !mbar_try(pv, (done - 1) & 1u); ++t) {}
+        for (uint32_t t = 0; done && t < kDrainPolls && !mbar_try(pv + 8 * ((done - 1) & 1u), ((done - 1) >> 1) & 1u); ++t) {}
       }
     }
   } else if (warp < 4) {                                    // ---- pairs: warp 2 the keys', warp 3 the values' ---------------------
@@ -373,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
             pair[x][j] = 0;
           }
         }
-        if (value) poison[i & 3u][token] = (uint8_t)groups;
+        if (value) poison[i & 7u][token] = (uint8_t)groups;
         bad |= groups != 0;
       }
       largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));
@@ -390,8 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         }
       const bool any = __any_sync(0xffffffffu, bad);
       if (lane == 0) {
-        if (value) { value_size[i & 3u] = largest > 0.0f ? power2(14 - up) : 0.0f; poisoned[i & 3u] = any; }
-        else key_back[i & 3u] = power2(-up);
+        if (value) { value_size[i & 7u] = largest > 0.0f ? power2(14 - up) : 0.0f; poisoned[i & 7u] = any; }
+        else key_back[i & 7u] = power2(-up);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(pairs_full + 8 * b);
@@ -400,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     const uint32_t w = warp - 12, ut = tid - 384;
 #pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
-      const uint32_t b = i & 1u, s = i % kRawStages;
+      const uint32_t b = i & 1u, s = i % kRawStages, vs = i % kValues;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;
       bool fine = mbar_wait(pairs_full + 8 * b, (i >> 1) & 1u, waits) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
       fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
@@ -438,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
 
       // Values: a lane has two tokens, 16 apart (so that a warp's reads of the codes meet fewer banks twice; P's columns are in the same order), a warp J
       // words of them; a word becomes pairs in 8 coordinates' rows.
-      if (!__all_sync(0xffffffffu, i < 2 || mbar_wait(v_empty + 8 * b, ((i >> 1) - 1) & 1u, waits))) break;
+      if (!__all_sync(0xffffffffu, i < kValues || mbar_wait(v_empty + 8 * vs, (i / kValues - 1) & 1u, waits))) break;
       {
         const uint32_t token = (lane & 15u) + 2 * (lane & 16u);
         const int j = (int)(w * J) / 8;
@@ -446,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         const uint32_t pair0 = value_pair[b][token * J + j], pair1 = value_pair[b][(token + 16) * J + j];
         const uint32_t step = __byte_perm(pair0, pair1, 0x5410), lo = __byte_perm(pair0, pair1, 0x7632);
         const uint8_t* const src = raw + (token >> 4) * S::kTile + 9 * D + (j * 16 + (token & 15u)) * 32 + word0 * 4;
-        uint8_t* const to = mem + S::kAtV + b * S::kV + (lane & 3u) * 4;
+        uint8_t* const to = mem + S::kAtV + vs * S::kV + (lane & 3u) * 4;
         uint32_t c0[J], c1[J];
         if constexpr (J == 2) {
           const uint2 x = token < have ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
@@ -471,9 +498,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       }
       async_fence();
       __syncwarp();
-      if (lane == 0) { mbar_arrive(v_full + 8 * b); mbar_arrive(pairs_empty + 8 * b); mbar_arrive(raw_empty + 8 * s); }
+      if (lane == 0) { mbar_arrive(v_full + 8 * vs); mbar_arrive(pairs_empty + 8 * b); mbar_arrive(raw_empty + 8 * s); }
     }
   } else {                                                  // ---- softmax -----------------------------------------------------------
+    // A thread has a row; warps 4-7 take the even steps and warps 8-11 the odd ones, each with its own maximum, sum and O, joined at the end. (With
+    // two threads to a row at every step these warps were the ones that all others waited for: 2500 cycles a step, most of them the latencies of one
+    // step's chain from S to P.)
     const uint32_t quarter = warp & 3u, r = 32 * quarter + lane, side = (warp - 4) >> 2, lanes = (32 * quarter) << 16;
     const uint32_t twins = 1 + quarter;                     // named barrier of the two warps that share their rows
     const bool live = r < rows;
@@ -514,47 +544,41 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       if (lane == 0) mbar_arrive(q_full);
     }
 #pragma unroll 1
-    for (uint32_t i = 0; i < steps; ++i) {
-      const uint32_t b = i & 1u, first = i * kStep + 32 * side;
-      fine = fine && mbar_wait(v_full + 8 * b, (i >> 1) & 1u, waits) && mbar_wait(s_full + 8 * b, (i >> 1) & 1u, waits);
-      fine = __all_sync(0xffffffffu, fine);
+    for (uint32_t i = side; i < steps; i += 2) {
+      const uint32_t round = i >> 1, first = i * kStep;
+      fine = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * side, round & 1u, waits));        // (the keys are unpacked, so both kinds' pairs have been seen to)
+      if (!fine) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      float sc[32] = {};
-      if (fine) tmem_load32(tmem + b * kStep + 32 * side + lanes, sc);
-      const float scale = factor * key_back[i & 3u];
-      float size = value_size[i & 3u];
+      float sc[kStep];
+      tmem_load64(tmem + side * kStep + lanes, sc);
+      const float scale = factor * key_back[i & 7u];
+      float size = value_size[i & 7u];
       if (size == 0.0f) size = cap;                         // values that are all zero are of any size
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (fine && lane == 0) mbar_arrive(s_empty + 8 * b);
+      if (lane == 0) mbar_arrive(s_empty + 8 * side);
       // The largest of scale * s: with a negative scale it comes from the smallest.
-      const float turn = scale < 0.0f ? -1.0f : 1.0f;
-      float high = -INFINITY;
-      if (first + 32 <= see) {
-        if (scale < 0.0f) {
+      float times = fabsf(scale);
+      if (!(scale > 0.0f)) {
+        const float turn = scale < 0.0f ? -1.0f : scale;    // (a scale of zero: products of zero, from here on by a scale of one)
 #pragma unroll
-          for (int x = 0; x < 32; ++x) sc[x] = -sc[x];
-        }
-#pragma unroll
-        for (int x = 0; x < 32; ++x) high = fmaxf(high, sc[x]);
-        high *= fabsf(scale);
-      } else {
-#pragma unroll
-        for (int x = 0; x < 32; ++x) {
-          const bool seen = first + x < see;
-          sc[x] = seen ? sc[x] * turn : 0.0f;
-          high = seen ? fmaxf(high, sc[x] * fabsf(scale)) : high;
-        }
+        for (int x = 0; x < (int)kStep; ++x) sc[x] *= turn;
+        if (scale == 0.0f) times = 1.0f;
       }
-      if (poisoned[i & 3u]) {
+      if (first + kStep > see) {
+#pragma unroll
+        for (int x = 0; x < (int)kStep; ++x)
+          if (first + x >= see) sc[x] = -INFINITY;
+      }
+      float highs[4] = {sc[0], sc[1], sc[2], sc[3]};
+#pragma unroll
+      for (int x = 4; x < (int)kStep; ++x) highs[x & 3] = fmaxf(highs[x & 3], sc[x]);
+      float high = fmaxf(fmaxf(highs[0], highs[1]), fmaxf(highs[2], highs[3])) * times;
+      if (poisoned[i & 7u]) {
 #pragma unroll 1
-        for (uint32_t x = 0; x < 32; ++x)
-          if (first + x < see) nan_groups |= poison[i & 3u][32 * side + x];
+        for (uint32_t x = 0; x < kStep; ++x)
+          if (first + x < see) nan_groups |= poison[i & 7u][x];
       }
-      row_max[b][side][r] = high;                           // (two, so that a step's is read before the next but one writes it)
-      fine = meet(twins, fine);
-      if (!fine) break;                                     // both of them, after the same number of meetings
-      high = fmaxf(high, row_max[b][side ^ 1u][r]);
       if (high == -INFINITY) high = kNoMax;                 // nothing seen
       const bool raise = high > top + 8.0f || size > cap;
       float f = 1.0f;
@@ -570,76 +594,76 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       // taken for larger ones than they are rather than their p for zero.)
       int32_t shift = (int32_t)(__float_as_uint(size) >> 23) - (int32_t)(__float_as_uint(cap) >> 23) + 7;
       if (shift < -40) shift = -40;
-      const float times = fabsf(scale), off = (float)shift - top;
-      float sum = 0.0f;
-      uint32_t packed[16];                                  // tokens x and x + 16, as the values' columns
-      if (first + 32 <= see) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const float p0 = exp2_approx(fmaf(sc[x], times, off)), p1 = exp2_approx(fmaf(sc[x + 16], times, off));
-          sum += p0 + p1;
-          packed[x] = pack16<QSGD_TYPE_F16>(p0, p1);
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const float p0 = first + x < see ? exp2_approx(fmaf(sc[x], times, off)) : 0.0f;
-          const float p1 = first + x + 16 < see ? exp2_approx(fmaf(sc[x + 16], times, off)) : 0.0f;
-          sum += p0 + p1;
-          packed[x] = pack16<QSGD_TYPE_F16>(p0, p1);
-        }
-      }
-      l = fmaf(sum, power2(-shift), l);
-      // The product before this one reads P, and adds to O.
-      if (i) {
-        fine = __all_sync(0xffffffffu, fine && mbar_wait(pv, (i - 1) & 1u, waits));
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (fine && __any_sync(0xffffffffu, raise)) {
+      const float off = (float)shift - top;
+      // The product before this one of the same half reads the same buffer of P, and adds to the same O.
+      if (round) {
+        fine = __all_sync(0xffffffffu, mbar_wait_here(pv + 8 * side, (round - 1) & 1u, waits));
+        if (!fine) break;
+        if (__any_sync(0xffffffffu, raise)) {
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-          for (uint32_t c = side * (D / 2); c < (side + 1) * (D / 2); c += 32) {
-            float o[32];
-            tmem_load32(tmem_o + c + lanes, o);
+          for (uint32_t c = 0; c < D; c += 16) {            // (as many as find room in registers beside the scores)
+            float o[16];
+            tmem_load16(tmem_o + side * D + c + lanes, o);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] *= f;
-            tmem_store32(tmem_o + c + lanes, o);
+            for (int x = 0; x < 16; ++x) o[x] *= f;
+            tmem_store16(tmem_o + side * D + c + lanes, o);
           }
         }
       }
-      if (!fine) continue;                                  // to the next meeting
+      float sums[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (uint32_t c = 0; c < 4; ++c)
-        *reinterpret_cast<uint4*>(mem + S::kAtP + r * 128 + (((4 * side + c) ^ (r & 7u)) << 4)) =
-            make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+      for (uint32_t c = 0; c < 8; ++c) {                    // 16 bytes: tokens x and x + 16, as the values' columns
+        uint32_t packed[4];
+#pragma unroll
+        for (uint32_t y = 0; y < 4; ++y) {
+          const uint32_t x = 32 * (c >> 2) + 4 * (c & 3u) + y;
+          const float p0 = exp2_approx(fmaf(sc[x], times, off)), p1 = exp2_approx(fmaf(sc[x + 16], times, off));
+          sums[y & 1u] += p0 + p1;
+          packed[y] = pack16<QSGD_TYPE_F16>(p0, p1);
+        }
+        *reinterpret_cast<uint4*>(mem + S::kAtP + side * S::kP + r * 128 + ((c ^ (r & 7u)) << 4)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+      }
+      l = fmaf(sums[0] + sums[1], power2(-shift), l);
       async_fence();
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(p_full);
+      if (lane == 0) mbar_arrive(p_full + 8 * side);
     }
-    if (steps && fine) {
-      fine = __all_sync(0xffffffffu, mbar_wait(pv, (steps - 1) & 1u, waits));
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // Both halves' products are done; the halves' maxima, sums and sizes change hands. Each writes half of the coordinates.
+#pragma unroll
+    for (uint32_t b = 0; b < 2; ++b) {
+      const uint32_t turns = (steps + 1 - b) / 2;
+      if (turns) fine = fine && mbar_wait(pv + 8 * b, (turns - 1) & 1u, waits);
     }
-    // The row's sum: both halves', in the same order for both.
+    fine = __all_sync(0xffffffffu, fine);
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    row_max[side][r] = top;
     row_sum[side][r] = l;
+    row_cap[side][r] = cap;
     row_nan[side][r] = nan_groups;
     fine = meet(twins, fine);
-    l = row_sum[0][r] + row_sum[1][r];
+    const float high = fmaxf(row_max[0][r], row_max[1][r]), e0 = exp2_approx(row_max[0][r] - high), e1 = exp2_approx(row_max[1][r] - high);
+    l = fmaf(row_sum[0][r], e0, row_sum[1][r] * e1);        // (the same in both)
+    top = high;
     nan_groups = row_nan[0][r] | row_nan[1][r];
     if (fine && found) {
       const uint64_t row = (uint64_t)seq.start + query;
       uint16_t* const out = p.out + row * p.out_token + (uint64_t)hh * p.out_head;
       const bool saw = see != 0;
-      const float back = saw ? cap * power2(-21) / l : 0.0f;                // o is sum (p 2^7 size / cap) (v 2^14 / size)
+      // O is sum (p 2^7 size / cap) (v 2^14 / size). (The division first: a sum that is not divided may lie outside fp32, and 2^-21 cap below its range.)
+      const float w0 = e0 / l, w1 = e1 / l, back0 = row_cap[0][r] * power2(-21), back1 = row_cap[1][r] * power2(-21);
 #pragma unroll 1
-      for (uint32_t c = side * (D / 2); c < (side + 1) * (D / 2); c += 32) {
-        float o[32];
-        if (steps) tmem_load32(tmem_o + c + lanes, o);
+      for (uint32_t c = side * (D / 2); c < (side + 1) * (D / 2); c += 16) {
+        float o[16], o1[16] = {};
+        if (steps) tmem_load16(tmem_o + c + lanes, o);
+        if (steps > 1) tmem_load16(tmem_o + D + c + lanes, o1);
         if (live) {
           const float nan = nan_groups >> (c / 64) & 1u ? NAN : 0.0f;
 #pragma unroll
-          for (int x = 0; x < 32; ++x) o[x] = saw ? o[x] * back + nan : 0.0f;
+          for (int x = 0; x < 16; ++x) o[x] = saw ? o[x] * w0 * back0 + o1[x] * w1 * back1 + nan : 0.0f;
 #pragma unroll
-          for (int x = 0; x < 32; x += 8)
+          for (int x = 0; x < 16; x += 8)
             *reinterpret_cast<uint4*>(out + c + x) =
                 make_uint4(pack16<TYPE>(o[x], o[x + 1]), pack16<TYPE>(o[x + 2], o[x + 3]), pack16<TYPE>(o[x + 4], o[x + 5]), pack16<TYPE>(o[x + 6], o[x + 7]));
         }
@@ -654,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 0) {
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem));
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
   }
   if (tid == 0 && given_up) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
 }
