@@ -4,11 +4,12 @@
 // fp16, and both products run on the fifth-generation tensor cores, sums in tensor memory:
 //   S = Q K^T   128 rows x 64 tokens,   O += P V   128 rows x head_dim
 // A CTA has 128 rows of one (sequence, key head) and goes over its tokens 64 at a time:
-//   warp 0       brings the packed tiles in by bulk copies, three steps ahead
+//   warp 0       brings the packed tiles in by bulk copies, four steps ahead
 //   warp 1       issues the products (one thread)
 //   warps 2, 3   the (lo, step) pairs of the keys, of the values: their largest number, and the pairs in fp16
 //   warps 4-11   softmax: two threads to a row of S, 32 tokens each; P goes to shared memory; O is scaled in tensor memory when a maximum rises by 2^8
-//   warps 12-19  unpack: keys as rows of a token, values turned round (rows of a coordinate), 128-byte swizzle, two buffers each
+//   warps 12-15  unpack the keys as rows of a token, 128-byte swizzle, two buffers
+//   warps 16-19  unpack the values turned round (rows of a coordinate), three buffers
 // Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
 // likewise at 2^11; numbers 2^-28 below the largest of 64 tokens lose bits, which is less than fp32 sums lose. Roundings: k and v to 11 bits, p to 11
 // bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
@@ -23,7 +24,7 @@ namespace qsgd {
 
 namespace {
 
-constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 3, kValues = 3;
+constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 4, kPairs = 4, kValues = 3;
 constexpr uint32_t kMostSorted = 256;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 constexpr float kNoMax = -1.0e30f;
@@ -190,19 +191,19 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   constexpr int J = S::kGroups;
   constexpr int TYPE = QSGD_TYPE_BF16;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[2 * kRawStages + 2 * kValues + 17];
+  __shared__ uint64_t bars[2 * kRawStages + 2 * kValues + 2 * kPairs + 13];
   __shared__ uint64_t scan[kThreads / 32];
   __shared__ uint64_t found_base;
   __shared__ uint32_t found_b, tmem_base, given_up;
   __shared__ int32_t length_of[kMostSorted];
   __shared__ uint32_t order[kMostSorted];
   __shared__ float key_back[8], value_size[8];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
-  __shared__ uint2 key_pair[2][kStep * J];                 // (step, step), (lo, lo) in fp16
-  __shared__ uint32_t value_pair[2][kStep * J];            // step, lo
+  __shared__ uint2 key_pair[kPairs][kStep * J];                 // (step, step), (lo, lo) in fp16
+  __shared__ uint32_t value_pair[kPairs][kStep * J];            // step, lo
   __shared__ float row_max[2][kRows], row_sum[2][kRows], row_cap[2][kRows];
   __shared__ uint32_t row_nan[2][kRows];
   __shared__ uint8_t poison[8][kStep];                     // groups of a token's values that hold what is no number
-  __shared__ uint32_t poisoned[8];                         // (of eight steps: the pairs may be five ahead of the softmax)
+  __shared__ uint32_t poisoned[8];                         // (of eight steps: the pairs may be seven ahead of the softmax)
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
   const Waits waits{&given_up, p.polls};
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -210,11 +211,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t raw_full = bar0, raw_empty = raw_full + 8 * kRawStages, k_full = raw_empty + 8 * kRawStages, k_empty = k_full + 16,
                  v_full = k_empty + 16, v_empty = v_full + 8 * kValues, s_full = v_empty + 8 * kValues, s_empty = s_full + 16, p_full = s_empty + 16, pv = p_full + 16,
-                 q_full = pv + 16, pairs_full = q_full + 8, pairs_empty = pairs_full + 16;
+                 q_full = pv + 16, pairs_full = q_full + 8, pairs_empty = pairs_full + 8 * kPairs;
   if (tid == 0) {
     for (uint32_t s = 0; s < kRawStages; ++s) { mbar_init(raw_full + 8 * s, 1); mbar_init(raw_empty + 8 * s, kUnpackWarps); }
     for (uint32_t s = 0; s < 2; ++s) {
-      mbar_init(k_full + 8 * s, kUnpackWarps); mbar_init(k_empty + 8 * s, 1);
+      mbar_init(k_full + 8 * s, kUnpackWarps / 2); mbar_init(k_empty + 8 * s, 1);
       mbar_init(s_full + 8 * s, 1); mbar_init(s_empty + 8 * s, kSoftmaxWarps / 2);
     }
     for (uint32_t s = 0; s < 2; ++s) {
@@ -222,8 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       mbar_init(pv + 8 * s, 1);                             // a product P V is done
     }
     mbar_init(q_full, kSoftmaxWarps);
-    for (uint32_t s = 0; s < 2; ++s) { mbar_init(pairs_full + 8 * s, 2); mbar_init(pairs_empty + 8 * s, kUnpackWarps); }
-    for (uint32_t s = 0; s < kValues; ++s) { mbar_init(v_full + 8 * s, kUnpackWarps); mbar_init(v_empty + 8 * s, 1); }
+    for (uint32_t s = 0; s < kPairs; ++s) { mbar_init(pairs_full + 8 * s, 2); mbar_init(pairs_empty + 8 * s, kUnpackWarps); }
+    for (uint32_t s = 0; s < kValues; ++s) { mbar_init(v_full + 8 * s, kUnpackWarps / 2); mbar_init(v_empty + 8 * s, 1); }
     given_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -377,10 +378,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     const bool value = warp == 3;
 #pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
-      const uint32_t b = i & 1u, s = i % kRawStages;
+      const uint32_t b = i % kPairs, s = i % kRawStages;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;     // tokens of the step that some row sees
       bool fine = mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
-      fine = fine && (i < 2 || mbar_wait(pairs_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
+      fine = fine && (i < kPairs || mbar_wait(pairs_empty + 8 * b, (i / kPairs - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw + (value ? 17 : 8) * D;
       float largest = 0.0f;
@@ -424,70 +425,59 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       if (lane == 0) mbar_arrive(pairs_full + 8 * b);
     }
   } else if (warp >= 12) {                                  // ---- unpacking ---------------------------------------------------------
-    const uint32_t w = warp - 12, ut = tid - 384;
+    const bool value = warp >= 16;
 #pragma unroll 1
     for (uint32_t i = 0; i < steps; ++i) {
-      const uint32_t b = i & 1u, s = i % kRawStages, vs = i % kValues;
+      const uint32_t b = i & 1u, s = i % kRawStages, vs = i % kValues, ps = i % kPairs;
       const uint32_t first = i * kStep, have = see_any - first < kStep ? see_any - first : kStep;
-      bool fine = mbar_wait(pairs_full + 8 * b, (i >> 1) & 1u, waits) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
-      fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
+      bool fine = mbar_wait(pairs_full + 8 * ps, (i / kPairs) & 1u, waits) && mbar_wait(raw_full + 8 * s, (i / kRawStages) & 1u, waits);
+      if (value) fine = fine && (i < kValues || mbar_wait(v_empty + 8 * vs, (i / kValues - 1) & 1u, waits));
+      else fine = fine && (i < 2 || mbar_wait(k_empty + 8 * b, ((i >> 1) - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw;
-
-      // Keys: a thread has 2 J words (of 8 coordinates) of one token; a word becomes 16 bytes of the token's row, in the order that the queries
-      // have too (0 4 1 5 2 6 3 7).
-      {
-        const uint32_t token = ut & 63u, part = ut >> 6;
-        constexpr int kWords = 2 * J;                       // D / 8 words over 4 threads
+      if (!value) {
+        // Keys: a thread has half the words (of 8 coordinates) of one token; a word becomes 16 bytes of the token's row, in the order that the
+        // queries have too (0 4 1 5 2 6 3 7).
+        const uint32_t ut = tid - 384, token = ut & 63u, part = ut >> 6;
+        constexpr int kWords = D / 16;
         const int j = (int)(part * kWords) / 8;
         const uint32_t word0 = part * kWords - 8 * j;
-        const uint2 pair = key_pair[b][token * J + j];
-        uint32_t words[kWords];
+        const uint2 pair = key_pair[ps][token * J + j];
         const uint8_t* const src = raw + (token >> 4) * S::kTile + (j * 16 + (token & 15u)) * 32 + word0 * 4;
-        if constexpr (J == 2) {
-          const uint4 c = token < have ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-          words[0] = c.x; words[1] = c.y; words[2] = c.z; words[3] = c.w;
-        } else {
-          const uint2 c = token < have ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
-          words[0] = c.x; words[1] = c.y;
-        }
         uint8_t* const row = mem + S::kAtK + b * S::kK + j * (kStep * 128) + token * 128;
+        uint4 c[kWords / 4];
+#pragma unroll
+        for (int x = 0; x < kWords / 4; ++x) c[x] = token < have ? *reinterpret_cast<const uint4*>(src + 16 * x) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int x = 0; x < kWords; ++x) {
+          const uint4& q = c[x / 4];
           uint32_t v[4];
-          values_of(words[x], pair.x, pair.y, v);
+          values_of(x % 4 == 0 ? q.x : x % 4 == 1 ? q.y : x % 4 == 2 ? q.z : q.w, pair.x, pair.y, v);
           *reinterpret_cast<uint4*>(row + (((word0 + x) ^ (token & 7u)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-      }
-      async_fence();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(k_full + 8 * b);
-
-      // Values: a lane has two tokens, 16 apart (so that a warp's reads of the codes meet fewer banks twice; P's columns are in the same order), a warp J
-      // words of them; a word becomes pairs in 8 coordinates' rows.
-      if (!__all_sync(0xffffffffu, i < kValues || mbar_wait(v_empty + 8 * vs, (i / kValues - 1) & 1u, waits))) break;
-      {
-        const uint32_t token = (lane & 15u) + 2 * (lane & 16u);
-        const int j = (int)(w * J) / 8;
-        const uint32_t word0 = w * J - 8 * j;
-        const uint32_t pair0 = value_pair[b][token * J + j], pair1 = value_pair[b][(token + 16) * J + j];
+      } else {
+        // Values: a lane has two tokens, 16 apart (so that a warp's reads of the codes meet fewer banks twice; P's columns are in the same order), a
+        // warp a quarter of their words; a word becomes pairs in 8 coordinates' rows.
+        const uint32_t w = warp - 16, token = (lane & 15u) + 2 * (lane & 16u);
+        constexpr int kWords = 2 * J;
+        const int j = (int)(w * kWords) / 8;
+        const uint32_t word0 = w * kWords - 8 * j;
+        const uint32_t pair0 = value_pair[ps][token * J + j], pair1 = value_pair[ps][(token + 16) * J + j];
         const uint32_t step = __byte_perm(pair0, pair1, 0x5410), lo = __byte_perm(pair0, pair1, 0x7632);
         const uint8_t* const src = raw + (token >> 4) * S::kTile + 9 * D + (j * 16 + (token & 15u)) * 32 + word0 * 4;
         uint8_t* const to = mem + S::kAtV + vs * S::kV + (lane & 3u) * 4;
-        uint32_t c0[J], c1[J];
-        if constexpr (J == 2) {
-          const uint2 x = token < have ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
-          const uint2 y = token + 16 < have ? *reinterpret_cast<const uint2*>(src + S::kTile) : make_uint2(0u, 0u);
-          c0[0] = x.x; c0[1] = x.y; c1[0] = y.x; c1[1] = y.y;
-        } else {
-          c0[0] = token < have ? *reinterpret_cast<const uint32_t*>(src) : 0u;
-          c1[0] = token + 16 < have ? *reinterpret_cast<const uint32_t*>(src + S::kTile) : 0u;
-        }
+        uint2 c0[J], c1[J];
 #pragma unroll
         for (int x = 0; x < J; ++x) {
+          c0[x] = token < have ? *reinterpret_cast<const uint2*>(src + 8 * x) : make_uint2(0u, 0u);
+          c1[x] = token + 16 < have ? *reinterpret_cast<const uint2*>(src + S::kTile + 8 * x) : make_uint2(0u, 0u);
+        }
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) {
+          const uint32_t w0 = x % 2 ? c0[x / 2].y : c0[x / 2].x, w1 = x % 2 ? c1[x / 2].y : c1[x / 2].x;
           uint32_t front[4], behind[4];
-          values_of(__byte_perm(c0[x], c1[x], 0x5410), step, lo, front);
-          values_of(__byte_perm(c0[x], c1[x], 0x7632), step, lo, behind);
+          values_of(__byte_perm(w0, w1, 0x5410), step, lo, front);
+          values_of(__byte_perm(w0, w1, 0x7632), step, lo, behind);
           uint8_t* const row = to + (64 * j + 8 * (word0 + x)) * 128;
 #pragma unroll
           for (uint32_t y = 0; y < 4; ++y) {
@@ -498,7 +488,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       }
       async_fence();
       __syncwarp();
-      if (lane == 0) { mbar_arrive(v_full + 8 * vs); mbar_arrive(pairs_empty + 8 * b); mbar_arrive(raw_empty + 8 * s); }
+      if (lane == 0) {
+        mbar_arrive(value ? v_full + 8 * vs : k_full + 8 * b);
+        mbar_arrive(pairs_empty + 8 * ps);
+        mbar_arrive(raw_empty + 8 * s);
+      }
     }
   } else {                                                  // ---- softmax -----------------------------------------------------------
     // A thread has a row; warps 4-7 take the even steps and warps 8-11 the odd ones, each with its own maximum, sum and O, joined at the end. (With
