@@ -15,9 +15,12 @@
 // bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
 //
 // What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
-// of the special-function units, and about 5000 warp instructions, half of them unpacking: 2500 cycles, issue slots at half (tensor pipe 18 %). The step's roles
-// hand over eleven barriers, and their code is as large as the instruction cache: out-of-line waits alone took a step from 3000 to 2500 cycles.
-// Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 97 us, 0.32 PFLOP/s; by cache_attend.cu 204.
+// of the special-function units, and about 5000 warp instructions, half of them unpacking. It takes 1800 cycles (1500 at head size 64), and no role waits
+// for long: softmax warps 80 percent of the time at work, unpacking ones as much. What took it there from 2700: issuing warps that go round as a whole
+// (addresses in uniform registers; one lane by itself took 1250 cycles a step to issue and let P wait for 2200), softmax warps in two halves on
+// alternate steps, and buffers enough that neither waits for the other's last step. Waits out of line, since the roles' code together is as
+// large as the instruction cache (in line: 500 cycles more).
+// Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 77 us, 0.40 PFLOP/s; by cache_attend.cu 204.
 #include "cache.cuh"
 
 namespace qsgd {
@@ -95,6 +98,7 @@ __device__ __forceinline__ bool mbar_wait_here(uint32_t bar, uint32_t parity, co
   *w.given_up = 1;
   return false;
 }
+// One lane of a whole warp, the same each time.
 __device__ __forceinline__ bool elected() {
   uint32_t yes;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
@@ -712,9 +716,9 @@ int launch_wide(const WideParams& p, cudaStream_t stream) {
 }  // namespace
 
 // A CTA has a row tile for itself, and all of its tokens, so that few tiles leave SMs idle, while cache_attend.cu spreads any rows over all SMs. A round of
-// tiles over the SMs takes 57, 190 and 366 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
-// 46, 108 and 200 for 4096 rows in all heads, 70, 199 and 375 for 8192, and 115, 374 and 727 for 16384. At head size 64: 51, 175 and 338 against 42, 117
-// and 213 for 8192 rows, 68, 215 and 408 for 16384. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays.
+// tiles over the SMs takes 44, 133 and 248 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
+// 46, 109 and 200 for 4096 rows in all heads, 49, 123 and 224 for 4608, and 70, 199 and 375 for 8192. At head size 64: 34, 107 and 204 against 32, 75 and
+// 131 for 4608 rows, 42, 117 and 213 for 8192. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays.
 bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads) {
   if (type != QSGD_TYPE_BF16 || (head_dim != 64 && head_dim != 128) || !view.starts || !view.sequences) return false;
   const uint64_t rows = (uint64_t)view.rows * (q_heads / view.heads);        // of a key head
@@ -723,7 +727,7 @@ bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type,
   if ((head_dim == 64 ? look_up<64>(&sms) : look_up<128>(&sms)) || sms < 1) return false;
   const uint64_t each = (rows + view.sequences - 1) / view.sequences, tiles = (each + kRows - 1) / kRows * view.sequences * view.heads;
   const uint64_t room = (tiles + sms - 1) / sms * sms * kRows;
-  return rows * view.heads * 12 >= room * (head_dim == 64 ? 9 : 5);
+  return rows * view.heads * 24 >= room * (head_dim == 64 ? 10 : 7);
 }
 
 int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const AttendArgs& a, cudaStream_t stream) {

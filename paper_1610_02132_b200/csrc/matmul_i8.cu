@@ -74,6 +74,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   *w.given_up = 1;
   return false;
 }
+// One lane of a whole warp, the same each time.
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
@@ -175,62 +181,72 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_i8_kernel(const __grid_con
 
   const uint32_t tiles = g.m_tiles * g.n_tiles;
   if (warp == 0) {                                          // ---- fills the ring ------------------------------------------------
-    if (lane == 0) {
-      Ring r;
-      bool fine = true;
-      // Behind the library's own quantizing kernel: the first stages' rows of b are on their way before that has written a.
-      uint32_t ahead = 0;
-      if (g.early) {
-        uint32_t m, n;
-        tile_at(g, blockIdx.x, &m, &n);
-        for (; ahead < g.stages && ahead < g.k_steps; ++ahead) {
+    // (The whole warp goes round here and in the next role, so that addresses are in uniform registers, and one lane issues: 37 rows on 5000 x 2885
+    // take 10.2 us, 11.4 with one lane in the loops; 2048 on 8192 x 4096 take 52.9 and 53.7.)
+    Ring r;
+    bool fine = true;
+    // Behind the library's own quantizing kernel: the first stages' rows of b are on their way before that has written a.
+    uint32_t ahead = 0;
+    if (g.early) {
+      uint32_t m, n;
+      tile_at(g, blockIdx.x, &m, &n);
+      for (; ahead < g.stages && ahead < g.k_steps; ++ahead) {
+        if (elected()) {
           const uint32_t bar = full0 + 8 * ahead;
           mbar_expect(bar, stage_bytes);
           tma_load(ring0 + ahead * stage_bytes + g.a_bytes, &map_b, ahead * kBK, n * g.width, bar);
         }
-        chain_wait();
+        __syncwarp();
       }
-      for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x) {
-        uint32_t m, n;
-        tile_at(g, i, &m, &n);
-        for (uint32_t k = 0; k < g.k_steps; ++k) {
-          if (r.fills >= g.stages && !mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, waits)) { fine = false; break; }
+      chain_wait();
+    }
+    for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x) {
+      uint32_t m, n;
+      tile_at(g, i, &m, &n);
+      for (uint32_t k = 0; k < g.k_steps; ++k) {
+        if (r.fills >= g.stages && !__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * r.stage, r.parity ^ 1u, waits))) { fine = false; break; }
+        if (elected()) {
           const uint32_t at = ring0 + r.stage * stage_bytes, bar = full0 + 8 * r.stage;
           if (r.fills >= ahead) {
             mbar_expect(bar, stage_bytes);
             tma_load(at + g.a_bytes, &map_b, k * kBK, n * g.width, bar);
           }
           tma_load(at, &map_a, k * kBK, m * kBM, bar);
-          r.next(g.stages);
         }
-      }
-      // What is in flight lands before the CTA's shared memory goes away, whether anybody still waits for it or not.
-      for (uint32_t back = 1; back <= g.stages && back <= r.fills; ++back) {
-        const uint32_t fill = r.fills - back;
-        for (uint32_t t = 0; t < kDrainPolls && !mbar_try(full0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
+        __syncwarp();
+        r.next(g.stages);
       }
     }
+    // What is in flight lands before the CTA's shared memory goes away, whether anybody still waits for it or not.
+    for (uint32_t back = 1; back <= g.stages && back <= r.fills; ++back) {
+      const uint32_t fill = r.fills - back;
+      for (uint32_t t = 0; t < kDrainPolls && !mbar_try(full0 + 8 * (fill % g.stages), (fill / g.stages) & 1u); ++t) {}
+    }
   } else if (warp == 1) {                                   // ---- issues the products -------------------------------------------
-    if (lane == 0) {
+    {
       const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((g.width >> 3) << 17) | ((kBM >> 4) << 24);     // s32 += s8 * s8
       Ring r;
       uint32_t done = 0;
       bool fine = true;
       for (uint32_t i = blockIdx.x; i < tiles && fine; i += gridDim.x, ++done) {
         const uint32_t half = done & 1u, use = done >> 1;
-        if (use && !mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, waits)) { fine = false; break; }
+        if (use && !__all_sync(0xffffffffu, mbar_wait(sums_empty0 + 8 * half, (use - 1) & 1u, waits))) { fine = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (uint32_t k = 0; k < g.k_steps; ++k) {
-          if (!mbar_wait(full0 + 8 * r.stage, r.parity, waits)) { fine = false; break; }
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t at = ring0 + r.stage * stage_bytes;
-          const uint64_t a = tile_desc(at), b = tile_desc(at + g.a_bytes);
+          if (!__all_sync(0xffffffffu, mbar_wait(full0 + 8 * r.stage, r.parity, waits))) { fine = false; break; }
+          if (elected()) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = ring0 + r.stage * stage_bytes;
+            const uint64_t a = tile_desc(at), b = tile_desc(at + g.a_bytes);
 #pragma unroll
-          for (uint32_t x = 0; x < kBK / 32; ++x) mma_i8(tmem + half * kMostWidth, a + 2 * x, b + 2 * x, idesc, k != 0 || x != 0);
-          tc_commit(empty0 + 8 * r.stage);
+            for (uint32_t x = 0; x < kBK / 32; ++x) mma_i8(tmem + half * kMostWidth, a + 2 * x, b + 2 * x, idesc, k != 0 || x != 0);
+            tc_commit(empty0 + 8 * r.stage);
+          }
+          __syncwarp();
           r.next(g.stages);
         }
-        if (fine) tc_commit(sums_full0 + 8 * half);
+        if (fine && elected()) tc_commit(sums_full0 + 8 * half);
+        __syncwarp();
       }
       // After a wait that ran out: products in flight are done before tensor memory is freed.
       if (!fine && r.fills) {
