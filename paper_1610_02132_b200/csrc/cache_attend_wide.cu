@@ -514,8 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     }
   } else {                                                  // ---- softmax -----------------------------------------------------------
     // A thread has a row; warps 4-7 take the even steps and warps 8-11 the odd ones, each with its own maximum, sum and O, joined at the end. (With
-    // two threads to a row at every step these warps were the ones that all others waited for: 2500 cycles a step, most of them the latencies of one
-    // step's chain from S to P.)
+    // two threads to a row at every step each step waited for the latencies of the whole chain from S to P.)
     const uint32_t quarter = warp & 3u, r = 32 * quarter + lane, side = (warp - 4) >> 2, lanes = (32 * quarter) << 16;
     const uint32_t twins = 1 + quarter;                     // named barrier of the two warps that share their rows
     const bool live = r < rows;

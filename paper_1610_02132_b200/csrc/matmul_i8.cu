@@ -30,8 +30,10 @@ constexpr uint32_t kRingBytes = 4 * (kBM + kMostWidth) * kBK;
 // rows that are not there go nowhere), so there is that much room behind the last stage.
 constexpr uint32_t kSmem = kRingBytes + kBM * kBK + 1024;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
-// Up to here matmul_i8_few.cu: 16 rows of 16384 x 4096 take 19.0 us there and 21.6 here, 32 rows 36.5 and 16.8 (4096 x 4096: 7.9 and 16, 16 rows).
-constexpr uint32_t kFewRows = 16;
+// Up to kFewRows rows, and up to twice as many of small products, matmul_i8_few.cu, which has a tile of 8 rows read w once more: 32 rows of 16384 x 4096
+// take 36.5 us there and 15.5 here, 16 rows 19.2 and 15.9; 16 rows of 8192 x 8192 27.3 and 21.5, of 4096 x 8192 13.5 and 20.6, of 8192 x 4096 15.2
+// and 13.1, of 4096 x 4096 7.8 and 12.3, of 16384 x 1024 6.7 and 7.8.
+constexpr uint32_t kFewRows = 8, kLargeCols = 8192, kLargeDepth = 2048;
 
 struct GemmParams {
   MatmulArgs p;
@@ -395,7 +397,7 @@ bool matmul_i8_many_takes(const MatmulArgs& p) {
   // TMA: rows on 16-byte boundaries. Tiles are counted in 32 bits.
   const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | p.a_stride | p.b_stride) & 15u) == 0;
   const uint64_t tiles = (uint64_t)((p.m + kBM - 1) / kBM) * ((p.n + kLeastWidth - 1) / kLeastWidth);
-  return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > kFewRows;
+  return aligned && p.a_stride >= p.k && p.b_stride >= p.k && tiles < (1u << 30) && p.m > (p.n >= kLargeCols && p.k >= kLargeDepth ? kFewRows : 2 * kFewRows);
 }
 
 int launch_matmul_i8_many(const MatmulArgs& p, bool early, cudaStream_t stream) {

@@ -78,7 +78,7 @@ def operands(m, n, k, seed, padded=True):
 
 
 SHAPES = [(1, 1, 1), (1, 16, 64), (1, 17, 100), (7, 33, 65), (8, 100, 512), (9, 64, 1000), (16, 40, 31), (17, 300, 130), (33, 129, 2000), (64, 256, 128),
-          (65, 257, 129), (100, 96, 4096), (128, 128, 128), (129, 255, 200), (200, 1000, 700), (513, 384, 320), (1, 5000, 16)]
+          (65, 257, 129), (100, 96, 4096), (128, 128, 128), (129, 255, 200), (200, 1000, 700), (513, 384, 320), (1, 5000, 16), (9, 8200, 2100), (16, 8192, 2048)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -118,7 +118,8 @@ def test_nothing_to_multiply():
 
 
 @pytest.mark.parametrize("x_dtype, dtype", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float32, torch.float16)])
-@pytest.mark.parametrize("m, n, k", [(1, 64, 128), (1, 1000, 4096), (5, 33, 77), (40, 512, 1024), (150, 200, 999), (2, 16, 9000), (3, 50, 20000)])
+@pytest.mark.parametrize("m, n, k", [(1, 64, 128), (1, 1000, 4096), (5, 33, 77), (40, 512, 1024), (150, 200, 999), (2, 16, 9000), (3, 50, 20000), (11, 8200, 2100), (128, 64, 700),
+                                     (129, 64, 700)])
 def test_linear(m, n, k, x_dtype, dtype):
     x, w = normal((m, k), m + k, x_dtype).cuda(), normal((n, k), n) * k ** -0.5
     codes, w_scale = Q.quantize_rows_alloc(w.cuda())
