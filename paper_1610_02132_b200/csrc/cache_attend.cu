@@ -10,6 +10,8 @@
 //   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two that puts the largest step so far at 64
 //            (p may reach 2^8). For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
 //            For fp16 p * step goes as the sum of two fp16 numbers, since one would put as much error into the output as rounding it does.
+//            Both sums are held under that power of two, which no lo exceeds by more than 2^10 either, until they are divided: the values may
+//            be as large as their type has them, the undivided sums then lie outside fp32 (2 percent of the time).
 //            The codes are centred here because these sums run over the whole sequence: 8 sum(p step) would grow until what is left
 //            after taking it off at the end is the error of its rounded sums.
 // A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
@@ -21,7 +23,7 @@
 //
 // What bounds it: HBM holds 9/8 * head_dim bytes a token and head, each read once; issue slots and the integer pipe are nearly as busy (350 warp
 // instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 62 %, integer pipe 55 %, tensor pipe 22 %). 64 sequences of
-// 16000 tokens: 241 us, 4.9 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
+// 16000 tokens: 249 us, 4.7 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
 // So everything is arranged around the stream of tiles. The tiles of all (sequence, key
 // head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
 // takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
@@ -29,7 +31,7 @@
 // at most two parts a CTA, and a second kernel joins those. (With tiles dealt out to the eight warps of a CTA, which met at the end of each
 // segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 21: a CTA had up to 40 segments one after another.)
 // Few and short segments need no such line: a cluster of CTAs has one each and joins it over its shared memory (one user's step, 1000 tokens, with
-// the write in front of it: 13.5 us against 16).
+// the write in front of it: 12 us against 16).
 #include "cache.cuh"
 
 namespace qsgd {

@@ -16,7 +16,7 @@
 //
 // What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
 // of the special-function units, and about 5000 warp instructions, half of them unpacking. It takes 1800 cycles (1500 at head size 64), and no role waits
-// for long: softmax warps 80 percent of the time at work, unpacking ones as much. What took it there from 2700: issuing warps that go round as a whole
+// for long: softmax warps 80 percent of the time at work, unpacking ones as much; issue slots 65 percent, tensor pipe 27. What took it there from 2700: issuing warps that go round as a whole
 // (addresses in uniform registers; one lane by itself took 1250 cycles a step to issue and let P wait for 2200), softmax warps in two halves on
 // alternate steps, and buffers enough that neither waits for the other's last step. Waits out of line, since the roles' code together is as
 // large as the instruction cache (in line: 500 cycles more).
