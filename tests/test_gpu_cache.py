@@ -1,5 +1,6 @@
 """The 4-bit cache against its plain statement: bytes and values are equal, attention within the bounds of its roundings."""
 import math
+import random
 
 import pytest
 import torch
@@ -492,6 +493,54 @@ def test_given_stream_and_repeated_calls():
         Q.qsgd_cache_attend(f.cache, f.table, f.len, q, again, ws, f.status, stream=s)
         s.synchronize()
         assert torch.equal(again, out)
+
+
+def test_both_kernels_and_a_product_on_several_streams():
+    """Tiles of 128 rows of both head sizes, the line of units and an 8-bit layer side by side give what they give one after another."""
+    cases = [(Filled([900, 500], 16, 24, dim, BF16, seed=dim).write_all(), [100, 64], 96) for dim in (64, 128)]
+    cases.append((Filled([3000] * 4, 16, 8, 128, BF16, seed=3).write_all(), None, 32))
+    calls = []
+    for f, runs, heads in cases:
+        q = values((sum(runs) if runs else 4, heads, f.cache.head_dim), BF16, 7).cuda()
+        out, ws = torch.empty_like(q), torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, heads), dtype=torch.uint8, device="cuda")
+        starts = starts_of(runs) if runs else None
+        calls.append((out, lambda s, f=f, q=q, out=out, ws=ws, starts=starts: Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status,
+                                                                                                  starts=starts, stream=s)))
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randn(70, 2048, generator=g).to(BF16).cuda(), torch.randint(-127, 128, (3000, 2048), generator=g).to(torch.int8).cuda()
+    scale, y = torch.rand(3000, generator=g).cuda(), torch.empty(70, 3000, dtype=BF16, device="cuda")
+    space = torch.empty(Q.qsgd_linear_i8_workspace_bytes(70, 2048), dtype=torch.uint8, device="cuda")
+    calls.append((y, lambda s: Q.qsgd_linear_i8(x, w, scale, y, space, stream=s)))
+    for _, call in calls:
+        call(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    alone = [out.clone() for out, _ in calls]
+    for out, _ in calls:
+        out.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(20):
+        for s, (_, call) in zip(streams, calls):
+            call(s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, out) for a, (out, _) in zip(alone, calls))
+    for f, _, _ in cases:
+        f.fine()
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_attend_drawn_shapes(seed):
+    r = random.Random(seed)
+    dtype, dim, page = r.choice([BF16, BF16, FP16]), r.choice([64, 128, 192, 256]), r.choice([16, 32, 48, 64, 128])
+    heads, group, n = r.choice([1, 2, 3, 8, 16, 25, 40]), r.choice([1, 2, 3, 4, 5, 8, 12, 16]), r.choice([1, 2, 3, 5, 9])
+    lengths, most = [r.randint(0, r.choice([20, 100, 400, 1200])) for _ in range(n)], max(1, min(200, 40000 // (heads * group * n)))
+    runs = [r.randint(0, most) for _ in range(n - 1)] + [r.randint(1, most)]
+    f = Filled(lengths + [5], page, heads, dim, dtype, seed=seed).write_all()
+    torch.cuda.synchronize()
+    before = Q.qsgd_launch_count()
+    q, out, lse = run_attend(f, heads * group, runs + [1], dtype, seed=seed, rows=sum(runs) + 1 + r.randint(0, 3))
+    check(out, lse, q, f.k, f.v, 1 / math.sqrt(dim), lengths + [5], runs + [1], dtype, wide=Q.qsgd_launch_count() - before == 1)
+    assert bool((out[sum(runs) + 1:] == 42).all())
 
 
 def test_refusals():
