@@ -157,20 +157,21 @@ __device__ __forceinline__ void quantize_group(const uint4 (&raw)[2], uint32_t (
   if (near < span || (near == span && rest > 0.0f)) ++step_bits;
   else if (step_bits && (below > span || (below == span && rest <= 0.0f))) --step_bits;
   if (span < 15.0f * 1.1754943508222875e-38f) step_bits = 0;                // step below the smallest normal fp32: every code is 0
-  // Slightly too large on purpose (the approximation is off by 2^-23 at most): a quotient is rounded to its nearest code or to one too high, never
-  // too low. The remainder, exact in one fused operation, tells the two apart.
+  // Slightly too large on purpose (the approximation is off by 2^-23 at most, the difference by 2^-24): a quotient is rounded to its nearest code or to
+  // one too high, never too low. The border below that code tells the two apart: rounded down, since then a number of 24 bits or fewer lies above it
+  // exactly where it lies above lo + (code - 1/2) * step itself, however far apart the exponents of the three are.
   const float step = from_bits16<TYPE>(step_bits), inverse = step > 0.0f ? reciprocal(step) * (1.0f + 0x1p-21f) : 0.0f;
-  const float half = step > 0.0f ? -0.5f * step : -INFINITY;                // without a step no value leaves code 0
+  const float base = step > 0.0f ? lo : -INFINITY;          // without a step no value leaves code 0
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const uint32_t w[4] = {raw[x].x, raw[x].y, raw[x].z, raw[x].w};
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
-      const float d = from_bits16<TYPE>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu) - lo;
-      const float t = fmaf(d, inverse, kTwo23);             // 2^23 + the quotient, rounded to a whole number
-      const float r = fmaf(kTwo23 - t, step, d);
-      codes = codes * 16u + (__float_as_uint(t) - (r <= half ? 1u : 0u));
+      const float v = from_bits16<TYPE>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu);
+      const float t = fmaf(v - lo, inverse, kTwo23);        // 2^23 + the quotient, rounded to a whole number
+      const float border = __fmaf_rd((t - kTwo23) - 0.5f, step, base);
+      codes = codes * 16u + (__float_as_uint(t) - (v <= border ? 1u : 0u));
     }
     codes_out[x] = fine ? codes - 0xfb000000u : 0u;         // less the exponents of the 2^23, as far as they lie in 32 bits
   }
