@@ -213,19 +213,37 @@ __global__ void __launch_bounds__(kThreads, 3) cache_write_kernel(const __grid_c
   check_starts(a.c);
 }
 
-// Eight values of the group's type from a word of codes.
+// Whether lo + step * code may need more than the 24 bits of fp32: a number of the type is a multiple of 2^-bits of its size, so the sums are not
+// if all of them lie below 2^24 times the smaller multiple. (Not the case in ordinary groups: lo is zero or of the values' size.)
+template <int TYPE>
+__device__ __forceinline__ bool sums_are_long(uint32_t pair) {
+  const float lo = fabsf(from_bits16<TYPE>(pair & 0xffffu)), step = from_bits16<TYPE>(pair >> 16);
+  return lo > 0.0f && fmaf(16.0f, step, lo) > (TYPE == QSGD_TYPE_BF16 ? 65536.0f : 8192.0f) * fminf(lo, step);
+}
+
+// Eight values of the group's type from a word of codes, rounded once. ODD: by way of fp32 numbers rounded to odd, which keep on which side of a
+// number of the type, or of the middle between two, the sum lies.
+template <int TYPE, bool ODD>
+__device__ __forceinline__ uint4 expand_word(uint32_t word, float lo, float step) {
+  const uint32_t even = word & 0x0f0f0f0fu, odd = (word >> 4) & 0x0f0f0f0fu;
+  auto sum = [&](float code) {
+    if (!ODD) return fmaf(step, code, lo);                  // step * code is exact in fp32, and so is the sum
+    const float below = __fmaf_rd(step, code, lo), above = __fmaf_ru(step, code, lo);
+    return __float_as_uint(below) & 1u ? below : above;     // (the same where it is exact)
+  };
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float c0 = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 + j)) - kTwo23;         // 2^23 + code, less 2^23
+    const float c1 = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 + j)) - kTwo23;
+    o[j] = pack16<TYPE>(sum(c0), sum(c1));
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
 template <int TYPE>
 __device__ __forceinline__ uint4 expand(uint32_t word, uint32_t pair) {
   const float lo = from_bits16<TYPE>(pair & 0xffffu), step = from_bits16<TYPE>(pair >> 16);
-  const uint32_t even = word & 0x0f0f0f0fu, odd = (word >> 4) & 0x0f0f0f0fu;
-  uint32_t o[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {                             // step * code is exact in fp32: one rounding there, one to the type
-    const float c0 = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 + j)) - kTwo23;         // 2^23 + code, less 2^23
-    const float c1 = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 + j)) - kTwo23;
-    o[j] = pack16<TYPE>(fmaf(step, c0, lo), fmaf(step, c1, lo));
-  }
-  return make_uint4(o[0], o[1], o[2], o[3]);
+  return sums_are_long<TYPE>(pair) ? expand_word<TYPE, true>(word, lo, step) : expand_word<TYPE, false>(word, lo, step);
 }
 
 template <int TYPE, int J>

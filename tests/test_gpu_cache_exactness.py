@@ -1,5 +1,6 @@
-"""What the 4-bit cache holds, against rational numbers: the nearest code, where 32 bits do not hold the
-differences on the way."""
+"""What the 4-bit cache holds and gives back, against rational numbers: the nearest code and one rounding, where 32 bits do not hold the
+differences and sums on the way."""
+import math
 from fractions import Fraction
 
 import pytest
@@ -27,6 +28,22 @@ def group_of(x):
         step = next_number(step, x.dtype, -1)
     s = Fraction(step)
     return lo, s, [sum(1 for i in range(15) if e - lo > (i + Fraction(1, 2)) * s) for e in v]
+
+
+def rounded(v, dtype):
+    """A rational number as the nearest of the type, the even one of two as near."""
+    near = float(torch.tensor(float(v), dtype=torch.float64).to(dtype))
+    best = None
+    for by in (-1, 0, 1):
+        if near == 0 and by:
+            continue
+        c = next_number(near, dtype, by)
+        if not math.isfinite(c):
+            continue
+        odd = int(torch.tensor(c, dtype=dtype).view(torch.int16)) & 1
+        if best is None or (abs(Fraction(c) - v), odd) < best[0]:
+            best = (abs(Fraction(c) - v), odd), c
+    return best[1]
 
 
 def groups(dtype):
@@ -90,4 +107,38 @@ def test_codes_are_the_nearest(dtype, dim):
         pair = tile[token // 16, 8 * dim: 9 * dim].view(dtype).view(16, dim // 64, 2)[token % 16, j]
         assert Fraction(float(pair[0])) == lo and Fraction(float(pair[1])) == step
         wrong += [(i, n, a, b) for n, (a, b) in enumerate(zip(got, codes)) if a != b]
+    assert not wrong, wrong[:5]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_values_read_back_are_rounded_once(dtype):
+    """lo far below step: step * code between two numbers of the type, and lo, beyond 32 bits, says which."""
+    pairs = []
+    for step in (1.0078125, 1.4921875, 129 / 64, 1.1640625) if dtype == BF16 else (1.0009765625, 1025 / 512, 1.2490234375, 1.0029296875):
+        for lo in (2.0 ** -30, -2.0 ** -30, 2.0 ** -40, -2.0 ** -126, 0.0, 2.0 ** -12) if dtype == BF16 else (2.0 ** -24, -2.0 ** -24, 2.0 ** -14, 0.0):
+            for size in (1.0, 64.0, -1.0) if dtype == BF16 else (1.0, 512.0, -1.0):
+                if size > 0:
+                    pairs.append((lo, step * size))
+    pairs += [(3.0, 0.0), (-1.0, 2.0), (-0.125, 2.0 ** -9), (1000.0, 0.25)]
+    tokens = -(-len(pairs) // 16) * 16
+    cache = Q.Cache(1, tokens, 1, 64, dtype)
+    data = torch.zeros(tokens // 16, 18 * 64, dtype=torch.uint8)
+    for i, (lo, step) in enumerate(pairs):
+        tile, slot = divmod(i, 16)
+        codes = torch.arange(64) % 16
+        for at in (0, 576):
+            data[tile, at + slot * 32: at + slot * 32 + 32] = (codes[0::2] | codes[1::2] << 4).to(torch.uint8)
+            data[tile, at + 512 + 4 * slot: at + 516 + 4 * slot] = torch.tensor([lo, step], dtype=dtype).view(torch.uint8)
+    cache.data.copy_(data.view(1, 1, -1))
+    table, lengths = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    starts, status = torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), Q.new_status()
+    k, v = torch.zeros(2, tokens, 1, 64, dtype=dtype, device="cuda")
+    Q.qsgd_cache_read(cache, table, lengths, k, v, status, starts=starts)
+    assert int(status.item()) == 0 and torch.equal(k, v)
+    wrong = []
+    for i, (lo, step) in enumerate(pairs):
+        lo, step = (Fraction(float(torch.tensor(e, dtype=dtype))) for e in (lo, step))
+        want = [rounded(lo + step * (c % 16), dtype) for c in range(64)]
+        wrong += [(float(lo), float(step), c, a, b) for c, (a, b) in enumerate(zip(k[i, 0].tolist(), want)) if a != b]
     assert not wrong, wrong[:5]
