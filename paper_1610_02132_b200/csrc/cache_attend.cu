@@ -7,11 +7,14 @@
 //   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp16 operands, fp32 sums). A row of q is multiplied by a
 //            power of two that puts its largest number at 2^11: 16-bit numbers of either type fit fp16 then, but for what lies 2^-21 and more
 //            below the largest, which loses no more than fp32 sums do.
-//   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two that puts the largest step so far at 64
-//            (p may reach 2^8). For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
+//   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two, of each row and group by itself, that puts the
+//            largest p * step so far at 32 to 64 and is lowered only when one passes it by 2^9. It follows p * step and not step, each row's own:
+//            a group beside a much larger one, a row in front of much larger values that it does not see, or sees with little weight, keep their bits.
+//            (With one power of two for all, 2^24 between two groups' steps left nothing of the smaller one's output.)
+//            For a bf16 output 11 bits of p are enough: a rounding of 2^-12 at most, next to 2^-9 of the output's own.
 //            For fp16 p * step goes as the sum of two fp16 numbers, since one would put as much error into the output as rounding it does.
-//            Both sums are held under that power of two, which no lo exceeds by more than 2^10 either, until they are divided: the values may
-//            be as large as their type has them, the undivided sums then lie outside fp32 (2 percent of the time).
+//            Both sums are held under that power of two, which no p * lo exceeds by more than 2^10 either, until they are divided: the values may
+//            be as large as their type has them, the undivided sums then lie outside fp32.
 //            The codes are centred here because these sums run over the whole sequence: 8 sum(p step) would grow until what is left
 //            after taking it off at the end is the error of its rounded sums.
 // A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
@@ -49,7 +52,7 @@ constexpr uint32_t kMostCluster = 8, kMostDirect = 128;     // CTAs that share a
 constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kDrainPolls = 1u << 22;   // bound of the waits for copies in flight
-constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;     // 2^-120, 2^126
+constexpr float kLeastCap = 1.9259299443872359e-34f, kMostCap = 8.5070591730234616e+37f;     // 2^-112, 2^126
 constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that differences of maxima are numbers
 
 template <bool V>
@@ -170,25 +173,33 @@ __device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
   c[3] = v & 0x00f000f0u;
 }
 
-// The largest pair (as a number) whose step is not above a power of two.
 // Of either half by itself.
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// What a power of two is held against: the step of a pair, or 2^-10 of its lo.
 template <int TYPE>
-__device__ __forceinline__ uint32_t cap_bits(float cap) {
-  const float lo = cap * 1024.0f, most = TYPE == QSGD_TYPE_F16 ? 65504.0f : 3.3895314e38f;
-  return to_bits16<TYPE>(cap) << 16 | to_bits16<TYPE>(lo < most ? lo : most);
+__device__ __forceinline__ float size_of_pair(uint32_t pair) {
+  return fmaxf(from_bits16<TYPE>(pair >> 16), fabsf(from_bits16<TYPE>(pair & 0xffffu)) * (1.0f / 1024.0f));
 }
 
-// The same less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
 __device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// The largest pair (as a number) of that size.
+template <int TYPE>
+__device__ __forceinline__ uint32_t pair_of_size(float size) {
+  const float lo = size * 1024.0f, most = TYPE == QSGD_TYPE_F16 ? 65504.0f : 3.3895314e38f;
+  return to_bits16<TYPE>(size < most ? size : most) << 16 | to_bits16<TYPE>(lo < most ? lo : most);
+}
+// Of a power of two from 2^-126 to 2^126.
+__device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
+
+// The codes less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
 __device__ __forceinline__ void unpack_centred(uint32_t w, uint32_t (&c)[4]) {
   unpack(w, c);
   c[0] = add_f16x2(c[0], 0x80088008u);
@@ -278,6 +289,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
   __shared__ float cta_m[R], cta_l[R];                      // of the CTA's part of a segment that a cluster has
   __shared__ Rows part_rows[2][kWarps];
   __shared__ uint32_t late[kWarps];                         // a wait ran out
+  __shared__ __align__(8) uint32_t row_see[kWarps][R];      // tokens that a row sees, in front of the end of the warp's tiles
+  __shared__ uint32_t row_see_any[kWarps];                  // and that some row does
   __shared__ Span spans[kWarps + 1];
   __shared__ uint32_t n_spans;
   __shared__ uint32_t part_open[2][kWarps];                 // 0: no part; 1: the segment ends inside the warp's stretch; 2: it goes on
@@ -388,7 +401,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     // Tokens that the first row sees (all rows see them) and that the last row sees.
     const int64_t all = seq.length - (int64_t)(seq.n - 1 - row0 / p.group), any = seq.length - (int64_t)(seq.n - 1 - (row0 + rows - 1) / p.group);
     const uint32_t see_all = all > 0 ? (uint32_t)all : 0u;
-    uint32_t see_any = any > 0 ? (uint32_t)any : 0u;
+    const uint32_t see_any = any > 0 ? (uint32_t)any : 0u;
     uint32_t tile_end = (see_any + kCacheTile - 1) / kCacheTile;
     if (tile_end > tile1) tile_end = tile1;
     const uint32_t count = tile0 < tile_end ? tile_end - tile0 : 0u;
@@ -416,7 +429,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     // ---- queries: operands, sums of each group, and how far each row sees ------------------------------------------------
     uint32_t qf[NT][J][4][2];
     float qsum[NT][J][2], factor[NT][2];
-    int32_t see[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t r = 8 * nt + g;
@@ -474,21 +486,15 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         qsum[nt][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
         qsum[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
-#pragma unroll
-      for (int e2 = 0; e2 < 2; ++e2) {
-        const uint32_t rr = 8 * nt + 2 * t + e2;
-        const int64_t far = rr < rows ? seq.length - (int64_t)(seq.n - 1 - (row0 + rr) / p.group) : 0;
-        see[nt][e2] = far > 0 ? (int32_t)far : 0;
-      }
     }
-    // What lies behind the warp's tiles is not there to see, whatever the rows' own bounds are.
+    // How far each row sees; what lies behind the warp's tiles is not there to see. (Where only masked tiles look for it.)
     const uint32_t bound = tile_end * kCacheTile;
-    if (see_any > bound) see_any = bound;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if ((uint32_t)see[nt][e] > bound) see[nt][e] = (int32_t)bound;
+    if (lane < (uint32_t)R) {
+      const int64_t far = lane < rows ? seq.length - (int64_t)(seq.n - 1 - (row0 + lane) / p.group) : 0;
+      row_see[warp][lane] = far <= 0 ? 0u : far < (int64_t)bound ? (uint32_t)far : bound;
+      if (lane == 0) row_see_any[warp] = see_any < bound ? see_any : bound;
+    }
+    __syncwarp();
 
     float o[NT][J][4][4], lsum[NT][2], osum[NT][J][2], top[NT][2];
 #pragma unroll
@@ -504,8 +510,16 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     }
 
     // ---- the warp's tiles, two at a time -------------------------------------------------------------------------------
-    float cap = kLeastCap;                                  // power of two that no step so far exceeds, nor 2^-10 of any lo
-    uint32_t cap_pair = cap_bits<TYPE>(kLeastCap);          // the largest step and lo that do not
+    // Of each row and group: the power of two that p * step is multiplied by, and p * lo, until they are divided. It takes no p * step so far above 2^15,
+    // and no p * lo above 2^25. And for each group a pair (lo, step): tokens up to it need no look at their p, which is 2^8 at most.
+    float times[NT][J][2];
+    uint32_t known[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      known[j] = 0;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) times[nt][j][0] = times[nt][j][1] = 64.0f / kLeastCap;
+    }
     auto take_tiles = [&](auto masked_, const uint8_t* const tiles, const uint32_t first) {
       constexpr bool kMasked = decltype(masked_)::value;
       const uint32_t ka = token_of(g), kb = ka + 8;
@@ -547,8 +561,20 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
       }
 
       // ---- softmax, against a maximum that is raised only when a score passes it by 2^8 ----------------------------------
+      int32_t see[NT][2];                                                   // of the two tiles
+      uint32_t see_any = 0;
+      if (kMasked) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint2 both = *reinterpret_cast<const uint2*>(&row_see[warp][8 * nt + 2 * t]);
+          see[nt][0] = (int32_t)(both.x - first); see[nt][1] = (int32_t)(both.y - first);
+        }
+        see_any = row_see_any[warp];
+      }
       uint32_t seen = 0xffffffffu;                                          // bit 4 * (NT * h + nt) + e
-      uint32_t widest = 0;                                                  // the largest step and the largest lo (sign aside)
+      uint32_t widest[J];                                                   // the largest step and the largest lo (sign aside) of the lane's tokens
+#pragma unroll
+      for (int j = 0; j < J; ++j) widest[j] = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -556,7 +582,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             sc[h][nt][e] *= factor[nt][e & 1];
-            if (kMasked && (int32_t)(16 * h + (e < 2 ? ka : kb)) >= see[nt][e & 1] - (int32_t)first) {
+            if (kMasked && (int32_t)(16 * h + (e < 2 ? ka : kb)) >= see[nt][e & 1]) {
               seen &= ~(1u << (4 * (NT * h + nt) + e));
               sc[h][nt][e] = -INFINITY;
             }
@@ -566,30 +592,36 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (kMasked && first + 16 * h + (x ? kb : ka) >= see_any) pair[h][x][j] = 0;      // was never written, perhaps
-            widest = max_u16x2(widest, pair[h][x][j] & 0xffff7fffu);
+            widest[j] = max_u16x2(widest[j], pair[h][x][j] & 0xffff7fffu);
           }
       }
-      bool raise = widest >> 16 > cap_pair >> 16 || (widest & 0xffffu) > (cap_pair & 0xffffu);
+      bool raise = false, wider = false;
+#pragma unroll
+      for (int j = 0; j < J; ++j) wider |= max_u16x2(widest[j], known[j]) != known[j];
+      float high[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          raise |= fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2])) > top[nt][e] + 8.0f;
-      if (__any_sync(0xffffffffu, raise)) {
-        float step = 0.0f;                                  // (a step that is no number is passed over: its products are none anyway)
+        for (int e = 0; e < 2; ++e) {
+          high[nt][e] = fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2]));
+          raise |= high[nt][e] > top[nt][e] + 8.0f;
+        }
+      raise = __any_sync(0xffffffffu, raise || wider);
+      if (raise) {
+        // The lane's largest p times its largest size, which no p * size exceeds.
+        bool over = false;
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t w = pair[x >> 1][x & 1][j];
-            step = fmaxf(step, fmaxf(from_bits16<TYPE>(w >> 16), fabsf(from_bits16<TYPE>(w & 0xffffu)) * (1.0f / 1024.0f)));
+          for (int e = 0; e < 2; ++e) {
+            over |= high[nt][e] > top[nt][e] + 8.0f;
+            const float near = exp2_approx(high[nt][e] - top[nt][e] - 15.0f);
+#pragma unroll
+            for (int j = 0; j < J; ++j) over |= !(near * times[nt][j][e] * size_of_pair<TYPE>(widest[j]) <= 1.0f);      // (true of what is no number)
           }
-#pragma unroll
-        for (int m = 4; m < 32; m <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, m));
-        const uint32_t bits = (__float_as_uint(fminf(step, kMostCap)) + 0x007fffffu) & 0xff800000u;      // the next power of two
-        const float cap_new = fmaxf(cap, __uint_as_float(bits)), shrink = cap / cap_new;
-        cap = cap_new;
-        cap_pair = cap_bits<TYPE>(cap);
+        raise = __any_sync(0xffffffffu, over);
+      }
+      if (raise) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -599,16 +631,36 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
             m = fmaxf(m, top[nt][e]);
-            const float f = exp2_approx(top[nt][e] - m), fo = f * shrink;
+            const float f = exp2_approx(top[nt][e] - m);
             top[nt][e] = m;
             lsum[nt][e] *= f;
+            float p4[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p4[x] = exp2_approx(sc[x >> 1][nt][e + 2 * (x & 1)] - m);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
+              float size = 0.0f;                            // (what is no number is passed over: its products are none anyway)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) size = fmaxf(size, p4[x] * size_of_pair<TYPE>(pair[x >> 1][x & 1][j]));
+#pragma unroll
+              for (int i = 4; i < 32; i <<= 1) size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, i));
+              // The largest so far and now, as the next power of two, goes to 64.
+              const float held = f * 64.0f * inverse_of_power(times[nt][j][e]), least = fminf(fmaxf(fmaxf(held, size), kLeastCap), kMostCap);
+              const float cap = __uint_as_float((__float_as_uint(least) + 0x007fffffu) & 0xff800000u), inverse = inverse_of_power(cap);
+              const float fo = held * inverse;              // (1 at most)
+              times[nt][j][e] = 64.0f * inverse;
               osum[nt][j][e] *= fo;
 #pragma unroll
               for (int r = 0; r < 4; ++r) { o[nt][j][r][e] *= fo; o[nt][j][r][e + 2] *= fo; }
             }
           }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          float most = times[0][j][0];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) most = fmaxf(most, fmaxf(times[nt][j][0], times[nt][j][1]));
+          known[j] = pair_of_size<TYPE>(128.0f * inverse_of_power(most));          // 2^15 / 2^8
+        }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -621,7 +673,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         }
 
       // ---- output ---------------------------------------------------------------------------------------------------------
-      const float times = __uint_as_float((260u << 23) - __float_as_uint(cap));           // 64 / cap, a power of two
       const uint32_t va = token_of(2 * t), vb = token_of(2 * t + 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -629,14 +680,15 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const float step_a = from_bits16<TYPE>(pair[h][0][j] >> 16), step_b = from_bits16<TYPE>(pair[h][1][j] >> 16);
-          const float times_a = step_a * times, times_b = step_b * times;
-          const float mid_a = fmaf(8.0f, times_a, from_bits16<TYPE>(pair[h][0][j] & 0xffffu) * times);
-          const float mid_b = fmaf(8.0f, times_b, from_bits16<TYPE>(pair[h][1][j] & 0xffffu) * times);
+          const float mid_a = fmaf(8.0f, step_a, from_bits16<TYPE>(pair[h][0][j] & 0xffffu));
+          const float mid_b = fmaf(8.0f, step_b, from_bits16<TYPE>(pair[h][1][j] & 0xffffu));
           uint32_t bh[NT][2], bl[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const float* const pr = sc[h][nt];
-            float w[4] = {pr[0] * times_a, pr[1] * times_a, pr[2] * times_b, pr[3] * times_b};
+            float pr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[e] = sc[h][nt][e] * times[nt][j][e & 1];
+            float w[4] = {pr[0] * step_a, pr[1] * step_a, pr[2] * step_b, pr[3] * step_b};
             if (kMasked) {                                  // what a row does not see may hold anything: no product with it
               float z[4] = {pr[0] * mid_a, pr[1] * mid_a, pr[2] * mid_b, pr[3] * mid_b};
 #pragma unroll
@@ -703,7 +755,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     const uint32_t slot = from_front ? 1u : 0u;             // a part without the segment's front is the stretch's first, one with it the last
     const Rows which{head, row0, rows, seq.start};
     float* const mine = reinterpret_cast<float*>(slot ? ring : ring + S::kRingSpace);
-    const float held = cap * (1.0f / 64.0f);                // undoes the power of two in o and osum
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -733,6 +784,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
+          const float held = inverse_of_power(times[nt][j][e]);         // undoes the power of two in o and osum
           float z = osum[nt][j][e];
 #pragma unroll
           for (int m = 4; m < 32; m <<= 1) z += __shfl_xor_sync(0xffffffffu, z, m);
