@@ -35,6 +35,8 @@
 // segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 21: a CTA had up to 40 segments one after another.)
 // Few and short segments need no such line: a cluster of CTAs has one each and joins it over its shared memory (one user's step, 1000 tokens, with
 // the write in front of it: 12 us against 16).
+#include <float.h>
+
 #include "cache.cuh"
 
 namespace qsgd {
@@ -53,7 +55,7 @@ constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its til
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kDrainPolls = 1u << 22;   // bound of the waits for copies in flight
 constexpr float kLeastCap = 1.9259299443872359e-34f, kMostCap = 8.5070591730234616e+37f;     // 2^-112, 2^126
-constexpr float kNoMax = -1.0e30f;        // maximum of nothing: finite, so that differences of maxima are numbers
+constexpr float kNoMax = -FLT_MAX;        // maximum of nothing: below any score, and finite, so that differences of maxima are numbers
 
 template <bool V>
 struct Constant { static constexpr bool value = V; };
@@ -83,6 +85,9 @@ struct AttendParams {
   float scale_log2;
   uint32_t polls;                         // bound of the waits for tiles
   uint32_t direct;                        // CTAs, a cluster, to a segment (0: a line of units)
+  // A segment's parts go with their sums times 2^-part_lost, so that all of them add up to no more than the largest value. (One power of two for all, from
+  // the longest sequence that the table can name: with each part's own, in its maximum, scores of 2^27 left no room for it there.)
+  float part_lost, part_times;
   JoinInfo* join;
   float* parts;                           // [CTA][2][rows * (dim + 2)]
 };
@@ -273,7 +278,8 @@ __device__ __forceinline__ uint16_t* out_row(const AttendParams& p, const Rows& 
 }
 // A row that saw no token has no maximum and no sum.
 __device__ __forceinline__ bool saw(float m, float l) { return m > kNoMax || !(l == 0.0f); }
-__device__ __forceinline__ float log_sum(float m, float l) { return saw(m, l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
+// lost: the power of two that the sum lacks.
+__device__ __forceinline__ float log_sum(float m, float l, float lost) { return saw(m, l) ? (m + (lost + log2f(l))) * 0.69314718055994531f : -INFINITY; }
 
 template <int TYPE, int D, int NT>
 __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_attend_kernel(const __grid_constant__ AttendParams p) {
@@ -769,16 +775,13 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         if (whole) {
           if (r < rows) {
             out = out_row(p, which, r, &lse_at);
-            if (p.lse && g == 0) p.lse[lse_at] = log_sum(top[nt][e], l);
+            if (p.lse && g == 0) p.lse[lse_at] = log_sum(top[nt][e], l, 0.0f);
             over = saw(top[nt][e], l) ? 1.0f / l : 0.0f;
           }
         } else {
-          // A part goes with its sum between 2^-12 and 2^-11, the power of two in its maximum, so that 2^11 of them add up to no more than the
-          // largest value.
-          const int32_t up = l > 0.0f && l < INFINITY ? (int32_t)(__float_as_uint(l) >> 23) - 127 + 12 : 0;
-          over = __uint_as_float((uint32_t)(127 - up) << 23);
+          over = p.part_times;
           if (g == 0) {
-            part_m[slot][warp][r] = top[nt][e] + (float)up;
+            part_m[slot][warp][r] = top[nt][e];
             part_l[slot][warp][r] = l * over;
           }
         }
@@ -850,7 +853,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
       uint16_t* const out = out_row(p, which, r, &lse_at);
       const float over = saw(m, l) ? 1.0f / l : 0.0f;
       *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
-      if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
+      if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l, p.part_lost);
     } else if (p.direct) {                                  // where the cluster's other CTAs look for it: nobody else's part, or this very place's
       *reinterpret_cast<float4*>(smem + S::kRingSpace + (r * S::kRowFloats + 4 * d4) * 4) = sum;
       if (d4 == 0) { cta_m[r] = m; cta_l[r] = l; }
@@ -895,7 +898,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
     uint16_t* const out = out_row(p, which, r, &lse_at);
     const float over = saw(m, l) ? 1.0f / l : 0.0f;
     *reinterpret_cast<uint2*>(out + 4 * d4) = make_uint2(pack16<TYPE>(sum.x * over, sum.y * over), pack16<TYPE>(sum.z * over, sum.w * over));
-    if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l);
+    if (p.lse && d4 == 0) p.lse[lse_at] = log_sum(m, l, p.part_lost);
   }
   cluster_barrier();                                        // no CTA leaves while another reads its shared memory
 }
@@ -940,7 +943,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const __grid_c
     uint64_t lse_at;
     uint16_t* const out = out_row(p, j.rows, r, &lse_at);
     out[threadIdx.x] = (uint16_t)to_bits16<TYPE>(saw(m, l) ? v / l : 0.0f);
-    if (p.lse && threadIdx.x == 0) p.lse[lse_at] = log_sum(m, l);
+    if (p.lse && threadIdx.x == 0) p.lse[lse_at] = log_sum(m, l, p.part_lost);
   }
 }
 
@@ -1014,6 +1017,12 @@ int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, cons
   p.group = a.q_heads / view.heads;
   p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
   p.polls = quantize_poll_limit();
+  // p is 2^8 at most, against each part's maximum.
+  const uint64_t longest = (uint64_t)view.table_pages * view.page_tiles * kCacheTile;
+  int lost = 9;
+  while (lost < 40 && longest >> (lost - 9)) ++lost;
+  p.part_lost = (float)lost;
+  p.part_times = ldexpf(1.0f, -lost);
   p.join = reinterpret_cast<JoinInfo*>(a.workspace);
   p.parts = reinterpret_cast<float*>(a.workspace + kMostCtas * sizeof(JoinInfo));
   // 16 rows to a tile where a sequence has more than 8 on average: the codes are unpacked half as often.

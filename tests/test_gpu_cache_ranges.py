@@ -151,3 +151,25 @@ def test_tokens_of_very_different_sizes_in_chunks(what, large, heads):
     assert (Q.qsgd_launch_count() - before == 1) == (heads == 148)
     f.fine()
     compare(f, q, out, lse, 0.25, [100], BF16, tile=heads == 148)
+
+
+@pytest.mark.parametrize("lengths, runs, heads, one", [([500], [1], 1, True), ([9000], [1], 1, True), ([300], [40], 2, False)])
+def test_scores_far_below_zero(lengths, runs, heads, one):
+    """All scores lower than any that a fixed number would stand for: the highest one still takes all."""
+    f = Filled(lengths, 16, heads, 128, BF16)
+    f.k[0][:] = -1e18
+    f.k[0][::7] = -0.99e18                                  # (one group's worth of the same number: held as it is)
+    f.write_all()
+    rows = sum(runs)
+    q = torch.full((rows, heads, 128), 1e15, dtype=BF16, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(rows, heads, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, heads), dtype=torch.uint8, device="cuda")
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=None if one else starts_of(runs), lse=lse)
+    f.fine()
+    v = F.held_value(f.v[0])
+    for i in range(rows):
+        n = lengths[0] - rows + i + 1
+        want, size = v[0:n:7].mean(0), v[0:n:7].abs().mean(0)
+        off = (out[i].double().cpu() - want).abs()
+        assert bool((off <= F.HALF_STEP[BF16] * want.abs() + 2.0 ** -10 * size + 2.0 ** -11 * 8 * 0.5).all())
+        assert bool(((lse[i].double().cpu() / (-0.9881e18 * 128 * 9.99e14 / math.sqrt(128)) - 1).abs() < 0.01).all())
