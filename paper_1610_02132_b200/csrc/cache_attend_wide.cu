@@ -641,19 +641,20 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       __syncwarp();
       if (lane == 0) mbar_arrive(p_full + 8 * side);
     }
-    // Both halves' products are done; the halves' maxima, sums and sizes change hands. Each writes half of the coordinates.
-#pragma unroll
-    for (uint32_t b = 0; b < 2; ++b) {
-      const uint32_t turns = (steps + 1 - b) / 2;
-      if (turns) fine = fine && mbar_wait(pv + 8 * b, (turns - 1) & 1u, waits);
-    }
+    // A half waits for its own products, whose phases it has followed: of the other half's it has seen none, and a wait for a phase by its parity is over at
+    // once when an earlier one of the same parity is. That those are done it learns from its twins at the barrier, where the halves' maxima, sums and
+    // sizes change hands, too. Each writes half of the coordinates.
+    const uint32_t turns = (steps + 1 - side) / 2;
+    if (turns) fine = fine && mbar_wait(pv + 8 * side, (turns - 1) & 1u, waits);
     fine = __all_sync(0xffffffffu, fine);
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     row_max[side][r] = top;
     row_sum[side][r] = l;
     row_cap[side][r] = cap;
     row_nan[side][r] = nan_groups;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     fine = meet(twins, fine);
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const float high = fmaxf(row_max[0][r], row_max[1][r]), e0 = exp2_approx(row_max[0][r] - high), e1 = exp2_approx(row_max[1][r] - high);
     l = fmaf(row_sum[0][r], e0, row_sum[1][r] * e1);        // (the same in both)
     top = high;

@@ -173,3 +173,23 @@ def test_scores_far_below_zero(lengths, runs, heads, one):
         off = (out[i].double().cpu() - want).abs()
         assert bool((off <= F.HALF_STEP[BF16] * want.abs() + 2.0 ** -10 * size + 2.0 ** -11 * 8 * 0.5).all())
         assert bool(((lse[i].double().cpu() / (-0.9881e18 * 128 * 9.99e14 / math.sqrt(128)) - 1).abs() < 0.01).all())
+
+
+@pytest.mark.parametrize("n", [1, 40, 64, 65, 128, 150, 192, 200, 256, 300, 330, 400, 449, 520])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_every_number_of_steps_in_chunks(n, dim):
+    """One to nine steps of 64 tokens: the two halves of a tile's softmax have as many, or one has one more. Each ten times, to the bit."""
+    f = Filled([n], 16, 296, dim, BF16).write_all()
+    runs = [min(n, 128)] if n >= 100 else [128]             # (more rows than tokens: the first see nothing)
+    q, out, lse, launches = launched(f, 296, runs, BF16)
+    assert launches == 1
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 296), dtype=torch.uint8, device="cuda")
+    for _ in range(10):
+        again = torch.empty_like(out)
+        Q.qsgd_cache_attend(f.cache, f.table, f.len, q, again, ws, f.status, starts=starts_of(runs))
+        assert torch.equal(out, again)
+    some = [0, 73, 295]                                     # of the heads
+    rows = runs[0] - max(0, runs[0] - n)
+    f.k, f.v = [x[:, some] for x in f.k], [x[:, some] for x in f.v]
+    compare(f, q[-rows:, some], out[-rows:, some], lse[-rows:, some], 1 / math.sqrt(dim), [rows], BF16, tile=True)
+    assert bool((out[:-rows] == 0).all()) and bool((lse[:-rows] == -math.inf).all())
