@@ -31,7 +31,7 @@ constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kS
 constexpr uint32_t kMostSorted = 256;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 constexpr float kNoMax = -1.0e30f;
-constexpr float kLeastCap = 7.5231638452626401e-37f;       // 2^-120
+constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;      // 2^-120, 2^126
 
 struct WideParams {
   CacheView c;
@@ -166,6 +166,8 @@ __device__ __forceinline__ int32_t lift(float largest, int32_t put) {
   const int32_t up = put - e;
   return up > 120 ? 120 : up;
 }
+__device__ __forceinline__ float power_above(float v) { return __uint_as_float((__float_as_uint(v) + 0x007fffffu) & 0xff800000u); }
+__device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }      // of 2^-126 to 2^126
 __device__ __forceinline__ float power2(int32_t e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
@@ -591,20 +593,26 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
           if (first + x < see) nan_groups |= poison[i & 7u][x];
       }
       if (high == -INFINITY) high = kNoMax;                 // nothing seen
-      const bool raise = high > top + 8.0f || size > cap;
+      // cap, a power of two of the row's own, follows its largest p * size: what it does not see, or hardly weighs, does not count.
+      const bool higher = high > top + 8.0f;
+      const float most = higher ? size : exp2_approx(high - top - 8.0f) * size;       // (2^-8 of the largest where the maximum stays: p is 2^8 at most)
+      const bool raise = higher || most > cap;
       float f = 1.0f;
       if (raise) {
-        const float new_top = fmaxf(top, high), new_cap = fmaxf(cap, size);
-        f = exp2_approx(top - new_top);
-        l *= f;
-        f *= cap / new_cap;
-        top = new_top;
-        cap = new_cap;
+        float held = cap;
+        if (higher) {
+          f = exp2_approx(top - high);
+          l *= f;
+          held *= f;
+          top = high;
+        }
+        cap = power_above(fminf(fmaxf(fmaxf(held, higher ? most : 256.0f * most), kLeastCap), kMostCap));
+        f = held * inverse_of_power(cap);                   // (1 at most)
       }
-      // P holds p * 2^7 * size / cap: at most 2^15, and 2^-14, where fp16 begins to lose bits, for p = 2^-21. (Values 2^-40 below the largest are
-      // taken for larger ones than they are rather than their p for zero.)
+      // P holds p * 2^7 * size / cap: at most 2^15, and 2^-14, where fp16 begins to lose bits, for p * size = 2^-21 * cap. (Below 2^-60 p itself would
+      // leave fp32; P is zero long before.)
       int32_t shift = (int32_t)(__float_as_uint(size) >> 23) - (int32_t)(__float_as_uint(cap) >> 23) + 7;
-      if (shift < -40) shift = -40;
+      if (shift < -60) shift = -60;
       const float off = (float)shift - top;
       // The product before this one of the same half reads the same buffer of P, and adds to the same O.
       if (round) {
@@ -635,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
         }
         *reinterpret_cast<uint4*>(mem + S::kAtP + side * S::kP + r * 128 + ((c ^ (r & 7u)) << 4)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
       }
-      l = fmaf(sums[0] + sums[1], power2(-shift), l);
+      l = fmaf(sums[0] + sums[1], power2(shift < 126 ? -shift : -126), l);       // (from there on p is nothing beside l)
       async_fence();
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();

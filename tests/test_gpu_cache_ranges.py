@@ -193,3 +193,25 @@ def test_every_number_of_steps_in_chunks(n, dim):
     f.k, f.v = [x[:, some] for x in f.k], [x[:, some] for x in f.v]
     compare(f, q[-rows:, some], out[-rows:, some], lse[-rows:, some], 1 / math.sqrt(dim), [rows], BF16, tile=True)
     assert bool((out[:-rows] == 0).all()) and bool((lse[:-rows] == -math.inf).all())
+
+
+@pytest.mark.parametrize("heads", [2, 148])
+@pytest.mark.parametrize("large", [2.0 ** 30, 2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("weight", [1, 2])
+@pytest.mark.parametrize("place", [0, 128])
+def test_large_values_of_little_weight_in_chunks(large, weight, place, heads):
+    """64 tokens of large values in one stretch, with weights of about 1 / large, or its square."""
+    f = Filled([333], 16, heads, 128, BF16)
+    some = slice(place, place + 64)
+    f.k[0].mul_(0.1)
+    f.k[0][some] = -weight * math.log(large) / 32
+    f.v[0][some] = (f.v[0][some].float() * large).to(BF16)
+    f.write_all()
+    q = values((100, heads, 128), BF16, 3).abs().clamp(0.5, 1.5).cuda()
+    out, lse = torch.empty_like(q), torch.empty(100, heads, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, heads), dtype=torch.uint8, device="cuda")
+    before = Q.qsgd_launch_count()
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts_of([100]), scale=0.25, lse=lse)
+    assert (Q.qsgd_launch_count() - before == 1) == (heads == 148)
+    f.fine()
+    compare(f, q, out, lse, 0.25, [100], BF16, tile=heads == 148)
