@@ -54,6 +54,15 @@ int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const Att
 
 int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, const AttendArgs& args, cudaStream_t stream);
 
+// The power of two that sums of p v have to lose so that they stay in fp32 whatever the values are, p being 2^8 at most: from the longest sequence
+// that the table can name.
+inline int attend_sums_lose(const CacheView& view) {
+  const uint64_t longest = (uint64_t)view.table_pages * view.page_tiles * kCacheTile;
+  int lost = 9;
+  while (lost < 40 && longest >> (lost - 9)) ++lost;
+  return lost;
+}
+
 #ifdef __CUDACC__
 // Pattern of a 16-bit number <-> fp32.
 template <int TYPE>

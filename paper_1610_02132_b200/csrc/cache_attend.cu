@@ -1017,10 +1017,7 @@ int launch_cache_attend(const CacheView& view, uint32_t head_dim, int type, cons
   p.group = a.q_heads / view.heads;
   p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
   p.polls = quantize_poll_limit();
-  // p is 2^8 at most, against each part's maximum.
-  const uint64_t longest = (uint64_t)view.table_pages * view.page_tiles * kCacheTile;
-  int lost = 9;
-  while (lost < 40 && longest >> (lost - 9)) ++lost;
+  const int lost = attend_sums_lose(view);                  // (p against each part's maximum)
   p.part_lost = (float)lost;
   p.part_times = ldexpf(1.0f, -lost);
   p.join = reinterpret_cast<JoinInfo*>(a.workspace);

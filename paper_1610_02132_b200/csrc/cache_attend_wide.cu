@@ -11,8 +11,11 @@
 //   warps 12-15  unpack the keys as rows of a token, 128-byte swizzle, two buffers
 //   warps 16-19  unpack the values turned round (rows of a coordinate), three buffers
 // Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
-// likewise at 2^11; numbers 2^-28 below the largest of 64 tokens lose bits, which is less than fp32 sums lose. Roundings: k and v to 11 bits, p to 11
-// bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through cache_attend.cu.)
+// likewise at 2^11; P holds p times a power of two of each row that follows its own largest p * v. Numbers 2^-28 below the largest of 64 tokens lose bits.
+// Where that is more than the rounding to 11 bits (a key, or a group of values, much smaller than another of the same step: each is a score, or an output, of
+// its own, and a row need not see the other) or scores are so large that a power of two beside them is lost, the tile is done again in fp32: attend_plainly.
+// Roundings: k and v to 11 bits, p to 11 bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through
+// cache_attend.cu.)
 //
 // What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
 // of the special-function units, and about 5000 warp instructions, half of them unpacking. It takes 1800 cycles (1500 at head size 64), and no role waits
@@ -21,6 +24,8 @@
 // alternate steps, and buffers enough that neither waits for the other's last step. Waits out of line, since the roles' code together is as
 // large as the instruction cache (in line: 500 cycles more).
 // Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 77 us, 0.40 PFLOP/s; by cache_attend.cu 204.
+#include <float.h>
+
 #include "cache.cuh"
 
 namespace qsgd {
@@ -30,7 +35,10 @@ namespace {
 constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kSoftmaxWarps = 8, kRawStages = 4, kPairs = 4, kValues = 3;
 constexpr uint32_t kMostSorted = 256;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
-constexpr float kNoMax = -1.0e30f;
+constexpr float kNoMax = -FLT_MAX;                         // maximum of nothing: below any score, and finite, so that differences of maxima are numbers
+// What the tiles' 11 bits and common powers of two are good for; a tile with more goes through attend_plainly. A step's largest key next to its smallest one
+// (its number of the largest size; keys of zeros aside), its largest group of values next to its smallest, the largest value at all, the size of a score.
+constexpr float kKeyRange = 65536.0f, kValueRange = 4096.0f, kMostValue = 8.5070591730234616e+37f, kMostScore = 8192.0f;
 constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;      // 2^-120, 2^126
 
 struct WideParams {
@@ -42,6 +50,7 @@ struct WideParams {
   uint32_t q_heads, group;
   float scale_log2;
   uint32_t polls;              // bound of the roles' waits
+  float times, back;           // for sums of p v in fp32: 2^-lost and 2^lost
 };
 
 template <int D>
@@ -196,6 +205,83 @@ __device__ __forceinline__ void values_of(uint32_t w, uint32_t step, uint32_t lo
   v[3] = fma_f16x2(sub_f16x2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u), step, lo);
 }
 
+// A tile's rows token by token in fp32, four rows to a warp: for tiles whose numbers differ too much in size. Keys and values are halved or smaller on the
+// way, since lo + 15 * step may lie outside fp32. (Four chunks of 256 queries over 4096 tokens, all tiles this way: 11 ms against 0.15. Ordinary models'
+// keys and values lie within a factor of a hundred.)
+template <int D>
+__device__ __noinline__ void attend_plainly(const WideParams& p, const SequenceRows& seq, uint32_t b, uint32_t head, uint32_t row0, uint32_t rows) {
+  constexpr int TYPE = QSGD_TYPE_BF16, V = D / 32, J = D / 64, kTogether = 4;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, j = lane * V / 64, byte = lane * V % 64 / 2;
+#pragma unroll 1
+  for (uint32_t r0 = warp * kTogether; r0 < rows; r0 += kThreads / 32 * kTogether) {
+    float q[kTogether][V], o[kTogether][V], top[kTogether], l[kTogether];
+    uint32_t see[kTogether], most = 0;
+#pragma unroll
+    for (int x = 0; x < kTogether; ++x) {
+      const bool live = r0 + x < rows;
+      const uint32_t query = (row0 + r0 + x) / p.group, hh = head * p.group + (row0 + r0 + x) - query * p.group;
+      const int64_t far = live ? seq.length - (int64_t)(seq.n - 1 - query) : 0;
+      see[x] = far > 0 ? (uint32_t)far : 0u;
+      most = see[x] > most ? see[x] : most;
+      const uint16_t* const src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)hh * p.q_head + lane * V;
+#pragma unroll
+      for (int y = 0; y < V; ++y) { q[x][y] = live ? from_bits16<TYPE>(__ldg(src + y)) : 0.0f; o[x][y] = 0.0f; }
+      top[x] = kNoMax;
+      l[x] = 0.0f;
+    }
+#pragma unroll 1
+    for (uint32_t t0 = 0; t0 < most; t0 += kCacheTile) {
+      const uint32_t tile = t0 / kCacheTile, page = tile / p.c.page_tiles;
+      int32_t at = __ldg(p.c.table + (uint64_t)b * p.c.table_stride + page);
+      if (at < 0 || (uint32_t)at >= p.c.n_pages) at = 0;    // (said by the role that brings the tiles in)
+      const uint8_t* const held = p.c.data + (uint64_t)at * p.c.page_stride + (uint64_t)head * p.c.head_stride +
+                                  (uint64_t)(tile - page * p.c.page_tiles) * Shape<D>::kTile;
+      const uint32_t end = most - t0 < kCacheTile ? most - t0 : kCacheTile;
+#pragma unroll 2
+      for (uint32_t slot = 0; slot < end; ++slot) {
+        float kv[2][V];                                     // half a key, and p.times a value
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+          const uint8_t* const part = held + side * 9 * D;
+          const uint32_t pair = __ldg(reinterpret_cast<const uint32_t*>(part + 8 * D) + slot * J + j);
+          const uint8_t* const codes = part + (j * 16 + slot) * 32 + byte;
+          const uint32_t word = V == 4 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(codes)) : (uint32_t)__ldg(codes);
+          const float by = side ? p.times : 0.5f, lo = from_bits16<TYPE>(pair & 0xffffu) * by, step = from_bits16<TYPE>(pair >> 16) * by;
+#pragma unroll
+          for (int y = 0; y < V; ++y) kv[side][y] = fmaf(step, (float)((word >> (4 * y)) & 15u), lo);
+        }
+#pragma unroll
+        for (int x = 0; x < kTogether; ++x) {
+          float s = 0.0f;
+#pragma unroll
+          for (int y = 0; y < V; ++y) s = fmaf(q[x][y], kv[0][y], s);
+#pragma unroll
+          for (int m = 1; m < 32; m <<= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+          if (t0 + slot < see[x]) {
+            s *= 2.0f * p.scale_log2;
+            const float high = fmaxf(top[x], s), f = exp2_approx(top[x] - high), e = exp2_approx(s - high);
+            top[x] = high;
+            l[x] = fmaf(l[x], f, e);
+#pragma unroll
+            for (int y = 0; y < V; ++y) o[x][y] = fmaf(e, kv[1][y], o[x][y] * f);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kTogether; ++x) {
+      if (r0 + x >= rows) continue;
+      const uint32_t query = (row0 + r0 + x) / p.group, hh = head * p.group + (row0 + r0 + x) - query * p.group;
+      const uint64_t row = (uint64_t)seq.start + query;
+      uint16_t* const out = p.out + row * p.out_token + (uint64_t)hh * p.out_head + lane * V;
+      const float over = see[x] ? 1.0f / l[x] : 0.0f;
+#pragma unroll
+      for (int y = 0; y < V; ++y) out[y] = (uint16_t)to_bits16<TYPE>(see[x] ? o[x][y] * over * p.back : 0.0f);
+      if (p.lse && lane == 0) p.lse[row * p.q_heads + hh] = see[x] ? (top[x] + log2f(l[x])) * 0.69314718055994531f : -INFINITY;
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __grid_constant__ WideParams p) {
   using S = Shape<D>;
@@ -206,6 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
   __shared__ uint64_t scan[kThreads / 32];
   __shared__ uint64_t found_base;
   __shared__ uint32_t found_b, tmem_base, given_up;
+  __shared__ uint32_t far_apart;                           // numbers too far apart for the tile: attend_plainly does it again
   __shared__ int32_t length_of[kMostSorted];
   __shared__ uint32_t order[kMostSorted];
   __shared__ float key_back[8], value_size[8];             // of a step's keys: what undoes their scaling; of its values: the power of two below the largest, or 0
@@ -236,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     mbar_init(q_full, kSoftmaxWarps);
     for (uint32_t s = 0; s < kPairs; ++s) { mbar_init(pairs_full + 8 * s, 2); mbar_init(pairs_empty + 8 * s, kUnpackWarps); }
     for (uint32_t s = 0; s < kValues; ++s) { mbar_init(v_full + 8 * s, kUnpackWarps / 2); mbar_init(v_empty + 8 * s, 1); }
-    given_up = 0;
+    given_up = far_apart = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(S::kTmem) : "memory");
@@ -404,27 +491,34 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       fine = fine && (i < kPairs || mbar_wait(pairs_empty + 8 * b, (i / kPairs - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw + (value ? 17 : 8) * D;
-      float largest = 0.0f;
+      float largest = 0.0f, smallest = FLT_MAX;             // (a key's number of the largest size; of the values, each group's)
       uint32_t pair[2][J];
       bool bad = false;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const uint32_t token = lane + 32 * x;
         uint32_t groups = 0;
+        float key = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           pair[x][j] = token < have ? *reinterpret_cast<const uint32_t*>(raw + (token >> 4) * S::kTile + ((token & 15u) * J + j) * 4) : 0u;
           const float lo = from_bits16<TYPE>(pair[x][j] & 0xffffu);
-          largest = fmaxf(largest, fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(pair[x][j] >> 16), lo))));
+          const float size = fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(pair[x][j] >> 16), lo)));
+          largest = fmaxf(largest, size);
+          key = fmaxf(key, size);
+          if (value && size > 0.0f) smallest = fminf(smallest, size);
           if (value && lo != lo) {                          // no number: zeros here, and the rows that see it are told
             groups |= 1u << j;
             pair[x][j] = 0;
           }
         }
+        if (!value && key > 0.0f) smallest = fminf(smallest, key);
         if (value) poison[i & 7u][token] = (uint8_t)groups;
         bad |= groups != 0;
       }
       largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));
+      smallest = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(smallest)));
+      if (lane == 0 && (largest > smallest * (value ? kValueRange : kKeyRange) || largest >= (value ? kMostValue : INFINITY))) far_apart = 1;
       const int32_t up = lift(largest, 14);
       const float times = power2(up);
 #pragma unroll
@@ -605,6 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
           l *= f;
           held *= f;
           top = high;
+          if (!(fabsf(top) <= kMostScore)) far_apart = 1;   // (the sum of it and of a shift would not be exact enough)
         }
         cap = power_above(fminf(fmaxf(fmaxf(held, higher ? most : 256.0f * most), kLeastCap), kMostCap));
         f = held * inverse_of_power(cap);                   // (1 at most)
@@ -667,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     l = fmaf(row_sum[0][r], e0, row_sum[1][r] * e1);        // (the same in both)
     top = high;
     nan_groups = row_nan[0][r] | row_nan[1][r];
-    if (fine && found) {
+    if (fine && found && !*(volatile uint32_t*)&far_apart) {
       const uint64_t row = (uint64_t)seq.start + query;
       uint16_t* const out = p.out + row * p.out_token + (uint64_t)hh * p.out_head;
       const bool saw = see != 0;
@@ -701,6 +796,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
   }
   if (tid == 0 && given_up) atomicOr(p.c.status, QSGD_DEV_TIMEOUT);
+  if (far_apart && !given_up) attend_plainly<D>(p, seq, found_b, head, row0, rows);
 }
 
 template <int D>
@@ -749,6 +845,9 @@ int launch_cache_attend_wide(const CacheView& view, uint32_t head_dim, const Att
   p.group = a.q_heads / view.heads;
   p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
   p.polls = quantize_poll_limit();
+  const int lost = attend_sums_lose(view);
+  p.times = ldexpf(1.0f, -lost);
+  p.back = ldexpf(1.0f, lost);
   return head_dim == 64 ? launch_wide<64>(p, stream) : launch_wide<128>(p, stream);
 }
 

@@ -112,9 +112,9 @@ def test_large_values_of_little_weight(dtype, large, place, dim):
 
 @pytest.mark.parametrize("dtype, large", [(BF16, 1e8), (BF16, 1e30), (FP16, 3e7)])
 @pytest.mark.parametrize("what", ["keys", "values"])
-@pytest.mark.parametrize("dim, heads, group", [(128, 2, 4), (256, 2, 2)])
+@pytest.mark.parametrize("dim, heads, group", [(128, 2, 4), (128, 148, 1), (64, 148, 1), (256, 2, 2)])
 def test_what_a_row_does_not_see(dtype, large, what, dim, heads, group):
-    """Later tokens of any size leave no trace in the rows in front of them."""
+    """Later tokens of any size leave no trace in the rows in front of them (148 heads: tiles of 128 rows in bf16)."""
     small = 1.0 if dtype == BF16 else 1e-3
     f = Filled([150], 16, heads, dim, dtype)
     x = f.k[0] if what == "keys" else f.v[0]
@@ -127,7 +127,7 @@ def test_what_a_row_does_not_see(dtype, large, what, dim, heads, group):
     compare(f, q[:80], out[:80], lse[:80], scale, [80], dtype, tile=launches == 1)
 
 
-@pytest.mark.parametrize("heads", [2])
+@pytest.mark.parametrize("heads", [2, 148])
 @pytest.mark.parametrize("large", [2.0 ** 20, 2.0 ** 60])
 @pytest.mark.parametrize("what", ["keys", "values", "groups"])
 def test_tokens_of_very_different_sizes_in_chunks(what, large, heads):
@@ -153,7 +153,7 @@ def test_tokens_of_very_different_sizes_in_chunks(what, large, heads):
     compare(f, q, out, lse, 0.25, [100], BF16, tile=heads == 148)
 
 
-@pytest.mark.parametrize("lengths, runs, heads, one", [([500], [1], 1, True), ([9000], [1], 1, True), ([300], [40], 2, False)])
+@pytest.mark.parametrize("lengths, runs, heads, one", [([500], [1], 1, True), ([9000], [1], 1, True), ([300], [40], 2, False), ([333], [100], 148, False)])
 def test_scores_far_below_zero(lengths, runs, heads, one):
     """All scores lower than any that a fixed number would stand for: the highest one still takes all."""
     f = Filled(lengths, 16, heads, 128, BF16)
@@ -215,3 +215,49 @@ def test_large_values_of_little_weight_in_chunks(large, weight, place, heads):
     assert (Q.qsgd_launch_count() - before == 1) == (heads == 148)
     f.fine()
     compare(f, q, out, lse, 0.25, [100], BF16, tile=heads == 148)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page, layout, lengths, runs, group", [(16, "gaps", [150, 0, 40], [100, 3, 60], 2), (48, "heads", [700, 333], [65, 64], 3),
+                                                               (128, "pages", [1000], [129], 1)])
+def test_tiles_of_wide_ranges_in_every_form(dim, page, layout, lengths, runs, group):
+    """Numbers too far apart for a tile's fp16, with pages, rows in front of the first token, heads that share keys, strides, and values that are none."""
+    heads = 100
+    f = Filled(lengths, page, heads, dim, BF16, layout=layout)
+    for k, v in zip(f.k, f.v):
+        v[::3] = (v[::3].float() * 1e25).to(BF16)
+        k[1::5] = (k[1::5].float() * 1e-20).to(BF16)
+    f.k[0][140:], f.v[0][20, :, -1] = math.inf, math.nan
+    f.write_all()
+    rows = sum(runs)
+    wide = values((rows, heads * group + 3, dim + 8), BF16, 8).cuda()
+    q, big = wide[:, 1: 1 + heads * group, :dim], torch.full((heads * group, rows + 2, dim + 8), 42.0, dtype=BF16, device="cuda")
+    out, lse = big.transpose(0, 1)[:rows, :, :dim], torch.full((rows + 2, heads * group), 42.0, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, heads * group), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    before = Q.qsgd_launch_count()
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts_of(runs), lse=lse[:rows])
+    tile = Q.qsgd_launch_count() - before == 1
+    assert tile or (dim, runs) == (64, [129])               # (a tile and one row of the next: too few rows for tiles at head size 64)
+    f.fine()
+    assert bool((big[:, rows:] == 42).all()) and bool((big[:, :, dim:] == 42).all()) and bool((lse[rows:] == 42).all())
+    again = torch.empty(rows, heads * group, dim, dtype=BF16, device="cuda")
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, again, ws, f.status, starts=starts_of(runs))
+    assert torch.equal(out.nan_to_num(7.0), again.nan_to_num(7.0))
+    at = 0
+    for b, (n, r) in enumerate(zip(lengths, runs)):
+        seen = torch.arange(n - r + 1, n + 1)               # tokens of each row
+        o, s = out[at: at + r], lse[at: at + r]
+        assert bool((o[seen <= 0] == 0).all()) and bool((s[seen <= 0] == -math.inf).all())
+        if b == 0:
+            bad = seen > 140
+            assert bool(o[bad].isnan().all()) and bool(s[bad].isnan().all()) and not bool(s[~bad].isnan().any())
+            assert bool(o[~bad & (seen > 20)][..., dim - 64:].isnan().all()) and not bool(o[~bad][..., : dim - 64].isnan().any())
+        some = [0, heads - 1]
+        pick = [h * group + i for h in some for i in range(group)]
+        for i in [i for i in range(r) if 0 < seen[i] <= (140 if b == 0 else n)][:: max(1, r // 7)]:
+            one = Filled([0], 16, 1, dim, BF16)
+            m = int(seen[i])
+            one.lengths, one.k, one.v = [m], [f.k[b][:m, some]], [f.v[b][:m, some]]
+            compare(one, q[at + i: at + i + 1, pick], o[i: i + 1, pick], s[i: i + 1, pick], 1 / math.sqrt(dim), [1], BF16, tile=tile)
+        at += r
