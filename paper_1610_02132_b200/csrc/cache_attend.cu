@@ -4,9 +4,9 @@
 //   s_t = sum_g step_tg * (q_g . c_tg) + lo_tg * sum(q_g),   p_t = 2^(a s_t - m),   a = scale * log2(e),
 //   o   = (sum_t p_t v_t) / sum_t p_t,    sum_t p_t v_tg = sum_t (p_t step_tg) (c_tg - 8) + sum_t p_t (lo_tg + 8 step_tg).
 // The codes go to the tensor cores as they are and the pairs are applied in fp32:
-//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp16 operands, fp32 sums). A row of q is multiplied by a
-//            power of two that puts its largest number at 2^11: 16-bit numbers of either type fit fp16 then, but for what lies 2^-21 and more
-//            below the largest, which loses no more than fp32 sums do.
+//   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp16 operands, fp32 sums). Each group of a row of q is multiplied
+//            by a power of two that puts its largest number at 2^11: 16-bit numbers of either type fit fp16 then, but for what lies 2^-21 and more
+//            below the group's largest, of which it keeps 2^-32.
 //   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two, of each row and group by itself, that puts the
 //            largest p * step so far at 32 to 64 and is lowered only when one passes it by 2^9. It follows p * step and not step, each row's own:
 //            a group beside a much larger one, a row in front of much larger values that it does not see, or sees with little weight, keep their bits.
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 
     // ---- queries: operands, sums of each group, and how far each row sees ------------------------------------------------
     uint32_t qf[NT][J][4][2];
-    float qsum[NT][J][2], factor[NT][2];
+    float qsum[NT][J][2], factor[NT][J][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t r = 8 * nt + g;
@@ -442,7 +442,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
       const uint32_t query = (row0 + r) / p.group, hh = (row0 + r) - query * p.group;
       const uint16_t* src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)(head * p.group + hh) * p.q_head + 16 * t;
       uint4 raw[J][2];
-      float top_q = 0.0f;
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         raw[j][0] = raw[j][1] = make_uint4(0, 0, 0, 0);
@@ -452,7 +451,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         }
       }
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j) {
+        float top_q = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t w[4] = {raw[j][h].x, raw[j][h].y, raw[j][h].z, raw[j][h].w};
@@ -460,19 +460,17 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
           for (int i = 0; i < 4; ++i)
             top_q = fmaxf(top_q, fmaxf(fabsf(from_bits16<TYPE>(w[i] & 0xffffu)), fabsf(from_bits16<TYPE>(w[i] >> 16))));
         }
-      top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 1));
-      top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 2));
-      // 2^(11 - e) for a largest number of [2^e, 2^(e + 1)); nothing to scale in a row of zeros, infinities or NaN
-      const int32_t e = (int32_t)(__float_as_uint(top_q) >> 23) - 127;
-      int32_t up = 11 - e;
-      if (up > 120) up = top_q > 0.0f ? 120 : 0;
-      if (e == 128) up = 0;
-      const float times = __uint_as_float((uint32_t)(127 + up) << 23);
-      const float back = p.scale_log2 * 16777216.0f * __uint_as_float((uint32_t)(127 - up) << 23);        // 2^24: see unpack
-      factor[nt][0] = __shfl_sync(0xffffffffu, back, 8 * t);
-      factor[nt][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
+        top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 1));
+        top_q = fmaxf(top_q, __shfl_xor_sync(0xffffffffu, top_q, 2));
+        // 2^(11 - e) for a largest number of [2^e, 2^(e + 1)); nothing to scale in a group of zeros, infinities or NaN
+        const int32_t e = (int32_t)(__float_as_uint(top_q) >> 23) - 127;
+        int32_t up = 11 - e;
+        if (up > 120) up = top_q > 0.0f ? 120 : 0;
+        if (e == 128) up = 0;
+        const float times = __uint_as_float((uint32_t)(127 + up) << 23);
+        const float back = p.scale_log2 * 16777216.0f * __uint_as_float((uint32_t)(127 - up) << 23);        // 2^24: see unpack
+        factor[nt][j][0] = __shfl_sync(0xffffffffu, back, 8 * t);
+        factor[nt][j][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
         float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -560,7 +558,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              sc[h][nt][e] = fmaf(e < 2 ? step_a : step_b, acc[nt][e], fmaf(e < 2 ? lo_a : lo_b, qsum[nt][j][e & 1], sc[h][nt][e]));
+              sc[h][nt][e] = fmaf(factor[nt][j][e & 1], fmaf(e < 2 ? step_a : step_b, acc[nt][e], (e < 2 ? lo_a : lo_b) * qsum[nt][j][e & 1]), sc[h][nt][e]);
         }
         load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 17 * D) + ka * J, pair[h][0]);
         load_pairs<J>(reinterpret_cast<const uint32_t*>(tile + 17 * D) + kb * J, pair[h][1]);
@@ -587,7 +585,6 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            sc[h][nt][e] *= factor[nt][e & 1];
             if (kMasked && (int32_t)(16 * h + (e < 2 ? ka : kb)) >= see[nt][e & 1]) {
               seen &= ~(1u << (4 * (NT * h + nt) + e));
               sc[h][nt][e] = -INFINITY;

@@ -12,8 +12,8 @@
 //   warps 16-19  unpack the values turned round (rows of a coordinate), three buffers
 // Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
 // likewise at 2^11; P holds p times a power of two of each row that follows its own largest p * v. Numbers 2^-28 below the largest of 64 tokens lose bits.
-// Where that is more than the rounding to 11 bits (a key, or a group of values, much smaller than another of the same step: each is a score, or an output, of
-// its own, and a row need not see the other) or scores are so large that a power of two beside them is lost, the tile is done again in fp32: attend_plainly.
+// Where that is more than the rounding to 11 bits (a group of a key or of a query much smaller than another one, of values than another of the same step: a row
+// need not see the other, its weight may be low, a small query may meet a large key) or scores are so large that a power of two beside them is lost, the tile is done again in fp32: attend_plainly.
 // Roundings: k and v to 11 bits, p to 11 bits, next to the output's 8. (For an fp16 output they would weigh as much as its own rounding: those go through
 // cache_attend.cu.)
 //
@@ -36,9 +36,9 @@ constexpr uint32_t kRows = 128, kStep = 64, kThreads = 640, kUnpackWarps = 8, kS
 constexpr uint32_t kMostSorted = 256;
 constexpr uint32_t kDrainPolls = 1u << 22;                 // bound of the waits for copies and products in flight
 constexpr float kNoMax = -FLT_MAX;                         // maximum of nothing: below any score, and finite, so that differences of maxima are numbers
-// What the tiles' 11 bits and common powers of two are good for; a tile with more goes through attend_plainly. A step's largest key next to its smallest one
-// (its number of the largest size; keys of zeros aside), its largest group of values next to its smallest, the largest value at all, the size of a score.
-constexpr float kKeyRange = 65536.0f, kValueRange = 4096.0f, kMostValue = 8.5070591730234616e+37f, kMostScore = 8192.0f;
+// What the tiles' 11 bits and common powers of two are good for; a tile with more goes through attend_plainly. The largest number of one group of a step's
+// keys next to that of another (groups of zeros aside), of its values, of a query row; the largest value at all; the size of a score.
+constexpr float kKeyRange = 65536.0f, kValueRange = 4096.0f, kQueryRange = 4096.0f, kMostValue = 8.5070591730234616e+37f, kMostScore = 8192.0f;
 constexpr float kLeastCap = 7.5231638452626401e-37f, kMostCap = 8.5070591730234616e+37f;      // 2^-120, 2^126
 
 struct WideParams {
@@ -491,28 +491,25 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       fine = fine && (i < kPairs || mbar_wait(pairs_empty + 8 * b, (i / kPairs - 1) & 1u, waits));
       if (!__all_sync(0xffffffffu, fine)) break;
       const uint8_t* const raw = mem + S::kAtRaw + s * S::kRaw + (value ? 17 : 8) * D;
-      float largest = 0.0f, smallest = FLT_MAX;             // (a key's number of the largest size; of the values, each group's)
+      float largest = 0.0f, smallest = FLT_MAX;             // (the groups' largest numbers)
       uint32_t pair[2][J];
       bool bad = false;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const uint32_t token = lane + 32 * x;
         uint32_t groups = 0;
-        float key = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           pair[x][j] = token < have ? *reinterpret_cast<const uint32_t*>(raw + (token >> 4) * S::kTile + ((token & 15u) * J + j) * 4) : 0u;
           const float lo = from_bits16<TYPE>(pair[x][j] & 0xffffu);
           const float size = fmaxf(fabsf(lo), fabsf(fmaf(15.0f, from_bits16<TYPE>(pair[x][j] >> 16), lo)));
           largest = fmaxf(largest, size);
-          key = fmaxf(key, size);
-          if (value && size > 0.0f) smallest = fminf(smallest, size);
+          if (size > 0.0f) smallest = fminf(smallest, size);
           if (value && lo != lo) {                          // no number: zeros here, and the rows that see it are told
             groups |= 1u << j;
             pair[x][j] = 0;
           }
         }
-        if (!value && key > 0.0f) smallest = fminf(smallest, key);
         if (value) poison[i & 7u][token] = (uint8_t)groups;
         bad |= groups != 0;
       }
@@ -625,12 +622,19 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attend_wide_kernel(const __
       // Half of the row of q, scaled, in the keys' order of coordinates.
       const uint16_t* const src = p.q + (uint64_t)(seq.start + query) * p.q_token + (uint64_t)hh * p.q_head;
       float largest = 0.0f;
+#pragma unroll 1
+      for (uint32_t j = 0; j < J; ++j) {
+        float group = 0.0f;
 #pragma unroll 2
-      for (uint32_t c = 0; c < D / 8; ++c) {
-        const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        for (uint32_t c = 8 * j; c < 8 * j + 8; ++c) {
+          const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(src + 8 * c)) : make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int y = 0; y < 4; ++y) largest = fmaxf(largest, fmaxf(fabsf(from_bits16<TYPE>(w[y] & 0xffffu)), fabsf(from_bits16<TYPE>(w[y] >> 16))));
+          for (int y = 0; y < 4; ++y) group = fmaxf(group, fmaxf(fabsf(from_bits16<TYPE>(w[y] & 0xffffu)), fabsf(from_bits16<TYPE>(w[y] >> 16))));
+        }
+        // (One of zeros has no say. The largest so far of two is the other one.)
+        if (j && group > 0.0f && largest > 0.0f && fmaxf(group, largest) > kQueryRange * fminf(group, largest)) far_apart = 1;
+        largest = fmaxf(largest, group);
       }
       const int32_t up = lift(largest, 11);
       const float times = power2(up);

@@ -30,10 +30,11 @@ def reference(f, b, q, scale, runs):
         s = torch.einsum("nkd,kgd->kgn", k[:m], qq) * scale
         p = torch.softmax(s, -1)
         # A score: as in the cache's own tests (rounded sums of |q| * 143 steps, 2^-20 of |q| |k|), but for each token, weighted; where rows of 128 share a
-        # tile, keys in fp16: half a step of 2^-11 of |q| |k|, the sums' roundings, and 2^-24 of |q| * the token's largest.
+        # tile, keys in fp16: half a step of 2^-11 of |q| |k|, the sums' roundings, and of each group 2^-23 of |q| * the token's largest.
         reach = torch.einsum("nkd,kgd->kgn", k[:m].abs(), qq.abs())
         fine = torch.einsum("nkj,kgj->kgn", kstep[:m], qq.abs().unflatten(-1, (-1, 64)).sum(-1)) * 143 * 68 * 2.0 ** -23 + reach * 2.0 ** -20
-        tile = reach * (2.0 ** -12 + 2.0 ** -16) + qq.abs().sum(-1, keepdim=True) * k[:m].abs().amax(-1).T[:, None] * 2.0 ** -24
+        tile = reach * (2.0 ** -12 + 2.0 ** -16) + torch.einsum("nkj,kgj->kgn", k[:m].abs().unflatten(-1, (-1, 64)).amax(-1),
+                                                                qq.abs().unflatten(-1, (-1, 64)).sum(-1)) * 2.0 ** -23
         out["err"].append(torch.stack([abs(scale) * (p * e).sum(-1).flatten() + abs(scale) * torch.where(p > 2.0 ** -40, e, 0.0).amax(-1).flatten()
                                        for e in (fine, tile)], -1))
         out["out"].append(torch.einsum("kgn,nkd->kgd", p, v[:m]).flatten(0, 1))
@@ -261,3 +262,27 @@ def test_tiles_of_wide_ranges_in_every_form(dim, page, layout, lengths, runs, gr
             one.lengths, one.k, one.v = [m], [f.k[b][:m, some]], [f.v[b][:m, some]]
             compare(one, q[at + i: at + i + 1, pick], o[i: i + 1, pick], s[i: i + 1, pick], 1 / math.sqrt(dim), [1], BF16, tile=tile)
         at += r
+
+
+@pytest.mark.parametrize("dtype, ratio", [(BF16, 2.0 ** 23), (BF16, 2.0 ** 40), (BF16, 2.0 ** 80), (FP16, 2.0 ** 13)])
+@pytest.mark.parametrize("swap", [False, True])
+@pytest.mark.parametrize("heads, dim, lengths, runs, one", [(2, 128, [700, 9], [1, 1], True), (2, 256, [5000], [1], True), (2, 128, [150], [40], False), (148, 128, [150], [100], False)])
+def test_queries_small_where_keys_are_large(dtype, ratio, swap, heads, dim, lengths, runs, one):
+    """A group of coordinates with large keys and small queries counts as much as one with small keys and large queries."""
+    f = Filled(lengths, 16, heads, dim, dtype)
+    groups = torch.ones(dim // 64)
+    groups[1 if swap else 0] = ratio ** 0.5
+    for k in f.k:
+        k.copy_((k.float() * groups.repeat_interleave(64) / ratio ** 0.25).to(dtype))
+    f.write_all()
+    q = (values((sum(runs), heads, dim), dtype, 3).float() / groups.repeat_interleave(64) * ratio ** 0.25).to(dtype).cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, heads), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    before = Q.qsgd_launch_count()
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=None if one else starts_of(runs), lse=lse)
+    tile = not one and Q.qsgd_launch_count() - before == 1
+    f.fine()
+    some = [0, heads - 1]
+    f.k, f.v = [x[:, some] for x in f.k], [x[:, some] for x in f.v]
+    compare(f, q[:, some], out[:, some], lse[:, some], 1 / math.sqrt(dim), runs, dtype, tile=tile)
