@@ -341,7 +341,8 @@ int qsgd_policy_decode_sgd_step(const void* const* msgs, const uint64_t* const* 
  * A cache of keys and values in 4 bits. 64 neighbouring values of a token and head form a bucket with
  * two numbers of the cache's type (F16 or BF16): lo, the smallest value (+0 for a zero of either sign), and step, the smallest number
  * of the type with 15 * step >= largest - smallest. A value x is held as c in 0 .. 15, the nearest to
- * (x - lo) / step, the lower one of two as near, and stands for lo + step * c: at most step / 2 away. A bucket that
+ * (x - lo) / step, the lower one of two as near (decided exactly), and stands for lo + step * c: at most step / 2 away. (Of a bucket
+ * with the type's largest numbers that may lie beyond them, and is then read as an infinity.) A bucket that
  * holds a value that is not finite, or whose span is beyond fp32, stands for NaN throughout; one whose step would lie below
  * 2^-126 stands for lo.
  *
@@ -404,11 +405,19 @@ int qsgd_cache_read(const qsgd_cache* cache, const qsgd_cache_rows* rows, void* 
  * Attention over the cache: each row is a query of q_heads heads (a multiple of the cache's heads; query
  * head h uses key head h / (q_heads / heads)) at the position of its token, and sees the tokens up to its own:
  *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q . k_t),  lse = ln sum_t p_t
- * over what the cache stands for (the sums are kept unscaled: values beyond 2^100 may give infinities). A row that sees no token (an empty sequence, or a row in front of the first
- * token) gives 0 and -infinity.
- *   q, out       [rows][q_heads][head_dim] as k and v above; scores, sums and the output are kept in fp32, p_t * step
- *                in 11 bits of fraction (22 for F16), the output is rounded to the type once. Where a sequence is split over the GPU
- *                follows from all lengths of the call, so the same call gives the same bits, another batch around a sequence perhaps not.
+ * over what the cache stands for. A row that sees no token (an empty sequence, or a row in front of the first
+ * token) gives 0 and -infinity. What a row does not see leaves no trace in it, whatever it is.
+ *   q, out       [rows][q_heads][head_dim] as k and v above. Scores, maxima, sums and lse are fp32; the output is rounded to the
+ *                type once, and is finite wherever values of the type's whole range have a finite mean. Before that, depending on the call:
+ *                - few rows to a sequence, F16, head_dim 192 or 256: p_t * step is rounded to 11 bits (22 for F16); numbers of a query
+ *                  2^-21 below the largest of their 64 neighbours (a bucket's coordinates) keep 2^-32 of that one.
+ *                - BF16, head_dim 64 or 128, starts given, and rows that fill the GPU's SMs in tiles of 128 (the runs' average
+ *                  counts): keys, values and p are rounded to 11 bits each, a score is off by up to 2^-12 * scale * sum |q| |k| by that.
+ *                  A tile whose buckets of keys, values or queries are too far apart for this (2^16, 2^12 and 2^12 between the largest numbers
+ *                  of two), or scores beyond 2^13, takes fp32 throughout, and far longer.
+ *                Values below 2^-86 may lose bits, and scale * q beyond 2^112 may give infinities or NaN. Where a sequence is split over the
+ *                GPU and which of the two is taken follows from all lengths and runs of the call, so the same call gives the same bits,
+ *                another batch around a sequence perhaps not.
  *   lse          [rows][q_heads] fp32, contiguous, or NULL
  *   workspace    qsgd_cache_attend_workspace_bytes() of scratch, 16-byte aligned. Every part that is read was
  *                written by the same call, so nothing needs clearing; calls that overlap on the GPU need one each.

@@ -20,21 +20,22 @@
 // A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
 // and one shift (and an exact addition each where they are centred); the powers of two are undone in q, and in the output's scale at the end.
 // For 64 sequences of 100 to 8000 tokens, 8 heads of 128: nibbles moved into place under a bf16 exponent, p in two bf16 numbers 143 us; nibbles under the
-// exponents of 1024 and 64 and a subtraction each 101; as now, with the -8 by a product with a constant operand 87; as now 84.
+// exponents of 1024 and 64 and a subtraction each 101; as now, with the -8 by a product with a constant operand 87; with an addition 84;
+// as now, with powers of two of each row and group, 87.
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
 // What bounds it: HBM holds 9/8 * head_dim bytes a token and head, each read once; issue slots and the integer pipe are nearly as busy (350 warp
-// instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 62 %, integer pipe 55 %, tensor pipe 22 %). 64 sequences of
-// 16000 tokens: 249 us, 4.7 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
+// instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 60 %, integer pipe 52 %, tensor pipe 21 %). 64 sequences of
+// 16000 tokens: 254 us, 4.6 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
 // So everything is arranged around the stream of tiles. The tiles of all (sequence, key
 // head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
 // takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
 // written out by its warp; what spans warps of a CTA is joined in shared memory; what spans CTAs leaves (m, sum, o) in the workspace,
 // at most two parts a CTA, and a second kernel joins those. (With tiles dealt out to the eight warps of a CTA, which met at the end of each
-// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 21: a CTA had up to 40 segments one after another.)
+// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 22: a CTA had up to 40 segments one after another.)
 // Few and short segments need no such line: a cluster of CTAs has one each and joins it over its shared memory (one user's step, 1000 tokens, with
-// the write in front of it: 12 us against 16).
+// the write in front of it: 12.4 us against 16).
 #include <float.h>
 
 #include "cache.cuh"

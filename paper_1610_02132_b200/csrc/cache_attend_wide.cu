@@ -5,9 +5,10 @@
 //   S = Q K^T   128 rows x 64 tokens,   O += P V   128 rows x head_dim
 // A CTA has 128 rows of one (sequence, key head) and goes over its tokens 64 at a time:
 //   warp 0       brings the packed tiles in by bulk copies, four steps ahead
-//   warp 1       issues the products (one thread)
+//   warp 1       issues the products (one lane of it)
 //   warps 2, 3   the (lo, step) pairs of the keys, of the values: their largest number, and the pairs in fp16
-//   warps 4-11   softmax: two threads to a row of S, 32 tokens each; P goes to shared memory; O is scaled in tensor memory when a maximum rises by 2^8
+//   warps 4-11   softmax: a thread to a row of S, four warps to every other step; P goes to shared memory; O is scaled in tensor memory when a maximum
+//                rises by 2^8
 //   warps 12-15  unpack the keys as rows of a token, 128-byte swizzle, two buffers
 //   warps 16-19  unpack the values turned round (rows of a coordinate), three buffers
 // Range: bf16 numbers need not fit fp16. The keys of a step, and its values, are multiplied by a power of two that puts their largest at 2^14, a query row
@@ -18,12 +19,12 @@
 // cache_attend.cu.)
 //
 // What bounds it: a step is 2 * 128 * 64 * head_dim multiply-adds, 512 cycles of the tensor cores at head_dim 128, 8192 exponentials, another 512 cycles
-// of the special-function units, and about 5000 warp instructions, half of them unpacking. It takes 1800 cycles (1500 at head size 64), and no role waits
+// of the special-function units, and about 5000 warp instructions, half of them unpacking. It takes 1800 cycles at 1.72 GHz (1500 at head size 64), and no role waits
 // for long: softmax warps 80 percent of the time at work, unpacking ones as much; issue slots 65 percent, tensor pipe 27. What took it there from 2700: issuing warps that go round as a whole
 // (addresses in uniform registers; one lane by itself took 1250 cycles a step to issue and let P wait for 2200), softmax warps in two halves on
 // alternate steps, and buffers enough that neither waits for the other's last step. Waits out of line, since the roles' code together is as
 // large as the instruction cache (in line: 500 cycles more).
-// Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 77 us, 0.40 PFLOP/s; by cache_attend.cu 204.
+// Four chunks of 256 queries, 32 heads on 8 of 128, over 700 to 4096 tokens: 78.5 us, 0.39 PFLOP/s; by cache_attend.cu 204.
 #include <float.h>
 
 #include "cache.cuh"
@@ -824,9 +825,10 @@ int launch_wide(const WideParams& p, cudaStream_t stream) {
 }  // namespace
 
 // A CTA has a row tile for itself, and all of its tokens, so that few tiles leave SMs idle, while cache_attend.cu spreads any rows over all SMs. A round of
-// tiles over the SMs takes 44, 133 and 248 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
-// 46, 109 and 200 for 4096 rows in all heads, 49, 123 and 224 for 4608, and 70, 199 and 375 for 8192. At head size 64: 34, 107 and 204 against 32, 75 and
-// 131 for 4608 rows, 42, 117 and 213 for 8192. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays.
+// tiles over the SMs takes 43, 131 and 247 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
+// 48, 113 and 207 for 4096 rows in all heads, 50, 127 and 231 for 4608, and 73, 211 and 398 for 8192. At head size 64: 35, 109 and 208 against 32, 77 and
+// 137 for 4608 rows, 42, 124 and 230 for 8192. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays. (The rows'
+// average counts: one kernel has the whole call, a long run and single tokens beside it too.)
 bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads) {
   if (type != QSGD_TYPE_BF16 || (head_dim != 64 && head_dim != 128) || !view.starts || !view.sequences) return false;
   const uint64_t rows = (uint64_t)view.rows * (q_heads / view.heads);        // of a key head

@@ -12,7 +12,8 @@
 // Four lanes share a group (two times 16 dense bytes and two words of codes each: with eight lanes what a group takes once, its span and step,
 // was done twice as often), a warp's eight teams neighbouring rows or heads; a team goes along its row's keys, or values, head by head.
 // 65536 tokens of 8 heads of 128 read back: 60 us, 5.7 TB/s (102 with a conversion instruction a code). 15.6 K tokens written and read back: 47 us (78 at
-// first, 53 with eight lanes to a group); writing is bound by issue slots: nine operations a value.
+// first, 53 with eight lanes to a group). Writing takes ten operations a value; its issue slots are two thirds full, and its warps wait most for what they
+// read (the next head's numbers are asked for when the present one's codes are stored) and at the CTA's meetings.
 #include <float.h>
 
 #include "cache.cuh"

@@ -1,8 +1,8 @@
 // Product in 8-bit integers for many rows: out[m][n] = (a_m . b_n) a_scale b_scale + bias on the fifth-generation tensor cores.
 //
 // Tiles of 128 x `width` of the output, each summed over K by tcgen05.mma (kind::i8, exact 32-bit sums in tensor memory). A persistent CTA per SM:
-// one thread keeps a ring of stages (128 columns of 128 rows of a and `width` rows of b, 128-byte swizzle) filled by TMA, which puts zeros where a or b
-// end; one thread issues the products; four warps take finished sums out of tensor memory, scale them and store them, while the next tile's
+// one warp keeps a ring of stages (128 columns of 128 rows of a and `width` rows of b, 128-byte swizzle) filled by TMA, which puts zeros where a or b
+// end; one warp issues the products (one lane of either, the others go round with it); four warps take finished sums out of tensor memory, scale them and store them, while the next tile's
 // products run into the other half of tensor memory.
 //
 // The width is what leaves the SMs least idle (pick_width): 256 for large products, where it halves the traffic from L2 against 128; fewer columns,
