@@ -409,8 +409,8 @@ int qsgd_cache_read(const qsgd_cache* cache, const qsgd_cache_rows* rows, void* 
  * token) gives 0 and -infinity. What a row does not see leaves no trace in it, whatever it is.
  *   q, out       [rows][q_heads][head_dim] as k and v above. Scores, maxima, sums and lse are fp32; the output is rounded to the
  *                type once, and is finite wherever values of the type's whole range have a finite mean. Before that, depending on the call:
- *                - few rows to a sequence, F16, head_dim 192 or 256: p_t * step is rounded to 11 bits (22 for F16); numbers of a query
- *                  2^-21 below the largest of their 64 neighbours (a bucket's coordinates) keep 2^-32 of that one.
+ *                - few rows to a sequence, F16, head_dim 192 or 256: p_t * step is rounded to 11 bits (20 for F16); a product of
+ *                  a query's number and a code is cut off at 2^-18 of the largest |q| in the 64 coordinates of the bucket.
  *                - BF16, head_dim 64 or 128, starts given, and rows that fill the GPU's SMs in tiles of 128 (the runs' average
  *                  counts): keys, values and p are rounded to 11 bits each, a score is off by up to 2^-12 * scale * sum |q| |k| by that.
  *                  A tile whose buckets of keys, values or queries are too far apart for this (2^16, 2^12 and 2^12 between the largest numbers

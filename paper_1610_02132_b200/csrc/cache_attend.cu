@@ -6,7 +6,7 @@
 // The codes go to the tensor cores as they are and the pairs are applied in fp32:
 //   scores   A = codes of 16 tokens, B = up to 8 query rows of one key head (m16n8k16, fp16 operands, fp32 sums). Each group of a row of q is multiplied
 //            by a power of two that puts its largest number at 2^11: 16-bit numbers of either type fit fp16 then, but for what lies 2^-21 and more
-//            below the group's largest, of which it keeps 2^-32.
+//            below the group's largest, of which it keeps 2^-36.
 //   output   A = codes of 16 coordinates x 16 tokens, B = p * step in fp16, times a power of two, of each row and group by itself, that puts the
 //            largest p * step so far at 32 to 64 and is lowered only when one passes it by 2^9. It follows p * step and not step, each row's own:
 //            a group beside a much larger one, a row in front of much larger values that it does not see, or sees with little weight, keep their bits.
@@ -17,17 +17,20 @@
 //            be as large as their type has them, the undivided sums then lie outside fp32.
 //            The codes are centred here because these sums run over the whole sequence: 8 sum(p step) would grow until what is left
 //            after taking it off at the end is the error of its rounded sums.
-// A nibble in the last four bits of an fp16 number is c * 2^-24, one in the four bits above c * 2^-20, so four pairs of codes take four masks
-// and one shift (and an exact addition each where they are centred); the powers of two are undone in q, and in the output's scale at the end.
+// A nibble in bits 4 to 7 of an fp16 number is c * 2^-20, below the normal ones: a mask and at most a shift each make the keys' operands. The values' are
+// centred by a multiply-add that makes normal numbers of them, (c - 8) * 2^-9, so that a nibble may lie in the last four bits, too (c * 2^-24), and one
+// shift does for four masks. The powers of two are undone in q's scale and in the output's at the end. (The tensor cores line products up by their exponents
+// as written, 2^-14 for numbers below the normal ones, and drop what lies 2^24 below the largest: beside c * 2^-20 that is 2^-18 of the largest q, beside c * 2^-24
+// it was 2^-14, an error of 10^-6 in fp16 scores and of 2^-13 * p * step in the output.)
 // For 64 sequences of 100 to 8000 tokens, 8 heads of 128: nibbles moved into place under a bf16 exponent, p in two bf16 numbers 143 us; nibbles under the
 // exponents of 1024 and 64 and a subtraction each 101; as now, with the -8 by a product with a constant operand 87; with an addition 84;
-// as now, with powers of two of each row and group, 87.
+// as now, with powers of two of each row and group and these operands, 89.
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
 // What bounds it: HBM holds 9/8 * head_dim bytes a token and head, each read once; issue slots and the integer pipe are nearly as busy (350 warp
 // instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 60 %, integer pipe 52 %, tensor pipe 21 %). 64 sequences of
-// 16000 tokens: 254 us, 4.6 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
+// 16000 tokens: 258 us, 4.6 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
 // So everything is arranged around the stream of tiles. The tiles of all (sequence, key
 // head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
 // takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
@@ -170,15 +173,6 @@ __device__ __forceinline__ float exp2_approx(float v) {
   return r;
 }
 
-// The codes of a word as fp16 pairs, pair s = nibble s of either half: c * 2^-24 for even s, c * 2^-20 for odd ones.
-__device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
-  const uint32_t v = w >> 8;
-  c[0] = w & 0x000f000fu;
-  c[1] = w & 0x00f000f0u;
-  c[2] = v & 0x000f000fu;
-  c[3] = v & 0x00f000f0u;
-}
-
 // Of either half by itself.
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -191,11 +185,6 @@ __device__ __forceinline__ float size_of_pair(uint32_t pair) {
   return fmaxf(from_bits16<TYPE>(pair >> 16), fabsf(from_bits16<TYPE>(pair & 0xffffu)) * (1.0f / 1024.0f));
 }
 
-__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 // The largest pair (as a number) of that size.
 template <int TYPE>
 __device__ __forceinline__ uint32_t pair_of_size(float size) {
@@ -205,13 +194,25 @@ __device__ __forceinline__ uint32_t pair_of_size(float size) {
 // Of a power of two from 2^-126 to 2^126.
 __device__ __forceinline__ float inverse_of_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
 
-// The codes less 8, exact: the difference is a multiple of 2^-24 below 2^-16.
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+// The codes of a word as fp16 pairs, pair s = nibble s of either half: c * 2^-20.
+__device__ __forceinline__ void unpack(uint32_t w, uint32_t (&c)[4]) {
+  c[0] = (w << 4) & 0x00f000f0u;
+  c[1] = w & 0x00f000f0u;
+  c[2] = (w >> 4) & 0x00f000f0u;
+  c[3] = (w >> 8) & 0x00f000f0u;
+}
+// The same as (c - 8) * 2^-9, exact: c * 2^-24 or c * 2^-20, times 2^15 or 2^11, less 2^-6.
 __device__ __forceinline__ void unpack_centred(uint32_t w, uint32_t (&c)[4]) {
-  unpack(w, c);
-  c[0] = add_f16x2(c[0], 0x80088008u);
-  c[1] = add_f16x2(c[1], 0x80808080u);
-  c[2] = add_f16x2(c[2], 0x80088008u);
-  c[3] = add_f16x2(c[3], 0x80808080u);
+  const uint32_t v = w >> 8;
+  c[0] = fma_f16x2(w & 0x000f000fu, 0x78007800u, 0xa400a400u);
+  c[1] = fma_f16x2(w & 0x00f000f0u, 0x68006800u, 0xa400a400u);
+  c[2] = fma_f16x2(v & 0x000f000fu, 0x78007800u, 0xa400a400u);
+  c[3] = fma_f16x2(v & 0x00f000f0u, 0x68006800u, 0xa400a400u);
 }
 
 template <int J>
@@ -469,7 +470,7 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
         if (up > 120) up = top_q > 0.0f ? 120 : 0;
         if (e == 128) up = 0;
         const float times = __uint_as_float((uint32_t)(127 + up) << 23);
-        const float back = p.scale_log2 * 16777216.0f * __uint_as_float((uint32_t)(127 - up) << 23);        // 2^24: see unpack
+        const float back = p.scale_log2 * 1048576.0f * __uint_as_float((uint32_t)(127 - up) << 23);         // 2^20: see unpack
         factor[nt][j][0] = __shfl_sync(0xffffffffu, back, 8 * t);
         factor[nt][j][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
         float sum = 0.0f;
@@ -482,12 +483,12 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
 #pragma unroll
           for (int i = 0; i < 4; ++i) {                     // coordinates i and i + 4 of each word of eight
             sum += x[i] + x[i + 4];
-            qf[nt][j][i][h] = pack16<QSGD_TYPE_F16>(i & 1 ? x[i] * 0.0625f : x[i], i & 1 ? x[i + 4] * 0.0625f : x[i + 4]);
+            qf[nt][j][i][h] = pack16<QSGD_TYPE_F16>(x[i], x[i + 4]);
           }
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sum *= 5.9604644775390625e-08f;                     // 2^-24, as the codes
+        sum *= 9.5367431640625e-07f;                        // 2^-20, as the codes
         qsum[nt][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
         qsum[nt][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
@@ -792,8 +793,8 @@ __global__ void __launch_bounds__((Shape<TYPE, D, NT>::kThreads), 1) cache_atten
           float v[8];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            v[i] = fmaf(o[nt][j][i][e], i & 1 ? 1048576.0f : 16777216.0f, z) * over * held;
-            v[i + 4] = fmaf(o[nt][j][i][e + 2], i & 1 ? 1048576.0f : 16777216.0f, z) * over * held;
+            v[i] = fmaf(o[nt][j][i][e], 512.0f, z) * over * held;                   // 2^9: see unpack_centred
+            v[i + 4] = fmaf(o[nt][j][i][e + 2], 512.0f, z) * over * held;
           }
           if (out) {
             *reinterpret_cast<uint4*>(out + 64 * j + 8 * g) =

@@ -286,3 +286,45 @@ def test_queries_small_where_keys_are_large(dtype, ratio, swap, heads, dim, leng
     some = [0, heads - 1]
     f.k, f.v = [x[:, some] for x in f.k], [x[:, some] for x in f.v]
     compare(f, q[:, some], out[:, some], lse[:, some], 1 / math.sqrt(dim), runs, dtype, tile=tile)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("code", [1, 8, 15])
+@pytest.mark.parametrize("place", [0, 1, 6])
+def test_small_numbers_of_a_query_beside_a_large_one(dtype, code, place):
+    """One token, whose score is the log-sum-exp. A product of the query's number and a code is cut off at 2^-18 of the largest |q|, 64 of them (twice, with
+    what is added up before), and the rest is fp32."""
+    cache, data = Q.Cache(1, 16, 1, 64, dtype), torch.zeros(18 * 64, dtype=torch.uint8)
+    codes = torch.full((64,), 15)
+    codes[place] = code
+    data[:32] = (codes[0::2] | codes[1::2] << 4).to(torch.uint8)
+    data[512:516] = torch.tensor([0.0, 1.0], dtype=dtype).view(torch.uint8)
+    cache.data.copy_(data.view(1, 1, -1))
+    table, lengths, status = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"), Q.new_status()
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(cache, 1), dtype=torch.uint8, device="cuda")
+    for k in range(0, 26, 2):
+        q = torch.full((1, 1, 64), 1024.0 * 2.0 ** -k * (1 + 2.0 ** -6), dtype=dtype)
+        q[0, 0, place] = 1024.0
+        out, lse = torch.empty(1, 1, 64, dtype=dtype, device="cuda"), torch.empty(1, 1, device="cuda")
+        Q.qsgd_cache_attend(cache, table, lengths, q.cuda(), out, ws, status, scale=1.0, lse=lse)
+        ref = float((q[0, 0].double() * codes).sum())
+        assert abs(float(lse) - ref) <= 2 * 64 * 2.0 ** -18 * float(q.max()) * 0.5 + 2.0 ** -21 * abs(ref), k
+    assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("runs", [[1], [5]])
+def test_outputs_that_cancel(runs):
+    """One token has nearly all weight and a value of zero made of lo and a code: what is left is the others', of fp16's smallest numbers."""
+    f = Filled([25], 16, 1, 128, FP16)
+    f.k[0].mul_(0.05)
+    f.k[0][10] = 11.0 / 128
+    f.v[0].mul_(0.1)
+    f.v[0][10] = ((torch.arange(128) % 16) - 7.0) / 16
+    f.write_all()
+    assert bool((F.held_value(f.v[0])[10, 0, 7::16] == 0).all())
+    q = torch.ones(sum(runs), 4, 128, dtype=FP16, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(sum(runs), 4, device="cuda")
+    ws = torch.empty(Q.qsgd_cache_attend_workspace_bytes(f.cache, 4), dtype=torch.uint8, device="cuda")
+    Q.qsgd_cache_attend(f.cache, f.table, f.len, q, out, ws, f.status, starts=starts_of(runs), scale=1.0, lse=lse)
+    f.fine()
+    compare(f, q, out, lse, 1.0, runs, FP16)
