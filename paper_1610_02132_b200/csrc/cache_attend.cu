@@ -24,7 +24,7 @@
 // it was 2^-14, an error of 10^-6 in fp16 scores and of 2^-13 * p * step in the output.)
 // For 64 sequences of 100 to 8000 tokens, 8 heads of 128: nibbles moved into place under a bf16 exponent, p in two bf16 numbers 143 us; nibbles under the
 // exponents of 1024 and 64 and a subtraction each 101; as now, with the -8 by a product with a constant operand 87; with an addition 84;
-// as now, with powers of two of each row and group and these operands, 89.
+// as now, with powers of two of each row and group and these operands, 89 by 16 warps and 80 by 12.
 // The rows of a score tile are permuted (token_of) so that the transpose of p between the two products is one movmatrix, and reads
 // of codes from shared memory meet no bank twice.
 //
@@ -55,7 +55,9 @@ constexpr uint32_t kLeastCta = 8;
 // 16 tokens take 7.4 us by one CTA and 9.7 by eight, 1000 take 13.5 and 10.9.
 constexpr uint32_t kDirectTokens = 1024, kClusterTokens = 96;
 constexpr uint32_t kMostCluster = 8, kMostDirect = 128;     // CTAs that share a segment, and all of those
-constexpr uint32_t kSegmentCost = 2;      // what a segment costs beside its tiles, in tiles
+// What a segment costs beside its tiles, in tiles. (Counted as 2, 4, 6 and 8: 64 users of 100 to 8000 tokens take 93.9, 84.4, 80.3 and 79.5 us, 128 of 50 to
+// 2000 64.0, 55.7, 52.2 and 51.0, 64 of 4000 each 78.3, 77.7, 77.5 and 79.5, 33 of 17 to 1500 with 16 heads of 64 22.2, 20.9, 20.1 and 21.4.)
+constexpr uint32_t kSegmentCost = 6;
 constexpr uint32_t kMostRowTile = 16;
 constexpr uint32_t kDrainPolls = 1u << 22;   // bound of the waits for copies in flight
 constexpr float kLeastCap = 1.9259299443872359e-34f, kMostCap = 8.5070591730234616e+37f;     // 2^-112, 2^126
@@ -252,11 +254,12 @@ __device__ __forceinline__ Sequence sequence_at(const AttendParams& p, uint32_t 
 template <int TYPE, int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT, kGroups = D / 64;
-  // A CTA fills its SM: with 128 registers a thread 16 warps, with 168 (D = 64, 16 rows) 12, else 8. (As two CTAs of 8, the second one's warps were given 18 % less of the SM's
-  // time than the first one's, and worked on alone at the end.)
-  static constexpr uint32_t kWarps = D > 128 ? 8 : NT == 1 ? 16 : D == 64 ? 12 : 8, kThreads = 32 * kWarps;
+  // A CTA fills its SM: at head size 64 with 128 registers a thread 16 warps, with 168 12, as at 128; else 8. (At 128, 16 warps have the registers of a row's and
+  // group's numbers in local memory: one user's step 12.4 us against 11.5, 131 K tokens 50.6 and 48.4, 64 users of 4000 tokens 82.4 and 78.4. As two CTAs
+  // of 8, the second one's warps were given 18 % less of the SM's time than the first one's, and worked on alone at the end.)
+  static constexpr uint32_t kWarps = D > 128 ? 8 : NT == 2 ? (D == 64 ? 12 : 8) : D == 64 ? 16 : 12, kThreads = 32 * kWarps;
   static constexpr uint32_t kTileBytes = 18 * D;
-  // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (16 warps: 150 KB), and room for the warp's part of the join.
+  // Ring stages of a warp, two tiles each: 9 KB at head sizes 64 and 128 (12 or 16 warps: 110 or 150 KB), and room for the warp's part of the join.
   static constexpr uint32_t kStages = D == 64 ? 4 : 2;
   static constexpr uint32_t kRing = kStages * 2 * kTileBytes;
   static constexpr uint32_t kRowFloats = D + 8;                             // of a part: rows shifted by 8 banks
