@@ -29,16 +29,16 @@
 // of codes from shared memory meet no bank twice.
 //
 // What bounds it: HBM holds 9/8 * head_dim bytes a token and head, each read once; issue slots and the integer pipe are nearly as busy (350 warp
-// instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 60 %, integer pipe 52 %, tensor pipe 21 %). 64 sequences of
-// 16000 tokens: 258 us, 4.6 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
+// instructions per 16 tokens at head size 128, of which 104 unpack codes and pairs; issue 60 %, integer pipe 54 %, tensor pipe 21 %). 64 sequences of
+// 16000 tokens: 271 us, 4.4 TB/s; the 2.9 us in front of the first copies and the 7 us behind the last tile are what shorter calls feel.
 // So everything is arranged around the stream of tiles. The tiles of all (sequence, key
 // head, row tile) segments form one line of units, kSegmentCost more to a segment for what starting one takes, and every WARP of the grid
 // takes an equal stretch of it, whatever the lengths are, through a ring of its own that bulk copies fill. A segment inside a stretch is
 // written out by its warp; what spans warps of a CTA is joined in shared memory; what spans CTAs leaves (m, sum, o) in the workspace,
 // at most two parts a CTA, and a second kernel joins those. (With tiles dealt out to the eight warps of a CTA, which met at the end of each
-// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 22: a CTA had up to 40 segments one after another.)
+// segment, 33 sequences of 17 to 1500 tokens with 16 heads took 85 us against 22, and 20 now: a CTA had up to 40 segments one after another.)
 // Few and short segments need no such line: a cluster of CTAs has one each and joins it over its shared memory (one user's step, 1000 tokens, with
-// the write in front of it: 12.4 us against 16).
+// the write in front of it: 11.5 us against 13.9).
 #include <float.h>
 
 #include "cache.cuh"
@@ -51,8 +51,8 @@ constexpr uint32_t kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 constexpr uint32_t kMostCtas = 1024;      // what the workspace is laid out for
 constexpr uint32_t kLeastStretch = 2;     // units of a warp's stretch at least, and of a CTA's
 constexpr uint32_t kLeastCta = 8;
-// Of a sequence at most to a CTA of a cluster: 8000 tokens take 16 us by a cluster of 8 and as long by the line. And at least, before one more is worth it:
-// 16 tokens take 7.4 us by one CTA and 9.7 by eight, 1000 take 13.5 and 10.9.
+// Of a sequence at most to a CTA of a cluster: 8000 tokens take 13.6 us by a cluster of 8 and 15.4 by the line. And at least, before one more is worth it:
+// 16 tokens take 6.4 us by one CTA and 7.6 by eight, 1000 take 11.5 and 8.8.
 constexpr uint32_t kDirectTokens = 1024, kClusterTokens = 96;
 constexpr uint32_t kMostCluster = 8, kMostDirect = 128;     // CTAs that share a segment, and all of those
 // What a segment costs beside its tiles, in tiles. (Counted as 2, 4, 6 and 8: 64 users of 100 to 8000 tokens take 93.9, 84.4, 80.3 and 79.5 us, 128 of 50 to

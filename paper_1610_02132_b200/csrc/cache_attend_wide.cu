@@ -826,8 +826,8 @@ int launch_wide(const WideParams& p, cudaStream_t stream) {
 
 // A CTA has a row tile for itself, and all of its tokens, so that few tiles leave SMs idle, while cache_attend.cu spreads any rows over all SMs. A round of
 // tiles over the SMs takes 43, 131 and 247 us for 2048, 8192 and 16384 tokens at head size 128, however few or empty the tiles are; cache_attend.cu
-// 48, 113 and 207 for 4096 rows in all heads, 50, 127 and 231 for 4608, and 73, 211 and 398 for 8192. At head size 64: 35, 109 and 208 against 32, 77 and
-// 137 for 4608 rows, 42, 124 and 230 for 8192. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays. (The rows'
+// 46, 114 and 212 for 4096 rows in all heads, 48, 126 and 236 for 4608, and 69, 213 and 406 for 8192. At head size 64: 35, 109 and 208 against 30, 73 and
+// 132 for 4608 rows, 42, 120 and 224 for 8192. So the rows have to fill that part of the rounds' room, 18944 on 148 SMs, from which on it pays. (The rows'
 // average counts: one kernel has the whole call, a long run and single tokens beside it too.)
 bool cache_attend_wide_takes(const CacheView& view, uint32_t head_dim, int type, uint32_t q_heads) {
   if (type != QSGD_TYPE_BF16 || (head_dim != 64 && head_dim != 128) || !view.starts || !view.sequences) return false;
